@@ -231,6 +231,91 @@ int32_t mgrit_residual_norm_mixed(const mgrit_problem_t* p, const mgrit_fc_layer
                                   const float* b, const float* u0, const float* U, double* norm_out,
                                   void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- The rest of a training step: opening and closing layers, loss, gradient clipping.  u^0 comes from an opening layer,
+ * a closing layer turns u^N into logits, the loss and its gradient turn those into lambda^N (the closing layer's dX), and
+ * all gradients -- the stack's from the adjoint solve and those of the end layers -- are clipped together.  These layers
+ * are not square, so they are no part of a stack; every size is allowed.  As above: the caller owns every buffer, device
+ * pointers are aligned to 16 bytes unless stated otherwise (so that a state inside U will do), work is enqueued on `hip_stream` of the current device, nothing
+ * is allocated, and a call without host outputs is kernel launches only and may be recorded into a graph (the same rule of a
+ * first call outside the capture).  Arrays are row-major without gaps; outputs may not overlap inputs or each other except
+ * where it is said.  Two calls that may overlap in time need a workspace each.  Results do not depend on the run: no sum is formed in an
+ * order that changes from one call to the next. */
+enum { MGRIT_ACT_IDENTITY = 2 };                           /* with MGRIT_ACT_TANH and _RELU; end layers only */
+
+/* An affine layer with activation, residual and step:
+ *   z = X W^T + b,  Y = R + scale act(z),  D = scale act'(z)      X [M][K], W [F][K], b [F], R, Y, D [M][F]
+ * (ReLU'(0) = 0; a NaN stays a NaN in every activation).  Types: X (and dX) xtype, W wtype, and R, Y, D, dY ytype, each MGRIT_FP32 or
+ * MGRIT_BF16; b, dW and db are float.  Operands enter the products as they are stored, sums are float: bf16 operands are
+ * not rounded again and float ones not rounded at all (unlike the solver's, whose MGRIT_BF16 rounds the state). */
+typedef struct mgrit_affine {
+  int32_t M;           /* rows (samples), >= 0; with 0 rows only dW and db are written, as zero                  */
+  int32_t K, F;        /* inputs and outputs per row, >= 1                                                       */
+  int32_t act;         /* MGRIT_ACT_TANH, _RELU or _IDENTITY                                                     */
+  int32_t xtype, wtype, ytype;
+  float   scale;       /* finite                                                                                 */
+} mgrit_affine_t;
+
+/* Workspace of the forward and of the backward pass; 0 if the layer is invalid or needs none (then the workspace
+ * pointer may be NULL; mgrit_affine_forward tells an invalid layer by its code).  Host only. */
+size_t  mgrit_affine_workspace_bytes(const mgrit_affine_t* p);
+size_t  mgrit_affine_backward_workspace_bytes(const mgrit_affine_t* p);
+
+/*   X, W      device, read only
+ *   b         device float or NULL (no bias)         R   device or NULL (no residual); may be Y itself
+ *   Y         device, out                            D   device, out, or NULL: the factors that the backward pass takes
+ * Errors: MGRIT_ERR_POINTER, _PROBLEM, _WORKSPACE, _HIP; MGRIT_ERR_UNSUPPORTED if an array has more than 2^38 elements. */
+int32_t mgrit_affine_forward(const mgrit_affine_t* p, const void* X, const void* W, const float* b, const void* R,
+                             void* Y, void* D, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* G = dY * D (entry by entry; D NULL: G = scale dY, for the identity only),
+ *   dX = G W,  dW = G^T X,  db = sum over the rows of G            (the residual's gradient is dY itself)
+ *   dX, dW, db  device, overwritten; each may be NULL if it is not wanted.  X is read for dW only and may be NULL without
+ *               it; likewise W for dX.
+ * G is not rounded: a product of two bf16 values enters the sums as it is. */
+int32_t mgrit_affine_backward(const mgrit_affine_t* p, const void* X, const void* W, const void* D, const void* dY,
+                              void* dX, float* dW, float* db, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Softmax cross-entropy of logits x [B][V] (type dtype) against labels [B]:
+ *   row r:  l_r = log(sum_v exp(x_rv)) - x_r,label(r),   loss = scale * sum of l_r, or with MGRIT_LOSS_MEAN of the mean over the
+ *   counted rows;   grad_rv = d loss / d x_rv
+ * A row with a negative label does not count: l_r = 0 and a zero gradient, whatever its logits hold.  If no row counts the loss
+ * is 0.  Logits of minus infinity take part as probability zero; a row whose label is such a class has l_r = +infinity and the
+ * gradient of the formula, a row that holds a NaN, +infinity or nothing but minus infinity has NaN for both.  A label of V or
+ * more gives its row NaN, too, and reads nothing out of range. */
+enum { MGRIT_LOSS_SUM = 0, MGRIT_LOSS_MEAN = 1 };
+typedef struct mgrit_loss {
+  int32_t B, V;        /* rows >= 0, classes >= 1                                                                */
+  int32_t dtype;       /* of logits and grad: MGRIT_FP32 or MGRIT_BF16                                           */
+  int32_t reduction;   /* MGRIT_LOSS_SUM or MGRIT_LOSS_MEAN                                                      */
+  float   scale;       /* finite                                                                                 */
+} mgrit_loss_t;
+
+size_t  mgrit_cross_entropy_workspace_bytes(const mgrit_loss_t* p);
+/*   logits    device, read only; int64 labels device        loss   device float [1] or NULL
+ *   row_loss  device float [B] (l_r, not scaled) or NULL    grad   device [B][V] or NULL; may be the logits themselves */
+int32_t mgrit_cross_entropy(const mgrit_loss_t* p, const void* logits, const int64_t* labels, float* loss,
+                            float* row_loss, void* grad, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Clipping of many gradients to one global norm:
+ *   norm = sqrt(sum over all tensors and entries of src^2),  dst = c src with c = norm > max_norm ? max_norm / norm : 1
+ * The squares are summed in double; c is rounded to float once and multiplies in float.  If the norm is not finite, c is 1,
+ * so that in-place gradients stay as they were.
+ *   tensors   host array of n descriptors, n >= 0; src and dst need the alignment of their element only.  dst may be src
+ *             (clipped in place), or NULL: the tensor counts and is not written.  Apart from that no dst may overlap any src.
+ *   max_norm  >= 0; infinity for the norm alone
+ *   norm      device float [1], or NULL (4-byte aligned)
+ *   norm_host host double or NULL: synchronises the stream, and MGRIT_ERR_NONFINITE tells a norm that is not finite */
+typedef struct mgrit_tensor {
+  const void* src;
+  void*       dst;
+  int64_t     count;   /* >= 0; with 0 the pointers are not looked at                                            */
+  int32_t     dtype;   /* MGRIT_FP32 or MGRIT_BF16                                                               */
+} mgrit_tensor_t;
+
+size_t  mgrit_clip_workspace_bytes(const mgrit_tensor_t* tensors, int32_t n);
+int32_t mgrit_clip_gradients(const mgrit_tensor_t* tensors, int32_t n, float max_norm, float* norm, double* norm_host,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Diagnostic launch tracing, off by default and the one piece of state the library keeps: between
  * mgrit_trace_begin() and mgrit_trace_end() every layer-step and gradient launch is bracketed by a
  * pair of HIP events on its stream.  mgrit_trace_end synchronises on the last event and returns,

@@ -10,4 +10,9 @@ from .binding import (  # noqa: F401
     mgrit_fas_forward_static, MGRIT_STATIC_SCRATCH_BYTES,
     mgrit_fc_layers_t, make_fc_layers, mgrit_workspace_bytes_mixed, mgrit_adjoint_workspace_bytes_mixed,
     mgrit_fas_forward_mixed, mgrit_fas_adjoint_mixed, mgrit_residual_norm_mixed,
+    MGRIT_ACT_TANH, MGRIT_ACT_RELU, MGRIT_ACT_IDENTITY, MGRIT_FP32, MGRIT_BF16, MGRIT_LOSS_SUM, MGRIT_LOSS_MEAN,
+    mgrit_affine_t, make_affine, mgrit_affine_workspace_bytes, mgrit_affine_backward_workspace_bytes,
+    mgrit_affine_forward, mgrit_affine_backward,
+    mgrit_loss_t, make_loss, mgrit_cross_entropy_workspace_bytes, mgrit_cross_entropy,
+    mgrit_tensor_t, make_tensor_list, mgrit_clip_workspace_bytes, mgrit_clip_gradients,
 )

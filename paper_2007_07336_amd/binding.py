@@ -42,6 +42,20 @@ class mgrit_fc_layers_t(ctypes.Structure):
                 ("dWfc", ctypes.c_void_p), ("dbfc", ctypes.c_void_p)]
 
 
+class mgrit_affine_t(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int32), ("K", ctypes.c_int32), ("F", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("xtype", ctypes.c_int32), ("wtype", ctypes.c_int32), ("ytype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class mgrit_loss_t(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reduction", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class mgrit_tensor_t(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -80,6 +94,22 @@ def lib() -> ctypes.CDLL:
         L.mgrit_fas_adjoint_mixed.restype = ctypes.c_int32
         L.mgrit_residual_norm_mixed.argtypes = [P, F, vp, vp, vp, vp, dp, vp, ctypes.c_size_t, vp]
         L.mgrit_residual_norm_mixed.restype = ctypes.c_int32
+        A, X, T = ctypes.POINTER(mgrit_affine_t), ctypes.POINTER(mgrit_loss_t), ctypes.POINTER(mgrit_tensor_t)
+        for name in ("mgrit_affine_workspace_bytes", "mgrit_affine_backward_workspace_bytes"):
+            getattr(L, name).argtypes = [A]
+            getattr(L, name).restype = ctypes.c_size_t
+        L.mgrit_affine_forward.argtypes = [A, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mgrit_affine_forward.restype = ctypes.c_int32
+        L.mgrit_affine_backward.argtypes = [A, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mgrit_affine_backward.restype = ctypes.c_int32
+        L.mgrit_cross_entropy_workspace_bytes.argtypes = [X]
+        L.mgrit_cross_entropy_workspace_bytes.restype = ctypes.c_size_t
+        L.mgrit_cross_entropy.argtypes = [X, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mgrit_cross_entropy.restype = ctypes.c_int32
+        L.mgrit_clip_workspace_bytes.argtypes = [T, ctypes.c_int32]
+        L.mgrit_clip_workspace_bytes.restype = ctypes.c_size_t
+        L.mgrit_clip_gradients.argtypes = [T, ctypes.c_int32, ctypes.c_float, vp, dp, vp, ctypes.c_size_t, vp]
+        L.mgrit_clip_gradients.restype = ctypes.c_int32
         L.mgrit_trace_begin.argtypes = []
         L.mgrit_trace_begin.restype = None
         L.mgrit_trace_end.argtypes = [dp, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64), dp,
@@ -242,6 +272,152 @@ def mgrit_residual_norm_mixed(p: mgrit_problem_t, fc: mgrit_fc_layers_t, W, b, u
     if check and rc != MGRIT_OK:
         raise MgritError(rc, "mgrit_residual_norm_mixed")
     return rc, out.value
+
+
+# ---- the rest of a training step: end layers, loss, clipping
+MGRIT_ACT_TANH, MGRIT_ACT_RELU, MGRIT_ACT_IDENTITY = 0, 1, 2
+MGRIT_FP32, MGRIT_BF16 = 0, 1
+MGRIT_LOSS_SUM, MGRIT_LOSS_MEAN = 0, 1
+
+
+def _torch_type(t: int):
+    import torch
+    return {MGRIT_FP32: torch.float32, MGRIT_BF16: torch.bfloat16}.get(t)
+
+
+def _check(where, **tensors):
+    """tensors: name = (tensor or None, number of values, torch type).  What the C side cannot see of a tensor: that it
+    has this many values of this type one behind the other, on the GPU of the others.  Returns that GPU, which the call
+    runs on whatever the current one is."""
+    given = [(name, v) for name, v in tensors.items() if v[0] is not None]
+    for name, (t, count, dtype) in given:
+        if dtype is None or t.dtype != dtype:
+            raise ValueError(f"{where}: {name} has type {t.dtype}, not {dtype}")
+        if count is not None and t.numel() != count:
+            raise ValueError(f"{where}: {name} has {t.numel()} values, not {count}")
+        if not t.is_contiguous():
+            raise ValueError(f"{where}: {name} is not contiguous")
+    device = None
+    for name, (t, _, _) in given:
+        if not t.is_cuda:
+            raise ValueError(f"{where}: {name} is not on a GPU")
+        if device is not None and t.device != device:
+            raise ValueError(f"{where}: {name} is on {t.device}, others on {device}")
+        device = t.device
+    return device
+
+
+def _call(where, device, stream, check, call):
+    """call(stream handle) on `device`, on `stream` or that device's current stream."""
+    import torch
+    if device is None:
+        raise ValueError(f"{where}: no tensor given")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"{where}: the stream is on {stream.device}, the tensors on {device}")
+    with torch.cuda.device(device):
+        rc = call(_stream(stream))
+    if check and rc != MGRIT_OK:
+        raise MgritError(rc, where)
+    return rc
+
+
+def _size(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def make_affine(*, M, K, F, act=MGRIT_ACT_IDENTITY, xtype=MGRIT_FP32, wtype=MGRIT_FP32, ytype=MGRIT_FP32, scale=1.0) -> mgrit_affine_t:
+    return mgrit_affine_t(M=M, K=K, F=F, act=act, xtype=xtype, wtype=wtype, ytype=ytype, scale=scale)
+
+
+def mgrit_affine_workspace_bytes(p: mgrit_affine_t) -> int:
+    return int(lib().mgrit_affine_workspace_bytes(ctypes.byref(p)))
+
+
+def mgrit_affine_backward_workspace_bytes(p: mgrit_affine_t) -> int:
+    return int(lib().mgrit_affine_backward_workspace_bytes(ctypes.byref(p)))
+
+
+def mgrit_affine_forward(p: mgrit_affine_t, X, W, b, R, Y, D, workspace, *, stream=None, check=True):
+    """Y = R + scale act(X W^T + b), D = scale act'(..): b, R, D may be None, and the workspace where none is needed."""
+    where, (x, w, y) = "mgrit_affine_forward", map(_torch_type, (p.xtype, p.wtype, p.ytype))
+    device = _check(where, X=(X, p.M * p.K, x), W=(W, p.F * p.K, w), b=(b, p.F, _torch_type(0)), R=(R, p.M * p.F, y),
+                    Y=(Y, p.M * p.F, y), D=(D, p.M * p.F, y), workspace=(workspace, None, workspace is not None and workspace.dtype))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_affine_forward(
+        ctypes.byref(p), _ptr(X), _ptr(W), _ptr(b), _ptr(R), _ptr(Y), _ptr(D), _ptr(workspace), _size(workspace), s))
+
+
+def mgrit_affine_backward(p: mgrit_affine_t, X, W, D, dY, dX, dW, db, workspace, *, stream=None, check=True):
+    """With G = dY * D (D None, identity only: scale dY): dX = G W, dW = G^T X, db = column sums of G; each may be None."""
+    where, (x, w, y) = "mgrit_affine_backward", map(_torch_type, (p.xtype, p.wtype, p.ytype))
+    f = _torch_type(0)
+    device = _check(where, X=(X, p.M * p.K, x), W=(W, p.F * p.K, w), D=(D, p.M * p.F, y), dY=(dY, p.M * p.F, y), dX=(dX, p.M * p.K, x),
+                    dW=(dW, p.F * p.K, f), db=(db, p.F, f), workspace=(workspace, None, workspace is not None and workspace.dtype))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_affine_backward(
+        ctypes.byref(p), _ptr(X), _ptr(W), _ptr(D), _ptr(dY), _ptr(dX), _ptr(dW), _ptr(db), _ptr(workspace), _size(workspace), s))
+
+
+def make_loss(*, B, V, dtype=MGRIT_FP32, reduction=MGRIT_LOSS_MEAN, scale=1.0) -> mgrit_loss_t:
+    return mgrit_loss_t(B=B, V=V, dtype=dtype, reduction=reduction, scale=scale)
+
+
+def mgrit_cross_entropy_workspace_bytes(p: mgrit_loss_t) -> int:
+    return int(lib().mgrit_cross_entropy_workspace_bytes(ctypes.byref(p)))
+
+
+def mgrit_cross_entropy(p: mgrit_loss_t, logits, labels, loss, row_loss, grad, workspace, *, stream=None, check=True):
+    """loss (1 value), row_loss (B) and grad (like logits, may be logits) may each be None; labels are int64."""
+    import torch
+    where, t, f = "mgrit_cross_entropy", _torch_type(p.dtype), torch.float32
+    device = _check(where, logits=(logits, p.B * p.V, t), labels=(labels, p.B, torch.int64), loss=(loss, 1, f), row_loss=(row_loss, p.B, f),
+                    grad=(grad, p.B * p.V, t), workspace=(workspace, None, workspace is not None and workspace.dtype))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_cross_entropy(
+        ctypes.byref(p), _ptr(logits), _ptr(labels), _ptr(loss), _ptr(row_loss), _ptr(grad), _ptr(workspace), _size(workspace), s))
+
+
+class TensorList:
+    """Tensors to clip: the descriptors handed to the library, and the tensors, which are kept alive."""
+
+    def __init__(self, src: Sequence, dst: Optional[Sequence] = None):
+        where, dst = "make_tensor_list", list(src) if dst is None else list(dst)
+        self.src, self.dst = list(src), dst
+        if len(self.src) != len(self.dst):
+            raise ValueError(f"{where}: {len(self.src)} tensors, {len(self.dst)} results")
+        self.array = (mgrit_tensor_t * max(1, len(self.src)))()
+        self.device = None
+        for i, (a, b) in enumerate(zip(self.src, self.dst)):
+            kind = [k for k in (MGRIT_FP32, MGRIT_BF16) if _torch_type(k) == a.dtype]
+            if not kind:
+                raise ValueError(f"{where}: tensor {i} has type {a.dtype}")
+            device = _check(where, **{f"tensor {i}": (a, None, a.dtype), f"result {i}": (b, a.numel(), a.dtype)})
+            if self.device is not None and device != self.device:
+                raise ValueError(f"{where}: tensor {i} is on {device}, others on {self.device}")
+            self.device = device
+            self.array[i] = mgrit_tensor_t(src=_ptr(a), dst=_ptr(b), count=a.numel(), dtype=kind[0])
+
+    def __len__(self):
+        return len(self.src)
+
+
+def make_tensor_list(src: Sequence, dst: Optional[Sequence] = None) -> TensorList:
+    """Tensors and where their clipped values go (None: into themselves; a None among dst: that tensor only counts)."""
+    return TensorList(src, dst)
+
+
+def mgrit_clip_workspace_bytes(tensors: TensorList) -> int:
+    return int(lib().mgrit_clip_workspace_bytes(tensors.array, len(tensors)))
+
+
+def mgrit_clip_gradients(tensors: TensorList, max_norm: float, norm, workspace, *, want_norm=False, stream=None, check=True):
+    """dst = src * min(1, max_norm / norm).  norm: one float on the GPU or None.  Returns (return code, the norm if want_norm, which
+    waits for the GPU)."""
+    import torch
+    where, host = "mgrit_clip_gradients", ctypes.c_double(0.0)
+    device = _check(where, norm=(norm, 1, torch.float32), workspace=(workspace, None, workspace is not None and workspace.dtype))
+    if device is not None and tensors.device is not None and device != tensors.device:
+        raise ValueError(f"{where}: norm or workspace on {device}, the tensors on {tensors.device}")
+    rc = _call(where, device or tensors.device, stream, check, lambda s: lib().mgrit_clip_gradients(
+        tensors.array, len(tensors), max_norm, _ptr(norm), ctypes.byref(host) if want_norm else None, _ptr(workspace), _size(workspace), s))
+    return rc, host.value if want_norm else None
 
 
 TRACE_CLASSES = ("dense_step_kernel<float,64,64>", "dense_step_kernel<float,128,128>",

@@ -1,0 +1,148 @@
+// Global norm of many tensors, and their scaling to at most a given norm.
+#include "mgrit_device.h"
+#include "mgrit_ops.h"
+
+namespace mgrit {
+
+namespace {
+
+constexpr int TH = 256, GRID = 2048;
+constexpr long long CHUNK = 4096;               // entries: a workgroup takes consecutive chunks, none across two tensors
+
+struct Entry {
+  const void* src;
+  void* dst;
+  long long count, chunk0;                      // chunk0: chunks of the tensors before
+  long long type;
+};
+constexpr int PER = 96;                         // entries that fit a kernel's arguments (4 KB)
+struct Entries { Entry e[PER]; };
+struct Space { double norm; double partial[GRID]; Entry table[1]; };
+
+// The list of tensors goes to the workspace by kernel arguments, which a captured graph keeps, in as many launches as it takes.
+__global__ __launch_bounds__(PER) void clip_table_kernel(Entries in, Entry* out, int n) {
+  if ((int)threadIdx.x < n) out[threadIdx.x] = in.e[threadIdx.x];
+}
+
+__device__ __forceinline__ float value(float v) { return v; }
+__device__ __forceinline__ float value(__bf16 v) { return static_cast<float>(v); }
+template <typename T> struct Vec { static constexpr int N = 16 / (int)sizeof(T); T v[N]; };
+template <typename T> struct __attribute__((packed)) AnyVec { Vec<T> v; };       // at any address
+
+// Calls run(entry, first, last) for this workgroup's share of every tensor
+template <typename R>
+__device__ __forceinline__ void for_share(const Entry* table, int n, long long chunks, R run) {
+  long long c = chunks * blockIdx.x / gridDim.x;
+  const long long c1 = chunks * (blockIdx.x + 1) / gridDim.x;
+  if (c >= c1) return;
+  int lo = 0, hi = n - 1;                       // the tensor that chunk c belongs to
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (table[mid].chunk0 <= c) lo = mid; else hi = mid - 1;
+  }
+  for (int t = lo; t < n && c < c1; ++t) {
+    const Entry e = table[t];
+    const long long of = c - e.chunk0, all = (e.count + CHUNK - 1) / CHUNK, take = all - of < c1 - c ? all - of : c1 - c;
+    const long long first = of * CHUNK, last = first + take * CHUNK < e.count ? first + take * CHUNK : e.count;
+    run(e, first, last);
+    c += take;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ double square_sum(const T* p, long long first, long long last) {
+  constexpr int N = Vec<T>::N;
+  const long long nv = (last - first) / N;
+  const T* q = p + first;
+  double s = 0.0;
+  for (long long v = threadIdx.x; v < nv; v += TH) {
+    const Vec<T> a = reinterpret_cast<const AnyVec<T>*>(q + v * N)->v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) { const double d = (double)value(a.v[i]); s += d * d; }
+  }
+  const long long at = nv * N + threadIdx.x;
+  if (at < last - first) { const double d = (double)value(q[at]); s += d * d; }
+  return s;
+}
+
+// Sum over the workgroup in a fixed order; thread 0 has it.
+__device__ __forceinline__ double workgroup_sum(double s) {
+  __shared__ double part[TH / 64];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+#pragma unroll
+  for (int w = 0; w < TH / 64; ++w) s += part[w];
+  return s;
+}
+
+__global__ __launch_bounds__(TH) void clip_norm_kernel(const Entry* table, int n, long long chunks, double* partial) {
+  double s = 0.0;
+  for_share(table, n, chunks, [&](const Entry& e, long long first, long long last) {
+    s += e.type ? square_sum(static_cast<const __bf16*>(e.src), first, last) : square_sum(static_cast<const float*>(e.src), first, last);
+  });
+  s = workgroup_sum(s);
+  if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_share(const T* src, T* dst, long long first, long long last, float c) {
+  constexpr int N = Vec<T>::N;
+  const long long nv = (last - first) / N;
+  for (long long v = threadIdx.x; v < nv; v += TH) {
+    Vec<T> a = reinterpret_cast<const AnyVec<T>*>(src + first + v * N)->v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.v[i] = static_cast<T>(value(a.v[i]) * c);
+    reinterpret_cast<AnyVec<T>*>(dst + first + v * N)->v = a;
+  }
+  const long long at = first + nv * N + threadIdx.x;
+  if (at < last) dst[at] = static_cast<T>(value(src[at]) * c);
+}
+
+// Every workgroup adds the partial sums up for itself, in the same order, which costs less than a launch between the two.
+__global__ __launch_bounds__(TH) void clip_scale_kernel(const Entry* table, int n, long long chunks, const double* partial, int parts, double* norm_out,
+                                                       float* norm, float max_norm) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += TH) s += partial[i];
+  const double nrm = sqrt(workgroup_sum(s));
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *norm_out = nrm;
+    if (norm) *norm = (float)nrm;
+  }
+  const float c = nrm > (double)max_norm && nrm < INFINITY ? (float)((double)max_norm / nrm) : 1.0f;
+  for_share(table, n, chunks, [&](const Entry& e, long long first, long long last) {
+    if (!e.dst || (c == 1.0f && e.dst == e.src)) return;
+    if (e.type) scale_share(static_cast<const __bf16*>(e.src), static_cast<__bf16*>(e.dst), first, last, c);
+    else scale_share(static_cast<const float*>(e.src), static_cast<float*>(e.dst), first, last, c);
+  });
+}
+
+}  // namespace
+
+size_t clip_workspace(int n, const ClipTensor*) { return sizeof(Space) + (size_t)n * sizeof(Entry); }
+
+hipError_t launch_clip(int n, const ClipTensor* t, float max_norm, float* norm, void* ws, const double** norm_dev, hipStream_t s) {
+  Space* sp = static_cast<Space*>(ws);
+  long long chunks = 0;
+  bool any = false;
+  for (int i = 0; i < n; i += PER) {
+    Entries in = {};
+    const int k = n - i < PER ? n - i : PER;
+    for (int j = 0; j < k; ++j) {
+      in.e[j] = Entry{t[i + j].src, t[i + j].dst, t[i + j].count, chunks, t[i + j].type};
+      chunks += (t[i + j].count + CHUNK - 1) / CHUNK;
+      any = any || t[i + j].dst;
+    }
+    hipLaunchKernelGGL(clip_table_kernel, dim3(1), dim3(PER), 0, s, in, sp->table + i, k);
+  }
+  const int grid = chunks < GRID ? (int)chunks : GRID;
+  if (grid > 0) hipLaunchKernelGGL(clip_norm_kernel, dim3((unsigned)grid), dim3(TH), 0, s, sp->table, n, chunks, sp->partial);
+  hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)(any ? grid : 1)), dim3(TH), 0, s, sp->table, any ? n : 0, any ? chunks : 0, sp->partial, grid, &sp->norm,
+                     norm, max_norm);
+  *norm_dev = &sp->norm;
+  return hipGetLastError();
+}
+
+}  // namespace mgrit

@@ -1,0 +1,200 @@
+"""End layers (mgrit_affine_forward, mgrit_affine_backward) against 64-bit products, entry by entry, with bounds that follow
+from the operands and the number of additions."""
+import pytest
+import torch
+
+import paper_2007_07336_amd as M
+from tests.ops_util import Affine, normal, near, sum_bound
+
+pytestmark = pytest.mark.gpu
+
+# rows, inputs, outputs: single values, rows and columns; sizes around 16, 32, 64 and 128; odd ones; heads with few classes; long sums
+SHAPES = [(1, 1, 1), (1, 7, 3), (3, 1, 5), (2, 9, 1), (5, 33, 10), (16, 64, 16), (17, 65, 15), (31, 31, 33), (32, 128, 64), (33, 100, 65),
+          (64, 256, 10), (65, 257, 129), (100, 784, 96), (128, 64, 127), (1, 1000, 500), (4, 2049, 10), (129, 30, 300), (257, 515, 70),
+          (7, 5000, 2), (300, 3, 3)]
+TYPES = ["fff", "bbb", "fbf", "bbf", "ffb", "bff"]
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("rows,K,F", SHAPES)
+def test_forward(rows, K, F, types):
+    Affine(rows, K, F, types, "identity").check_forward()
+    Affine(rows, K, F, types, "tanh", 0.25, residual=True, seed=10).check_forward(factor=True)
+    Affine(rows, K, F, types, "relu", -1.5, bias=False, seed=20).check_forward(factor=True)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("rows,K,F", SHAPES)
+def test_backward(rows, K, F, types):
+    Affine(rows, K, F, types, "identity", 0.75).check_backward(None)
+    a = Affine(rows, K, F, types, "tanh", 0.5, seed=10)
+    a.check_backward(a.forward(factor=True)[1])
+
+
+# sizes that the kernels for many rows, wide layers and long sums take
+@pytest.mark.parametrize("types", ["fff", "bbb", "fbf", "bbf"])
+@pytest.mark.parametrize("rows,K,F", [(512, 512, 512), (513, 520, 500), (1024, 256, 384), (300, 1111, 777), (2048, 64, 256), (256, 2048, 1000),
+                                      (1000, 704, 1290), (32, 4096, 4096), (32, 20000, 10), (2000, 1024, 10), (640, 10, 2000), (16, 520, 9000)])
+def test_large(rows, K, F, types):
+    a = Affine(rows, K, F, types, "tanh", 0.5, residual=True)
+    _, D = a.check_forward(factor=True)
+    a.check_backward(D)
+    Affine(rows, K, F, types, "identity", seed=3).check_backward(None)
+
+
+def test_gradients_against_differences():
+    """d/dt of the sum of dY * Y along random directions of X, W and b, from float64 differences of the plain form."""
+    a = Affine(37, 50, 21, "fff", "tanh", 0.5)
+    dX, dW, db = a.backward(a.forward(factor=True)[1])
+
+    def value(t, vX, vW, vb):
+        z = (a.X.double() + t * vX) @ (a.W.double() + t * vW).T + a.b.double() + t * vb
+        return float((a.dY.double() * 0.5 * torch.tanh(z)).sum())
+
+    for seed in range(4):
+        vX, vW, vb = (normal(t.shape, 1.0, "f", 100 + 3 * seed + i).double() for i, t in enumerate((a.X, a.W, a.b)))
+        h = 1e-5
+        want = (value(h, vX, vW, vb) - value(-h, vX, vW, vb)) / (2 * h)
+        got = float((dX.double() * vX).sum() + (dW.double() * vW).sum() + (db.double() * vb).sum())
+        size = float((dX.double() * vX).abs().sum() + (dW.double() * vW).abs().sum() + (db.double() * vb).abs().sum())
+        # sums of at most 50 + 2 products; the differences are off by h^2 of a third derivative below the size, and 1e-16 / h
+        assert abs(got - want) <= (60 * 2.0 ** -23 + 1e-8) * size
+
+
+def test_outputs_that_are_not_wanted():
+    a = Affine(40, 72, 33, "fff", "identity")
+    dX, dW, db = a.backward(None)
+    for keep in ("dX", "dW", "db"):
+        o = {"dX": a.new((40, 72)), "dW": a.new((33, 72)), "db": a.new((33,))}
+        M.mgrit_affine_backward(a.p, a.X if keep == "dW" else None, a.W if keep == "dX" else None, None, a.dY,
+                                *(o[k] if k == keep else None for k in ("dX", "dW", "db")), a.ws)
+        assert torch.equal(o[keep], {"dX": dX, "dW": dW, "db": db}[keep])
+
+
+@pytest.mark.parametrize("types,rows,K,F", [("fff", 70, 130, 90), ("bbb", 600, 512, 512), ("fbf", 8, 4096, 10)])
+def test_residual_may_be_the_output(types, rows, K, F):
+    a = Affine(rows, K, F, types, "tanh", residual=True)
+    Y, _ = a.forward()
+    R = a.R.clone()
+    M.mgrit_affine_forward(a.p, a.X, a.W, a.b, R, R, None, a.ws)
+    assert torch.equal(R, Y)
+
+
+@pytest.mark.parametrize("types", ["fff", "bbb", "fbf"])
+@pytest.mark.parametrize("rows,K,F", [(6, 40, 10), (130, 200, 150), (512, 512, 512), (32, 4096, 64)])
+def test_infinities_and_nan_stay_in_their_rows_and_columns(rows, K, F, types):
+    a = Affine(rows, K, F, types)
+    a.X[1, 3] = float("inf")
+    a.X[2, 0] = float("nan")
+    a.W[5, 7] = float("-inf")
+    a.dY[4, 2] = float("inf")
+    Y, _ = a.forward()
+    z = a.X.double() @ a.W.double().T + a.b.double()
+    fine = torch.isfinite(z)
+    bound = sum_bound(a.X.double().nan_to_num(0, 0, 0), a.W.double().nan_to_num(0, 0, 0), K) + 2.0 ** -22 * z.abs().nan_to_num(0, 0, 0)
+    near(Y, z, torch.where(fine, bound, 0.0), "Y")
+    dX, dW, db = a.backward(None)
+    for got, want in ((dX, a.dY.double() @ a.W.double()), (dW, a.dY.double().T @ a.X.double()), (db, a.dY.double().sum(0))):
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+        assert torch.equal(got[torch.isinf(want)].double(), want[torch.isinf(want)])
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-18, 1e18, 3e37])
+@pytest.mark.parametrize("rows,K,F", [(40, 60, 30), (512, 512, 512)])
+def test_large_and_small_magnitudes(rows, K, F, size):
+    """Operands far from one: float sums keep their relative accuracy as long as products and sums are normal numbers."""
+    a = Affine(rows, K, F, "fff", "identity", bias=False)
+    a.X.mul_(size)
+    a.dY.mul_(size / 1e3)
+    a.check_forward()
+    dX, dW, db = a.new((rows, K)), None, a.new((F,))
+    M.mgrit_affine_backward(a.p, None, a.W, None, a.dY, dX, dW, db, a.ws)
+    near(dX, a.dY.double() @ a.W.double(), sum_bound(a.dY.double(), a.W.double().T, F + 2), "dX")
+
+
+def test_no_rows():
+    p = M.make_affine(M=0, K=5, F=3)
+    e = torch.empty((0, 5), device="cuda")
+    y = torch.empty((0, 3), device="cuda")
+    dW, db = torch.full((3, 5), 7.0, device="cuda"), torch.full((3,), 7.0, device="cuda")
+    W = torch.ones((3, 5), device="cuda")
+    assert M.mgrit_affine_forward(p, e, W, None, None, y, None, None) == 0
+    assert M.mgrit_affine_backward(p, e, W, None, y, e, dW, db, None) == 0
+    assert not dW.any() and not db.any()
+
+
+@pytest.mark.parametrize("rows,K,F,types", [(7, 33, 10, "fff"), (513, 520, 500, "bbb"), (32, 20000, 10, "fbf"), (300, 1111, 777, "fff"), (1, 512, 3000, "bbb")])
+def test_nothing_is_written_past_the_outputs(rows, K, F, types):
+    a = Affine(rows, K, F, types, "tanh")
+
+    def guarded(shape, t):
+        n, pad = shape[0] * (shape[1] if len(shape) > 1 else 1), 4096
+        whole = torch.full((n + 2 * pad,), 7.0, dtype=t, device="cuda")
+        return whole, whole[pad:pad + n].view(shape), pad
+
+    o = [guarded((rows, F), a.dY.dtype), guarded((rows, F), a.dY.dtype), guarded((rows, K), a.X.dtype), guarded((F, K), torch.float32),
+         guarded((F,), torch.float32)]
+    M.mgrit_affine_forward(a.p, a.X, a.W, a.b, None, o[0][1], o[1][1], a.ws)
+    M.mgrit_affine_backward(a.p, a.X, a.W, o[1][1], a.dY, o[2][1], o[3][1], o[4][1], a.ws)
+    for whole, inner, pad in o:
+        assert bool((whole[:pad] == 7.0).all()) and bool((whole[pad + inner.numel():] == 7.0).all())
+        assert not bool((inner == 7.0).all())
+
+
+@pytest.mark.parametrize("rows,K,F,types", [(48, 100, 60, "fff"), (512, 512, 512, "bbb"), (32, 8192, 10, "fbf"), (1, 1024, 4096, "bbb"), (300, 700, 500, "fff")])
+def test_captured_calls_replay_with_new_inputs(rows, K, F, types):
+    a = Affine(rows, K, F, types, "tanh", 0.5, residual=True)
+    Y, D = a.forward(factor=True)
+    outs = (Y, D) + a.backward(D)
+
+    def calls():
+        M.mgrit_affine_forward(a.p, a.X, a.W, a.b, a.R, Y, D, a.ws)
+        M.mgrit_affine_backward(a.p, a.X, a.W, D, a.dY, *outs[2:], a.ws)
+
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        calls()
+    torch.cuda.synchronize()
+    for replay in range(3):
+        a.X.copy_(normal((rows, K), 1.0, types[0], 50 + replay))
+        a.dY.copy_(normal((rows, F), 1.0, types[2], 60 + replay))
+        calls()
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.fill_(float("nan"))
+        a.ws is None or a.ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, w in zip(outs, want):
+            assert torch.equal(t, w), replay
+
+
+def test_another_stream_and_its_order():
+    """Work goes to the stream that is handed over, behind what it holds already."""
+    a = Affine(200, 300, 100, "fff", "identity")
+    X = a.X.clone()
+    want, _ = a.forward()
+    a.X.zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    Y = a.new((200, 100))
+    with torch.cuda.stream(side):
+        busy = torch.randn(2048, 2048, device="cuda")
+        for _ in range(8):
+            busy = busy @ busy * 1e-3
+        a.X.copy_(X)
+    M.mgrit_affine_forward(a.p, a.X, a.W, a.b, None, Y, None, a.ws, stream=side)
+    side.synchronize()
+    assert torch.equal(Y, want)
+
+
+def test_the_same_call_gives_the_same_bits():
+    for rows, K, F, types in ((100, 1031, 517, "fff"), (32, 20000, 10, "fbf"), (512, 640, 512, "bbb")):
+        a = Affine(rows, K, F, types, "tanh")
+        _, D = a.forward(factor=True)
+        first = a.backward(D)
+        for _ in range(3):
+            assert all(torch.equal(x, y) for x, y in zip(first, a.backward(D)))

@@ -1,0 +1,141 @@
+"""Clipping to a global norm (mgrit_clip_gradients) against 64-bit sums."""
+import math
+
+import pytest
+import torch
+
+import paper_2007_07336_amd as M
+from tests.ops_util import HALF, TINY, TYPES, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def _clip(src, dst, max_norm, norm=True, **kw):
+    t = M.make_tensor_list(src, dst)
+    ws = torch.full((M.mgrit_clip_workspace_bytes(t),), 0xFF, dtype=torch.uint8, device="cuda")
+    n = torch.full((1,), float("nan"), device="cuda") if norm else None
+    return (n,) + M.mgrit_clip_gradients(t, max_norm, n, ws, **kw)
+
+
+def _check(src, max_norm):
+    """Out of place, then in place: both as src * min(1, max_norm / norm) with one rounding of the factor to float, one of the product and
+    one to the type."""
+    norm = math.sqrt(sum(float((t.double() ** 2).sum()) for t in src))
+    dst = [torch.full_like(t, float("nan")) for t in src]
+    n, rc, host = _clip(src, dst, max_norm, want_norm=True)
+    assert rc == 0 and abs(host - norm) <= 1e-12 * norm + TINY
+    assert abs(float(n) - norm) <= 2.0 ** -24 * norm * 1.0001 + TINY
+    c = max_norm / norm if norm > max_norm else 1.0
+    for s, d in zip(src, dst):
+        want = s.double() * c
+        err = (d.double() - want).abs()
+        bound = want.abs() * ((2.0 ** -23 * 1.01 if c != 1.0 else 0.0) + (HALF[s.dtype] * 1.01 if s.dtype == torch.bfloat16 and c != 1.0 else 0.0)) + TINY
+        assert bool((err <= bound).all()), (s.shape, s.dtype)
+    own = [t.clone() for t in src]
+    n2, _, _ = _clip(own, None, max_norm)
+    assert torch.equal(n, n2)
+    for a, b in zip(own, dst):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("t", ["f", "b"])
+@pytest.mark.parametrize("max_norm", [0.0, 0.5, 1e6])
+@pytest.mark.parametrize("shapes", [[(1,)], [(3,), (1,), (1000,)], [(4095,), (4096,), (4097,)], [(256, 256, 8), (256, 8)], [(1 << 20,)], [(5000000,), (7,)]])
+def test_sizes(shapes, max_norm, t):
+    _check([normal(s, 1.0, t, i) for i, s in enumerate(shapes)], max_norm)
+
+
+@pytest.mark.parametrize("count", [2, 95, 96, 97, 193, 700])
+def test_many_tensors_of_both_types(count):
+    g = torch.Generator().manual_seed(count)
+    sizes = (torch.rand(count, generator=g) * 9).exp().int().tolist()
+    _check([normal((n,), 1e-3, "b" if i % 3 == 1 else "f", i) for i, n in enumerate(sizes)], 0.1)
+
+
+@pytest.mark.parametrize("t", ["f", "b"])
+def test_views_at_any_offset(t):
+    """Source and result at offsets of their own, one behind the other: what lies between and around stays."""
+    n, offs = 70000, [0, 1, 2, 3, 5, 6, 7, 8, 9, 13]
+    flat, out = normal((len(offs) * n + 64,), 1.0, t), torch.full((len(offs) * n + 64,), 7.0, dtype=TYPES[t], device="cuda")
+    src = [flat[i * n + o:i * n + o + n - 50] for i, o in enumerate(offs)]
+    back = offs[::-1]
+    dst = [out[i * n + o:i * n + o + n - 50] for i, o in enumerate(back)]
+    norm = math.sqrt(sum(float((s.double() ** 2).sum()) for s in src))
+    _clip(src, dst, norm / 4)
+    for s, d in zip(src, dst):
+        assert torch.equal(d, (s.float() * 0.25).to(s.dtype)) or float((d.double() - s.double() / 4).abs().max()) <= 2 * HALF[s.dtype] * float(s.abs().max())
+    kept = torch.ones_like(out, dtype=torch.bool)
+    for i, o in enumerate(back):
+        kept[i * n + o:i * n + o + n - 50] = False
+    assert bool((out[kept] == 7.0).all())
+
+
+def test_extremes_do_not_overflow_the_squares():
+    a = torch.full((1000,), 1e30, device="cuda")
+    n, rc, host = _clip([a], None, 1.0, want_norm=True)
+    assert abs(host / (1e30 * math.sqrt(1000)) - 1) < 1e-7
+    assert float((a.double() * math.sqrt(1000) - 1).abs().max()) < 1e-6
+    b = torch.full((1000,), 1e-30, device="cuda")
+    n, rc, host = _clip([b], None, 1.0, want_norm=True)
+    assert abs(host / (1e-30 * math.sqrt(1000)) - 1) < 1e-7 and bool((b == 1e-30).all())
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_a_norm_that_is_not_finite_leaves_the_gradients(bad):
+    a, b = normal((5000,)), normal((300,), 1.0, "b")
+    a[4321] = bad
+    keep = [a.clone(), b.clone()]
+    n, rc, host = _clip([a, b], None, 0.1, want_norm=True, check=False)
+    assert rc == -5 and not math.isfinite(host) and not math.isfinite(float(n))
+    out = [torch.zeros_like(a), torch.zeros_like(b)]
+    n, rc, _ = _clip([a, b], out, 0.1)
+    assert rc == 0
+    for x, y, z in zip((a, b), keep, out):
+        assert torch.equal(x.nan_to_num(0.5), y.nan_to_num(0.5)) and torch.equal(z.nan_to_num(0.5), y.nan_to_num(0.5))
+
+
+def test_empty_tensors_and_tensors_that_only_count():
+    a, b, e = normal((100,)), normal((200,), 1.0, "f", 1), torch.empty((0,), device="cuda")
+    keep = b.clone()
+    norm = math.sqrt(float((a.double() ** 2).sum() + (b.double() ** 2).sum()))
+    n, _, host = _clip([e, a, e, b], [e, a, None, None], norm / 2, want_norm=True)
+    assert abs(host - norm) < 1e-12 * norm and torch.equal(b, keep)
+    assert abs(float((a.double() ** 2).sum()) - float((normal((100,)).double() ** 2).sum()) / 4) < 1e-6 * norm ** 2
+    n, _, host = _clip([e], None, 1.0, want_norm=True)
+    assert host == 0.0 and float(n) == 0.0
+    n, _, host = _clip([b], [None], float("inf"), want_norm=True)
+    assert abs(host ** 2 - float((b.double() ** 2).sum())) < 1e-9 and torch.equal(b, keep)
+    z = torch.zeros((50,), device="cuda")
+    n, _, host = _clip([z], None, 0.0, want_norm=True)
+    assert host == 0.0 and not z.any()
+
+
+def test_no_tensors():
+    n = torch.full((1,), 5.0, device="cuda")
+    t = M.make_tensor_list([])
+    ws = torch.empty(M.mgrit_clip_workspace_bytes(t), dtype=torch.uint8, device="cuda")
+    assert M.mgrit_clip_gradients(t, 1.0, n, ws, want_norm=True)[1] == 0.0 and float(n) == 0.0
+
+
+def test_captured_calls_replay():
+    src = [normal((n,), 1.0, "b" if n % 2 else "f", n) for n in (3, 1000, 70001, 64)]
+    dst = [torch.empty_like(t) for t in src]
+    t = M.make_tensor_list(src, dst)
+    n = torch.empty((1,), device="cuda")
+    ws = torch.empty(M.mgrit_clip_workspace_bytes(t), dtype=torch.uint8, device="cuda")
+    M.mgrit_clip_gradients(t, 2.0, n, ws)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        M.mgrit_clip_gradients(t, 2.0, n, ws)
+    for replay in range(3):
+        for i, s in enumerate(src):
+            s.copy_(normal(s.shape, 1.0 + replay, "b" if s.dtype == torch.bfloat16 else "f", 40 + replay + i))
+        M.mgrit_clip_gradients(t, 2.0, n, ws)
+        want = [x.clone() for x in dst + [n]]
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, w) for x, w in zip(dst + [n], want)), replay
