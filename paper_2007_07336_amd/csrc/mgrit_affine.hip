@@ -53,6 +53,66 @@ __device__ __forceinline__ void finish(const Epilogue& e, long long at, long lon
   if (e.D) static_cast<OT*>(e.D)[at] = narrow<OT>(e.scale * o.d);
 }
 
+// Eight results of one row.  whole: all eight exist and lie on a multiple of eight
+template <typename T> struct Eight { T v[8]; };
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(p);
+  *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(p + 4);
+}
+__device__ __forceinline__ void load8(const __bf16* p, float (&v)[8]) {
+  const bf16x8 b = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = widen(b[k]);
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *reinterpret_cast<floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<floatx4*>(p + 4) = floatx4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(__bf16* p, const float (&v)[8]) {
+  bf16x8 b;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) b[k] = narrow<__bf16>(v[k]);
+  *reinterpret_cast<bf16x8*>(p) = b;
+}
+template <typename OT>
+__device__ __forceinline__ void put8(OT* p, const float (&v)[8], bool whole, long long left) {
+  if (whole) {
+    store8(p, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < left) p[k] = narrow<OT>(v[k]);
+  }
+}
+template <typename OT>
+__device__ __forceinline__ void finish8(const Epilogue& e, long long at, float (&v)[8], const float (&bias)[8], bool whole, long long left) {
+  OT* out = static_cast<OT*>(e.out) + at;
+  if (!e.fwd) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= e.scale;
+    put8(out, v, whole, left);
+    return;
+  }
+  float d[8], r[8];
+  if (e.R) {
+    const OT* R = static_cast<const OT*>(e.R) + at;
+    if (whole) {
+      load8(R, r);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r[k] = k < left ? widen(R[k]) : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const Out o = activate(v[k] + bias[k], e.act);
+    v[k] = e.R ? r[k] + e.scale * o.y : e.scale * o.y;
+    d[k] = e.scale * o.d;
+  }
+  put8(out, v, whole, left);
+  if (e.D) put8(static_cast<OT*>(e.D) + at, d, whole, left);
+}
+
 // ------------------------------------------------------------------------------------------ any size, any order
 // Tile of 64 x 64 outputs, four wavefronts with 32 x 32 of them each; slabs of the contraction go through registers (the
 // next one is in flight while this one is multiplied) into LDS, rows along k.  With float operands on the float matrix
@@ -231,6 +291,317 @@ hipError_t launch_types(const Product& q, float* partial, int parts, hipStream_t
   return launch_tiles<float, float, float, HF, AS, BS>(q, partial, parts, s);
 }
 
+// ------------------------------------------------------------------------------------------ large products
+// Operands as planes: rows along k, padded with zeros to whole slabs of 128 bytes (64 bf16 or 32 float), 16-byte pieces.  What the
+// caller has in this form is read in place; anything else -- transposed, ragged, with a factor, of another type -- is laid
+// out in the workspace first (lay_out_kernel), which costs a pass over the operand and keeps the multiplying loop free of
+// everything but multiplications.
+typedef __attribute__((address_space(3))) void LdsPtr;
+typedef __attribute__((address_space(1))) const void GlobalPtr;
+
+template <typename CT> struct Mma;
+template <> struct Mma<__bf16> {
+  typedef bf16x8 Frag;
+  static __device__ __forceinline__ void go(Frag a, Frag b, floatx16& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<float> {
+  typedef floatx4 Frag;       // (lanes 0-31 take four k, lanes 32-63 the next four, one each per instruction)
+  static __device__ __forceinline__ void go(Frag a, Frag b, floatx16& c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+  }
+};
+
+struct Plane {
+  const void* p;
+  long long ld;                // bytes from row to row
+  long long part;              // bytes from part to part
+};
+struct WideArgs {
+  Plane A, B;
+  Epilogue e;
+  long long I, J;
+  int slabs;                   // of one pass over the contraction
+  int passes;                  // pairs of parts that are multiplied: pass s takes A's part pa[s] and B's part pb[s]
+  int pa[6], pb[6];
+  int per;                     // slabs that one workgroup takes (blockIdx.y: which), all passes counted
+  float* partial;              // several workgroups: their sums
+};
+
+// Tile of BT x BT outputs, four wavefronts with a quarter each.  A slab of both operands is 2 BT rows of 128 bytes in LDS, its
+// 16-byte pieces in the order piece ^ (row & 7): the hardware writes LDS in lane order, so the lanes pick their pieces in that
+// order from memory, and eight lanes that read the same piece of eight rows meet different banks.  Two slabs are in LDS: while one
+// is multiplied in four steps, the next one is on its way.  Behind the last step's reads a barrier says that nobody needs the old slab
+// any more and that the next one has arrived; the loads of the one after go out at once and have a whole slab's time.
+template <typename CT, int BT, typename OT>
+__global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(WideArgs a) {
+  typedef typename Mma<CT>::Frag Frag;
+  constexpr int T = BT / 64, NL = BT / 32, SLAB = BT * 128;       // 32 x 32 tiles along a wavefront's side; loads per operand and slab
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave >> 1, wj = wave & 1;
+  // tiles in groups of GM rows of tiles, so that the tiles that an XCD works on at a time share few panels of both operands
+  constexpr int GM = 4;
+  const long long ti = (a.I + BT - 1) / BT, tj = (a.J + BT - 1) / BT;
+  const long long L = logical_block(), group = L / (GM * tj), first = group * GM, size = ti - first < GM ? ti - first : GM, in = L - group * GM * tj;
+  const long long i0 = (first + in % size) * BT, j0 = in / size * BT;
+
+  const int total = a.slabs * a.passes, t0 = (int)blockIdx.y * a.per, t1 = t0 + a.per < total ? t0 + a.per : total;
+  unsigned offA[NL], offB[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
+    const long long ra = i0 + r < a.I ? r : a.I - 1 - i0, rb = j0 + r < a.J ? r : a.J - 1 - j0;
+    offA[i] = (unsigned)(ra * a.A.ld) + piece * 16;
+    offB[i] = (unsigned)(rb * a.B.ld) + piece * 16;
+  }
+  const char* baseA = static_cast<const char*>(a.A.p) + i0 * a.A.ld;
+  const char* baseB = static_cast<const char*>(a.B.p) + j0 * a.B.ld;
+  int pass = t0 / a.slabs, slab = t0 - pass * a.slabs;           // of the next slab to load
+  auto issue = [&](int buf) {
+    const char* pa = baseA + a.pa[pass] * a.A.part + slab * 128LL;
+    const char* pb = baseB + a.pb[pass] * a.B.part + slab * 128LL;
+    unsigned char* la = lds + buf * 2 * SLAB + wave * (BT / 4) * 128;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) __builtin_amdgcn_global_load_lds((GlobalPtr*)(pa + offA[i]), (LdsPtr*)(la + i * 1024), 16, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) __builtin_amdgcn_global_load_lds((GlobalPtr*)(pb + offB[i]), (LdsPtr*)(la + SLAB + i * 1024), 16, 0, 0);
+    if (++slab == a.slabs) { slab = 0; ++pass; }
+  };
+  const int c = lane & 31, g = lane >> 5;
+  const unsigned char* readA = lds + (wi * (BT / 2) + c) * 128;
+  const unsigned char* readB = lds + SLAB + (wj * (BT / 2) + c) * 128;
+  Frag fa[2][T], fb[2][T];
+  auto read = [&](int buf, int step, int set) {
+    const int at = buf * 2 * SLAB + (((2 * step + g) ^ (c & 7)) << 4);
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      fa[set][i] = *reinterpret_cast<const Frag*>(readA + at + i * 32 * 128);
+      fb[set][i] = *reinterpret_cast<const Frag*>(readB + at + i * 32 * 128);
+    }
+  };
+  floatx16 acc[T][T];
+#pragma unroll
+  for (int i = 0; i < T; ++i)
+#pragma unroll
+    for (int j = 0; j < T; ++j) acc[i][j] = zero16();
+
+  issue(0);
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  if (t0 + 1 < t1) issue(1);
+  read(0, 0, 0);
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+#pragma unroll
+    for (int step = 0; step < 4; ++step) {
+      if (step < 3) {
+        read(buf, step + 1, (step + 1) & 1);
+      } else {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + 2 < t1) issue(buf);
+        if (t + 1 < t1) read(buf ^ 1, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int j = 0; j < T; ++j) Mma<CT>::go(fa[step & 1][i], fb[step & 1][j], acc[i][j]);
+    }
+  }
+
+  // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands
+  constexpr int W = BT / 2, PITCH = W + 4;
+  float* strip = reinterpret_cast<float*>(lds) + wave * 32 * PITCH;
+  const int lc = lane % (W / 8) * 8, lr = lane / (W / 8);
+  const long long col = j0 + wj * W + lc;
+  const long long n = a.I * a.J;
+  const bool whole = a.J % 8 == 0 && col + 8 <= a.J;
+  float bias[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) bias[k] = a.e.fwd && a.e.bias && !a.partial && col + k < a.J ? a.e.bias[col + k] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < T; ++i) {
+#pragma unroll
+    for (int j = 0; j < T; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) strip[((r & 3) + 8 * (r >> 2) + 4 * g) * PITCH + j * 32 + c] = acc[i][j][r];
+    __builtin_amdgcn_wave_barrier();
+    for (int r = lr; r < 32; r += 512 / W) {
+      const long long row = i0 + wi * W + i * 32 + r, at = row * a.J + col;
+      float v[8];
+      *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(strip + r * PITCH + lc);
+      *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(strip + r * PITCH + lc + 4);
+      if (row < a.I) {
+        if (a.partial) put8(a.partial + blockIdx.y * n + at, v, whole, a.J - col);
+        else finish8<OT>(a.e, at, v, bias, whole, a.J - col);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Operand -> planes: rows x (k padded to whole slabs) of CT, PARTS of them: 1 as it is (or widened); 2: the product of two bf16
+// values, 16 significant bits, is the sum of two.  Workgroup: 64 rows x 64 k; where rows are the fast index in memory they
+// change places in LDS.
+template <typename T, typename CT, int PARTS, bool HF, bool KSLOW>
+__global__ __launch_bounds__(256) void lay_out_kernel(const T* p, const T* f, long long ld, long long rows, long long Kc, CT* out, long long ldo, long long part) {
+  __shared__ float tile[64][65];
+  const long long kt = (ldo + 63) / 64, L = blockIdx.x;
+  const long long r0 = L / kt * 64, k0 = L % kt * 64;
+  const int t = threadIdx.x;
+  if (KSLOW) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = t % 16 * 4, k = t / 16 + 16 * i;
+      const long long at = (k0 + k) * ld + r0 + r, left = k0 + k < Kc ? rows - r0 - r : 0;
+      Four<T> a, b;
+      if (ld % 4 == 0 && left >= 4) {
+        a = *reinterpret_cast<const Four<T>*>(__builtin_assume_aligned(p + at, 4 * sizeof(T)));
+        if (HF) b = *reinterpret_cast<const Four<T>*>(__builtin_assume_aligned(f + at, 4 * sizeof(T)));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          a.v[j] = j < left ? p[at + j] : T(0.0f);
+          if (HF) b.v[j] = j < left ? f[at + j] : T(0.0f);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) tile[k][r + j] = HF ? widen(a.v[j]) * widen(b.v[j]) : widen(a.v[j]);
+    }
+    __syncthreads();
+  }
+  for (int n = t; n < 512; n += 256) {             // eight k of a row
+    const int r = n / 8, k = n % 8 * 8;
+    if (r0 + r >= rows || k0 + k >= ldo) continue;
+    float v[8];
+    if (KSLOW) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = tile[k + j][r];
+    } else {
+      const long long at = (r0 + r) * ld + k0 + k, left = Kc - k0 - k;
+      float b[8];
+      if (ld % 8 == 0 && left >= 8) {
+        load8(p + at, v);
+        if (HF) load8(f + at, b);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[j] = j < left ? widen(p[at + j]) : 0.0f;
+          if (HF) b[j] = j < left ? widen(f[at + j]) : 0.0f;
+        }
+      }
+      if (HF)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= b[j];
+    }
+    CT* o = out + (r0 + r) * ldo + k0 + k;
+    store8(o, v);
+    if (PARTS == 2) {
+      float lo[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) lo[j] = v[j] - widen(narrow<CT>(v[j]));
+      store8(o + part, lo);
+    }
+  }
+}
+
+template <typename CT> constexpr int slab_of() { return 128 / (int)sizeof(CT); }
+
+struct WidePlan {
+  bool wide, bf16;
+  int bt, slabs, passes, parts;       // parts: workgroups that share a tile's contraction
+  bool copyA, copyB;
+  long long ldp;                      // entries from row to row of a laid out plane
+  size_t offB, offP, bytes;
+};
+inline bool in_place(const Operand& o, bool bf16, long long Kc) {
+  const int slab = bf16 ? 64 : 32;
+  return !o.kslow && !o.f && (o.type != 0) == bf16 && Kc % slab == 0 && o.ld == Kc;
+}
+WidePlan wide_plan(const Product& q) {
+  WidePlan w = {};
+  const long long t128 = (q.I + 127) / 128 * ((q.J + 127) / 128);
+  w.wide = q.I >= 128 && q.J >= 128 && q.Kc >= 64 && t128 >= 16 && q.Kc < (1LL << 22) && t128 < (1LL << 30);
+  if (!w.wide) return w;
+  w.bf16 = q.A.type && q.B.type;
+  const int slab = w.bf16 ? 64 : 32;
+  const long long t256 = (q.I + 255) / 256 * ((q.J + 255) / 256);
+  w.bt = t256 >= 192 ? 256 : 128;
+  w.passes = w.bf16 && q.A.f ? 2 : 1;
+  w.slabs = (int)((q.Kc + slab - 1) / slab);
+  w.ldp = (long long)w.slabs * slab;
+  const long long tiles = w.bt == 256 ? t256 : t128;
+  const int total = w.slabs * w.passes;
+  long long parts = tiles >= 256 ? 1 : 512 / tiles;
+  if (parts > total / 8) parts = total / 8 > 0 ? total / 8 : 1;
+  w.parts = (int)parts;
+  w.copyA = !in_place(q.A, w.bf16, q.Kc);
+  w.copyB = !in_place(q.B, w.bf16, q.Kc);
+  const size_t es = w.bf16 ? 2 : 4;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  w.offB = w.copyA ? up((size_t)w.passes * q.I * w.ldp * es) : 0;
+  w.offP = w.offB + (w.copyB ? up((size_t)q.J * w.ldp * es) : 0);
+  w.bytes = w.offP + (w.parts > 1 ? (size_t)w.parts * q.I * q.J * sizeof(float) : 0);
+  return w;
+}
+
+template <typename T, typename CT, int PARTS, bool HF>
+hipError_t lay_out(const Operand& o, long long rows, long long Kc, void* out, long long ldp, hipStream_t s) {
+  const dim3 grid((unsigned)((rows + 63) / 64 * ((ldp + 63) / 64)));
+  const T *p = static_cast<const T*>(o.p), *f = static_cast<const T*>(o.f);
+  if (o.kslow) hipLaunchKernelGGL((lay_out_kernel<T, CT, PARTS, HF, true>), grid, dim3(256), 0, s, p, f, o.ld, rows, Kc, static_cast<CT*>(out), ldp, rows * ldp);
+  else hipLaunchKernelGGL((lay_out_kernel<T, CT, PARTS, HF, false>), grid, dim3(256), 0, s, p, f, o.ld, rows, Kc, static_cast<CT*>(out), ldp, rows * ldp);
+  return hipGetLastError();
+}
+hipError_t lay_out(const Operand& o, bool bf16, long long rows, long long Kc, void* out, long long ldp, hipStream_t s) {
+  if (bf16) return o.f ? lay_out<__bf16, __bf16, 2, true>(o, rows, Kc, out, ldp, s) : lay_out<__bf16, __bf16, 1, false>(o, rows, Kc, out, ldp, s);
+  if (o.type) return o.f ? lay_out<__bf16, float, 1, true>(o, rows, Kc, out, ldp, s) : lay_out<__bf16, float, 1, false>(o, rows, Kc, out, ldp, s);
+  return o.f ? lay_out<float, float, 1, true>(o, rows, Kc, out, ldp, s) : lay_out<float, float, 1, false>(o, rows, Kc, out, ldp, s);
+}
+
+template <typename CT, int BT, typename OT>
+hipError_t launch_wide_tiles(const WideArgs& a, int parts, hipStream_t s) {
+  static LdsOptIn opt;
+  const size_t smem = 4 * BT * 128;
+  const hipError_t e = opt.raise(reinterpret_cast<const void*>(&product_wide_kernel<CT, BT, OT>), smem);
+  if (e != hipSuccess) return e;
+  const long long tiles = (a.I + BT - 1) / BT * ((a.J + BT - 1) / BT);
+  hipLaunchKernelGGL((product_wide_kernel<CT, BT, OT>), dim3((unsigned)tiles, (unsigned)parts), dim3(256), smem, s, a);
+  return hipGetLastError();
+}
+template <typename CT, int BT>
+hipError_t launch_wide_out(const WideArgs& a, int parts, hipStream_t s) {
+  return a.e.otype ? launch_wide_tiles<CT, BT, __bf16>(a, parts, s) : launch_wide_tiles<CT, BT, float>(a, parts, s);
+}
+
+hipError_t join_parts(const Product& q, const float* partial, int parts, hipStream_t s) {
+  const long long n = q.I * q.J, blocks = (n + 255) / 256;
+  hipLaunchKernelGGL(join_parts_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, q.e, partial, parts, n, q.J);
+  return hipGetLastError();
+}
+
+hipError_t launch_wide_product(const Product& q, const WidePlan& w, void* ws, hipStream_t s) {
+  char* base = static_cast<char*>(ws);
+  const long long es = w.bf16 ? 2 : 4;
+  hipError_t e = hipSuccess;
+  if (w.copyA) e = lay_out(q.A, w.bf16, q.I, q.Kc, base, w.ldp, s);
+  if (e == hipSuccess && w.copyB) e = lay_out(q.B, w.bf16, q.J, q.Kc, base + w.offB, w.ldp, s);
+  if (e != hipSuccess) return e;
+  WideArgs a = {};
+  a.A = w.copyA ? Plane{base, w.ldp * es, q.I * w.ldp * es} : Plane{q.A.p, q.A.ld * es, 0};
+  a.B = w.copyB ? Plane{base + w.offB, w.ldp * es, 0} : Plane{q.B.p, q.B.ld * es, 0};
+  a.e = q.e;
+  a.I = q.I; a.J = q.J;
+  a.slabs = w.slabs;
+  a.passes = w.passes;
+  for (int i = 0; i < w.passes; ++i) { a.pa[i] = i; a.pb[i] = 0; }
+  a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;
+  const int parts = (w.slabs * w.passes + a.per - 1) / a.per;          // none of them empty
+  a.partial = parts > 1 ? reinterpret_cast<float*>(base + w.offP) : nullptr;
+  if (w.bf16) e = w.bt == 256 ? launch_wide_out<__bf16, 256>(a, parts, s) : launch_wide_out<__bf16, 128>(a, parts, s);
+  else e = w.bt == 256 ? launch_wide_out<float, 256>(a, parts, s) : launch_wide_out<float, 128>(a, parts, s);
+  if (e != hipSuccess || parts == 1) return e;
+  return join_parts(q, a.partial, parts, s);
+}
+
 // ------------------------------------------------------------------------------------------ sums of columns
 // Workgroup (64 columns, chunk of rows): four wavefronts take every fourth row; then the chunks are added up.
 constexpr int CHUNK = 256;
@@ -261,11 +632,15 @@ __global__ __launch_bounds__(256) void zero_kernel(float* out, long long n) {
 }  // namespace
 
 size_t product_workspace(const Product& q) {
+  const WidePlan w = wide_plan(q);
+  if (w.wide) return w.bytes;
   const int parts = parts_of(q);
   return parts > 1 ? (size_t)parts * (size_t)q.I * (size_t)q.J * sizeof(float) : 0;
 }
 
 hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
+  const WidePlan w = wide_plan(q);
+  if (w.wide) return launch_wide_product(q, w, ws, s);
   const int parts = parts_of(q);
   float* partial = static_cast<float*>(ws);
   hipError_t e;
@@ -273,9 +648,7 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
   else if (!q.A.kslow) e = q.A.f ? launch_types<true, false, true>(q, partial, parts, s) : launch_types<false, false, true>(q, partial, parts, s);
   else e = q.A.f ? launch_types<true, true, true>(q, partial, parts, s) : launch_types<false, true, true>(q, partial, parts, s);
   if (e != hipSuccess || parts == 1) return e;
-  const long long n = q.I * q.J, blocks = (n + 255) / 256;
-  hipLaunchKernelGGL(join_parts_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, q.e, partial, parts, n, q.J);
-  return hipGetLastError();
+  return join_parts(q, partial, parts, s);
 }
 
 size_t column_sum_workspace(long long M, long long F) {
