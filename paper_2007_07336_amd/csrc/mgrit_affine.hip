@@ -297,7 +297,11 @@ hipError_t launch_types(const Product& q, float* partial, int parts, hipStream_t
 // out in the workspace first (lay_out_kernel), which costs a pass over the operand and keeps the multiplying loop free of
 // everything but multiplications.
 typedef __attribute__((address_space(3))) void LdsPtr;
-typedef __attribute__((address_space(1))) const void GlobalPtr;
+// 16 bytes per lane from base + each lane's offset + along to `to` and the 1008 bytes behind it, in lane order
+__device__ __forceinline__ void to_lds(const char* base, int offset, int along, unsigned char* to) {
+  __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, -1, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsPtr*)to, 16, offset, along, 0, 0);
+}
 
 template <typename CT> struct Mma;
 template <> struct Mma<__bf16> {
@@ -322,8 +326,7 @@ struct WideArgs {
   Epilogue e;
   long long I, J;
   int slabs;                   // of one pass over the contraction
-  int passes;                  // pairs of parts that are multiplied: pass s takes A's part pa[s] and B's part pb[s]
-  int pa[6], pb[6];
+  int passes;                  // A's parts, each of which is multiplied with B
   int per;                     // slabs that one workgroup takes (blockIdx.y: which), all passes counted
   float* partial;              // several workgroups: their sums
 };
@@ -346,38 +349,38 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
   const long long i0 = (first + in % size) * BT, j0 = in / size * BT;
 
   const int total = a.slabs * a.passes, t0 = (int)blockIdx.y * a.per, t1 = t0 + a.per < total ? t0 + a.per : total;
-  unsigned offA[NL], offB[NL];
+  int offA[NL], offB[NL];
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
     const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
     const long long ra = i0 + r < a.I ? r : a.I - 1 - i0, rb = j0 + r < a.J ? r : a.J - 1 - j0;
-    offA[i] = (unsigned)(ra * a.A.ld) + piece * 16;
-    offB[i] = (unsigned)(rb * a.B.ld) + piece * 16;
+    offA[i] = (int)(ra * a.A.ld) + piece * 16;
+    offB[i] = (int)(rb * a.B.ld) + piece * 16;
   }
   const char* baseA = static_cast<const char*>(a.A.p) + i0 * a.A.ld;
   const char* baseB = static_cast<const char*>(a.B.p) + j0 * a.B.ld;
-  int pass = t0 / a.slabs, slab = t0 - pass * a.slabs;           // of the next slab to load
-  auto issue = [&](int buf) {
-    const char* pa = baseA + a.pa[pass] * a.A.part + slab * 128LL;
-    const char* pb = baseB + a.pb[pass] * a.B.part + slab * 128LL;
-    unsigned char* la = lds + buf * 2 * SLAB + wave * (BT / 4) * 128;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) __builtin_amdgcn_global_load_lds((GlobalPtr*)(pa + offA[i]), (LdsPtr*)(la + i * 1024), 16, 0, 0);
-#pragma unroll
-    for (int i = 0; i < NL; ++i) __builtin_amdgcn_global_load_lds((GlobalPtr*)(pb + offB[i]), (LdsPtr*)(la + SLAB + i * 1024), 16, 0, 0);
-    if (++slab == a.slabs) { slab = 0; ++pass; }
+  // the next slab to load: of which pass (A's parts, each against B from its start), and how far along the rows
+  int left = a.slabs - t0 % a.slabs, along = t0 % a.slabs * 128;
+  baseA += t0 / a.slabs * a.A.part;
+  auto load = [&](int buf, int i) {                              // load i of 2 NL
+    unsigned char* to = lds + buf * 2 * SLAB + wave * (BT / 4) * 128 + (i < NL ? i * 1024 : SLAB + (i - NL) * 1024);
+    to_lds(i < NL ? baseA : baseB, i < NL ? offA[i % NL] : offB[i % NL], along, to);
+  };
+  auto next = [&]() {
+    along += 128;
+    if (--left == 0) { left = a.slabs; along = 0; baseA += a.A.part; }
   };
   const int c = lane & 31, g = lane >> 5;
   const unsigned char* readA = lds + (wi * (BT / 2) + c) * 128;
   const unsigned char* readB = lds + SLAB + (wj * (BT / 2) + c) * 128;
-  Frag fa[2][T], fb[2][T];
-  auto read = [&](int buf, int step, int set) {
-    const int at = buf * 2 * SLAB + (((2 * step + g) ^ (c & 7)) << 4);
+  int piece[4];
 #pragma unroll
-    for (int i = 0; i < T; ++i) {
-      fa[set][i] = *reinterpret_cast<const Frag*>(readA + at + i * 32 * 128);
-      fb[set][i] = *reinterpret_cast<const Frag*>(readB + at + i * 32 * 128);
-    }
+  for (int step = 0; step < 4; ++step) piece[step] = ((2 * step + g) ^ (c & 7)) << 4;
+  Frag fa[2][T], fb[2][T];
+  auto read = [&](int buf, int step, int n) {                    // fragment n of 2 T
+    const int at = buf * 2 * SLAB + piece[step] + (n / 2) * 32 * 128;
+    if (n & 1) fb[step & 1][n / 2] = *reinterpret_cast<const Frag*>(readB + at);
+    else       fa[step & 1][n / 2] = *reinterpret_cast<const Frag*>(readA + at);
   };
   floatx16 acc[T][T];
 #pragma unroll
@@ -385,27 +388,49 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
 #pragma unroll
     for (int j = 0; j < T; ++j) acc[i][j] = zero16();
 
-  issue(0);
-  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-  if (t0 + 1 < t1) issue(1);
-  read(0, 0, 0);
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+  // One slab.  In every step the reads of the next one are spread over the first half of the multiplications, and behind the
+  // barrier the loads over all of them: the order is fixed in groups of T / 2 multiplications.
+  auto multiply = [&](int buf, auto more, auto last) {
 #pragma unroll
     for (int step = 0; step < 4; ++step) {
-      if (step < 3) {
-        read(buf, step + 1, (step + 1) & 1);
-      } else {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t + 2 < t1) issue(buf);
-        if (t + 1 < t1) read(buf ^ 1, 0, 0);
+      if (step == 3) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+      for (int n = 0; n < 2 * T; ++n) {
+        if (n < T && !(step == 3 && last)) {
+          read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n);
+          read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n + 1);
+        }
+        if (step == 3 && more) {
+#pragma unroll
+          for (int k = 0; k < 2 * NL / (2 * T); ++k) load(buf, n * (2 * NL / (2 * T)) + k);
+        }
+#pragma unroll
+        for (int k = 0; k < T / 2; ++k) {
+          const int m = n * (T / 2) + k;
+          Mma<CT>::go(fa[step & 1][m / T], fb[step & 1][m % T], acc[m / T][m % T]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int i = 0; i < T; ++i)
-#pragma unroll
-        for (int j = 0; j < T; ++j) Mma<CT>::go(fa[step & 1][i], fb[step & 1][j], acc[i][j]);
+      if (step == 3 && more) next();
     }
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+#pragma unroll
+  for (int i = 0; i < 2 * NL; ++i) load(0, i);
+  next();
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  if (t0 + 1 < t1) {
+#pragma unroll
+    for (int i = 0; i < 2 * NL; ++i) load(1, i);
+    next();
   }
+#pragma unroll
+  for (int n = 0; n < 2 * T; ++n) read(0, 0, n);
+  int buf = 0;
+  for (int t = t0; t < t1 - 2; ++t, buf ^= 1) multiply(buf, yes, no);
+  if (t0 + 1 < t1) { multiply(buf, no, no); buf ^= 1; }
+  multiply(buf, no, yes);
 
   // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands
   constexpr int W = BT / 2, PITCH = W + 4;
@@ -519,7 +544,7 @@ inline bool in_place(const Operand& o, bool bf16, long long Kc) {
 WidePlan wide_plan(const Product& q) {
   WidePlan w = {};
   const long long t128 = (q.I + 127) / 128 * ((q.J + 127) / 128);
-  w.wide = q.I >= 128 && q.J >= 128 && q.Kc >= 64 && t128 >= 16 && q.Kc < (1LL << 22) && t128 < (1LL << 30);
+  w.wide = q.I >= 128 && q.J >= 128 && q.Kc >= 64 && t128 >= 16 && q.Kc <= (1LL << 20) && t128 < (1LL << 30);
   if (!w.wide) return w;
   w.bf16 = q.A.type && q.B.type;
   const int slab = w.bf16 ? 64 : 32;
@@ -592,7 +617,6 @@ hipError_t launch_wide_product(const Product& q, const WidePlan& w, void* ws, hi
   a.I = q.I; a.J = q.J;
   a.slabs = w.slabs;
   a.passes = w.passes;
-  for (int i = 0; i < w.passes; ++i) { a.pa[i] = i; a.pb[i] = 0; }
   a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;
   const int parts = (w.slabs * w.passes + a.per - 1) / a.per;          // none of them empty
   a.partial = parts > 1 ? reinterpret_cast<float*>(base + w.offP) : nullptr;
