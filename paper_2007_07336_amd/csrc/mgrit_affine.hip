@@ -352,7 +352,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
   int offA[NL], offB[NL];
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
+    const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
     const long long ra = i0 + r < a.I ? r : a.I - 1 - i0, rb = j0 + r < a.J ? r : a.J - 1 - j0;
     offA[i] = (int)(ra * a.A.ld) + piece * 16;
     offB[i] = (int)(rb * a.B.ld) + piece * 16;
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
   const unsigned char* readB = lds + SLAB + (wj * (BT / 2) + c) * 128;
   int piece[4];
 #pragma unroll
-  for (int step = 0; step < 4; ++step) piece[step] = ((2 * step + g) ^ (c & 7)) << 4;
+  for (int step = 0; step < 4; ++step) piece[step] = ((2 * step + g) ^ ((c >> 1) & 7)) << 4;
   Frag fa[2][T], fb[2][T];
   auto read = [&](int buf, int step, int n) {                    // fragment n of 2 T
     const int at = buf * 2 * SLAB + piece[step] + (n / 2) * 32 * 128;
@@ -388,9 +388,11 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
 #pragma unroll
     for (int j = 0; j < T; ++j) acc[i][j] = zero16();
 
-  // One slab.  In every step the reads of the next one are spread over the first half of the multiplications, and behind the
-  // barrier the loads over all of them: the order is fixed in groups of T / 2 multiplications.
-  auto multiply = [&](int buf, auto more, auto last) {
+  // One slab.  In every step the reads of the next one are spread over the first half of the multiplications; the order is fixed
+  // in groups of T / 2 multiplications.  The loads of the slab after the next begin behind the barrier and are spread over SPREAD
+  // steps: the address unit takes 16 cycles for one, and a wavefront that waits for it multiplies nothing.
+  constexpr int SPREAD = 3, PER = (2 * NL + 2 * T * SPREAD - 1) / (2 * T * SPREAD);       // loads in a group
+  auto multiply = [&](int buf, auto rest, auto more, auto last) {
 #pragma unroll
     for (int step = 0; step < 4; ++step) {
       if (step == 3) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -400,9 +402,11 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
           read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n);
           read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n + 1);
         }
-        if (step == 3 && more) {
+        const int group = (step + 1) % 4 * 2 * T + n;
 #pragma unroll
-          for (int k = 0; k < 2 * NL / (2 * T); ++k) load(buf, n * (2 * NL / (2 * T)) + k);
+        for (int k = group * PER; k < (group + 1) * PER && k < 2 * NL; ++k) {
+          if (step == 3 && more) load(buf, k);
+          if (step < 3 && rest) load(buf ^ 1, k);
         }
 #pragma unroll
         for (int k = 0; k < T / 2; ++k) {
@@ -411,7 +415,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (step == 3 && more) next();
+      if (step == SPREAD - 2 && rest) next();
     }
   };
   constexpr std::true_type yes{};
@@ -422,15 +426,14 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   if (t0 + 1 < t1) {
 #pragma unroll
-    for (int i = 0; i < 2 * NL; ++i) load(1, i);
-    next();
+    for (int i = 0; i < 2 * T * PER && i < 2 * NL; ++i) load(1, i);
   }
 #pragma unroll
   for (int n = 0; n < 2 * T; ++n) read(0, 0, n);
   int buf = 0;
-  for (int t = t0; t < t1 - 2; ++t, buf ^= 1) multiply(buf, yes, no);
-  if (t0 + 1 < t1) { multiply(buf, no, no); buf ^= 1; }
-  multiply(buf, no, yes);
+  for (int t = t0; t < t1 - 2; ++t, buf ^= 1) multiply(buf, yes, yes, no);
+  if (t0 + 1 < t1) { multiply(buf, yes, no, no); buf ^= 1; }
+  multiply(buf, no, no, yes);
 
   // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands
   constexpr int W = BT / 2, PITCH = W + 4;
