@@ -24,6 +24,15 @@ __device__ __forceinline__ float tanh_with_slope(float z, float* slope) {
   return a < 0.35f ? series : copysignf((1.0f - e) * r, z);
 }
 
+// v = hi + lo, both representable in bf16 if v has 16 significant bits.  What overflows by rounding is cut instead; an infinity or
+// a NaN stays in hi.
+__device__ __forceinline__ void split2(float v, float* hi, float* lo) {
+  float h = widen(narrow<__bf16>(v));
+  if (fabsf(h) == INFINITY && fabsf(v) < INFINITY) h = copysignf(0x1.fep127f, v);
+  *hi = h;
+  *lo = fabsf(h) < INFINITY ? v - h : 0.0f;
+}
+
 struct Out { float y, d; };
 // act(z) and act'(z); a NaN stays one
 __device__ __forceinline__ Out activate(float z, int act) {
@@ -292,15 +301,20 @@ hipError_t launch_types(const Product& q, float* partial, int parts, hipStream_t
 }
 
 // ------------------------------------------------------------------------------------------ large products
-// Operands as planes: rows along k, padded with zeros to whole slabs of 128 bytes (64 bf16 or 32 float), 16-byte pieces.  What the
-// caller has in this form is read in place; anything else -- transposed, ragged, with a factor, of another type -- is laid
-// out in the workspace first (lay_out_kernel), which costs a pass over the operand and keeps the multiplying loop free of
-// everything but multiplications.
+// Operands as planes of CT in memory, 16-byte pieces: rows along k, padded with zeros to whole slabs (64 bf16 or 32 float), or
+// with k slow, as the backward pass meets its operands, rows of any multiple of 16 bytes.  What the caller has in this form is read
+// in place; anything else -- ragged, with a factor, of another type -- is laid out in the workspace first, which costs a pass
+// over the operand and keeps the multiplying loop free of everything but multiplications.
 typedef __attribute__((address_space(3))) void LdsPtr;
-// 16 bytes per lane from base + each lane's offset + along to `to` and the 1008 bytes behind it, in lane order
-__device__ __forceinline__ void to_lds(const char* base, int offset, int along, unsigned char* to) {
-  __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, -1, 0x00020000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsPtr*)to, 16, offset, along, 0, 0);
+// 16 bytes per lane from base + each lane's offset + along to LDS address `to` and the 1008 bytes behind it, in lane order; zeros from
+// base + room on.  In assembly so that the compiler does not see a load that writes LDS: it would hold back every transposing read
+// until all loads have arrived (backward pass of 8192 x 4096 x 4096 bf16: 1781 us).  There is no result register, and what is
+// waited for stands in the kernel.
+typedef int int4v __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void to_lds(const char* base, int offset, int along, unsigned room, unsigned to) {
+  const unsigned long long b = reinterpret_cast<unsigned long long>(base);
+  const int4v rsrc = {(int)(unsigned)b, (int)(unsigned)(b >> 32), (int)room, 0x00020000};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(to), "v"(offset), "s"(rsrc), "s"(along) : "memory");
 }
 
 template <typename CT> struct Mma;
@@ -317,26 +331,110 @@ template <> struct Mma<float> {
 };
 
 struct Plane {
-  const void* p;
-  long long ld;                // bytes from row to row
+  const char* p;
+  long long ld;                // bytes from row to row (k slow: from k to k)
   long long part;              // bytes from part to part
 };
 struct WideArgs {
   Plane A, B;
   Epilogue e;
-  long long I, J;
+  long long I, J, Kc;
   int slabs;                   // of one pass over the contraction
   int passes;                  // A's parts, each of which is multiplied with B
   int per;                     // slabs that one workgroup takes (blockIdx.y: which), all passes counted
   float* partial;              // several workgroups: their sums
 };
 
-// Tile of BT x BT outputs, four wavefronts with a quarter each.  A slab of both operands is 2 BT rows of 128 bytes in LDS, its
-// 16-byte pieces in the order piece ^ (row & 7): the hardware writes LDS in lane order, so the lanes pick their pieces in that
-// order from memory, and eight lanes that read the same piece of eight rows meet different banks.  Two slabs are in LDS: while one
+// One operand's way into LDS and registers.  A slab is SLAB bytes of LDS, either BT rows of 128 bytes along k or 128 / sizeof(CT) rows
+// of BT entries.  The hardware writes LDS in lane order, so the lanes pick their 16-byte pieces from memory in the order that
+// spreads the later reads over the banks: along k, piece ^ (row / 2 & 7), so that sixteen rows' pieces of one k meet different banks;
+// with k slow, the four rows that a transposing read takes from (bf16), or the two that the wavefront's halves take (float), lie
+// 64 or 128 bytes apart.
+template <typename CT, int BT, bool KS>
+struct Stream {
+  typedef typename Mma<CT>::Frag Frag;
+  static constexpr int ES = sizeof(CT), T = BT / 64, NL = BT / 32, KSLAB = 128 / ES, ROW = BT * ES;   // ROW: bytes of a row with k slow
+  static constexpr int SLAB = BT * 128;
+  const char* base;            // of the next slab to load
+  long long room;              // bytes from there to the end (k slow)
+  int along, offset[NL];
+  int at[KS ? T : 4];          // where this lane reads: per tile (k slow) or per step
+
+  // rows r0.. of `rows`; skip: slabs before the first one; side: which half of the tile this wavefront reads
+  __device__ __forceinline__ void init(const Plane& p, long long r0, long long rows, long long Kc, int part, int skip, int wave, int lane, int side) {
+    const int c = lane & 31, g = lane >> 5;
+    if constexpr (KS) {
+      base = p.p + part * p.part + r0 * ES + (long long)skip * KSLAB * p.ld;
+      room = Kc * p.ld - r0 * ES - (long long)skip * KSLAB * p.ld;
+      along = 0;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int byte = (wave * NL + i) * 1024 + lane * 16, k = byte / ROW, piece = byte % ROW / 16;
+        const int from = ES == 2 ? piece ^ ((k & 3) << 2) : piece ^ ((k >> 2 & 1) << 3);
+        offset[i] = (int)(k * p.ld) + from * 16;
+      }
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        const int first = side * (BT / 2) + i * 32;
+        if (ES == 2) {
+          const int l16 = lane & 15, k = 8 * g + (l16 >> 2), col = first + 16 * (c >> 4) + 4 * (l16 & 3);
+          at[i] = k * ROW + (((col >> 3) ^ ((k & 3) << 2)) << 4) + (col & 7) * 2;
+        } else {
+          const int col = first + c;
+          at[i] = 4 * g * ROW + (((col >> 2) ^ (g << 3)) << 4) + (col & 3) * 4;
+        }
+      }
+    } else {
+      base = p.p + part * p.part + r0 * p.ld;
+      along = skip * 128;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
+        offset[i] = (int)((r0 + r < rows ? r : rows - 1 - r0) * p.ld) + piece * 16;
+      }
+#pragma unroll
+      for (int step = 0; step < 4; ++step) at[step] = (side * (BT / 2) + c) * 128 + (((2 * step + g) ^ ((c >> 1) & 7)) << 4);
+    }
+  }
+  __device__ __forceinline__ void load(int i, unsigned slab, int wave) const {
+    const unsigned most = 0xffffffffu;
+    to_lds(base, offset[i], along, KS && room < (long long)most ? (unsigned)room : most, slab + (wave * NL + i) * 1024);
+  }
+  __device__ __forceinline__ void next(const Plane& p) {
+    if (KS) { base += KSLAB * p.ld; room -= KSLAB * p.ld; }
+    else along += 128;
+  }
+  // from behind the last slab to the first one, of the next part (A) or the same (B)
+  __device__ __forceinline__ void again(const Plane& p, int slabs, bool next_part) {
+    if (KS) { base -= (long long)slabs * KSLAB * p.ld; room += (long long)slabs * KSLAB * p.ld; }
+    else along = 0;
+    if (next_part) base += p.part;
+  }
+  // fragment of tile i in step `step`
+  __device__ __forceinline__ Frag read(const unsigned char* slab, int step, int i) const {
+    if constexpr (!KS) {
+      return *reinterpret_cast<const Frag*>(slab + at[step] + i * 32 * 128);
+    } else if constexpr (ES == 2) {
+      // a sixteenth of the wavefront hands in 4 k x 16 rows and each lane gets four k of its row
+      typedef __attribute__((address_space(3))) short4v* Lds4;
+      const unsigned char* q = slab + at[i] + step * 16 * ROW;
+      const bf16x4 lo = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(q)));
+      const bf16x4 hi = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(q + 4 * ROW)));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const unsigned char* q = slab + at[i] + step * 8 * ROW;
+      Frag f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const float*>(q + j * ROW);
+      return f;
+    }
+  }
+};
+
+// Tile of BT x BT outputs, four wavefronts with a quarter each.  Two slabs of both operands are in LDS: while one
 // is multiplied in four steps, the next one is on its way.  Behind the last step's reads a barrier says that nobody needs the old slab
 // any more and that the next one has arrived; the loads of the one after go out at once and have a whole slab's time.
-template <typename CT, int BT, typename OT>
+template <typename CT, int BT, typename OT, bool AS, bool BS>
 __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(WideArgs a) {
   typedef typename Mma<CT>::Frag Frag;
   constexpr int T = BT / 64, NL = BT / 32, SLAB = BT * 128;       // 32 x 32 tiles along a wavefront's side; loads per operand and slab
@@ -349,38 +447,28 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
   const long long i0 = (first + in % size) * BT, j0 = in / size * BT;
 
   const int total = a.slabs * a.passes, t0 = (int)blockIdx.y * a.per, t1 = t0 + a.per < total ? t0 + a.per : total;
-  int offA[NL], offB[NL];
-#pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
-    const long long ra = i0 + r < a.I ? r : a.I - 1 - i0, rb = j0 + r < a.J ? r : a.J - 1 - j0;
-    offA[i] = (int)(ra * a.A.ld) + piece * 16;
-    offB[i] = (int)(rb * a.B.ld) + piece * 16;
-  }
-  const char* baseA = static_cast<const char*>(a.A.p) + i0 * a.A.ld;
-  const char* baseB = static_cast<const char*>(a.B.p) + j0 * a.B.ld;
-  // the next slab to load: of which pass (A's parts, each against B from its start), and how far along the rows
-  int left = a.slabs - t0 % a.slabs, along = t0 % a.slabs * 128;
-  baseA += t0 / a.slabs * a.A.part;
+  Stream<CT, BT, AS> sa;
+  Stream<CT, BT, BS> sb;
+  sa.init(a.A, i0, a.I, a.Kc, t0 / a.slabs, t0 % a.slabs, wave, lane, wi);
+  sb.init(a.B, j0, a.J, a.Kc, 0, t0 % a.slabs, wave, lane, wj);
+  int left = a.slabs - t0 % a.slabs;                             // of this pass: A's parts one by one, each against the whole of B
+  const unsigned lds_at = (unsigned)(unsigned long long)(LdsPtr*)lds;
   auto load = [&](int buf, int i) {                              // load i of 2 NL
-    unsigned char* to = lds + buf * 2 * SLAB + wave * (BT / 4) * 128 + (i < NL ? i * 1024 : SLAB + (i - NL) * 1024);
-    to_lds(i < NL ? baseA : baseB, i < NL ? offA[i % NL] : offB[i % NL], along, to);
+    const unsigned slab = lds_at + buf * 2 * SLAB;
+    if (i < NL) sa.load(i, slab, wave);
+    else sb.load(i - NL, slab + SLAB, wave);
   };
   auto next = [&]() {
-    along += 128;
-    if (--left == 0) { left = a.slabs; along = 0; baseA += a.A.part; }
+    sa.next(a.A);
+    sb.next(a.B);
+    if (--left == 0) { left = a.slabs; sa.again(a.A, a.slabs, true); sb.again(a.B, a.slabs, false); }
   };
   const int c = lane & 31, g = lane >> 5;
-  const unsigned char* readA = lds + (wi * (BT / 2) + c) * 128;
-  const unsigned char* readB = lds + SLAB + (wj * (BT / 2) + c) * 128;
-  int piece[4];
-#pragma unroll
-  for (int step = 0; step < 4; ++step) piece[step] = ((2 * step + g) ^ ((c >> 1) & 7)) << 4;
   Frag fa[2][T], fb[2][T];
   auto read = [&](int buf, int step, int n) {                    // fragment n of 2 T
-    const int at = buf * 2 * SLAB + piece[step] + (n / 2) * 32 * 128;
-    if (n & 1) fb[step & 1][n / 2] = *reinterpret_cast<const Frag*>(readB + at);
-    else       fa[step & 1][n / 2] = *reinterpret_cast<const Frag*>(readA + at);
+    const unsigned char* slab = lds + buf * 2 * SLAB;
+    if (n & 1) fb[step & 1][n / 2] = sb.read(slab + SLAB, step, n / 2);
+    else       fa[step & 1][n / 2] = sa.read(slab, step, n / 2);
   };
   floatx16 acc[T][T];
 #pragma unroll
@@ -466,47 +554,24 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
   }
 }
 
-// Operand -> planes: rows x (k padded to whole slabs) of CT, PARTS of them: 1 as it is (or widened); 2: the product of two bf16
-// values, 16 significant bits, is the sum of two.  Workgroup: 64 rows x 64 k; where rows are the fast index in memory they
-// change places in LDS.
-template <typename T, typename CT, int PARTS, bool HF, bool KSLOW>
-__global__ __launch_bounds__(256) void lay_out_kernel(const T* p, const T* f, long long ld, long long rows, long long Kc, CT* out, long long ldo, long long part) {
-  __shared__ float tile[64][65];
-  const long long kt = (ldo + 63) / 64, L = blockIdx.x;
-  const long long r0 = L / kt * 64, k0 = L % kt * 64;
+// Operand -> planes of CT: rows x (k padded to ldo with zeros), PARTS of them: 1 as it is (or widened); 2: the product of two bf16
+// values, which has 16 significant bits, as the sum of two.  A thread has eight columns of every eighth row of a workgroup's
+// span x 256 entries.  With `sums` the columns' sums over the span as well (of the gradient, for the bias), and PARTS = 0 is
+// those alone.  Bound by memory: 8192 x 4096 bf16 with factors into two planes, 256 MB, with sums: see the table of cases.
+template <typename T, typename CT, int PARTS, bool HF>
+__global__ __launch_bounds__(256) void lay_out_kernel(const T* p, const T* f, long long rows, long long K, CT* out, long long ldo, long long part, int span,
+                                                      float scale, float* sums) {
+  const long long tiles = ((PARTS ? ldo : K) + 255) / 256, chunk = blockIdx.x / tiles;
   const int t = threadIdx.x;
-  if (KSLOW) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = t % 16 * 4, k = t / 16 + 16 * i;
-      const long long at = (k0 + k) * ld + r0 + r, left = k0 + k < Kc ? rows - r0 - r : 0;
-      Four<T> a, b;
-      if (ld % 4 == 0 && left >= 4) {
-        a = *reinterpret_cast<const Four<T>*>(__builtin_assume_aligned(p + at, 4 * sizeof(T)));
-        if (HF) b = *reinterpret_cast<const Four<T>*>(__builtin_assume_aligned(f + at, 4 * sizeof(T)));
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          a.v[j] = j < left ? p[at + j] : T(0.0f);
-          if (HF) b.v[j] = j < left ? f[at + j] : T(0.0f);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) tile[k][r + j] = HF ? widen(a.v[j]) * widen(b.v[j]) : widen(a.v[j]);
-    }
-    __syncthreads();
-  }
-  for (int n = t; n < 512; n += 256) {             // eight k of a row
-    const int r = n / 8, k = n % 8 * 8;
-    if (r0 + r >= rows || k0 + k >= ldo) continue;
-    float v[8];
-    if (KSLOW) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = tile[k + j][r];
-    } else {
-      const long long at = (r0 + r) * ld + k0 + k, left = Kc - k0 - k;
-      float b[8];
-      if (ld % 8 == 0 && left >= 8) {
+  const long long k = blockIdx.x % tiles * 256 + t % 32 * 8, r0 = chunk * span, r1 = r0 + span < rows ? r0 + span : rows;
+  const long long left = K - k;
+  const bool whole = K % 8 == 0 && left >= 8;
+  float s[8] = {};
+  if (k < (PARTS ? ldo : K)) {
+    for (long long r = r0 + t / 32; r < r1; r += 8) {
+      const long long at = r * K + k;
+      float v[8], b[8];
+      if (whole) {
         load8(p + at, v);
         if (HF) load8(f + at, b);
       } else {
@@ -516,46 +581,112 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T* p, const T* f, lo
           if (HF) b[j] = j < left ? widen(f[at + j]) : 0.0f;
         }
       }
-      if (HF)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= b[j];
-    }
-    CT* o = out + (r0 + r) * ldo + k0 + k;
-    store8(o, v);
-    if (PARTS == 2) {
-      float lo[8];
+      for (int j = 0; j < 8; ++j) {
+        if (HF) v[j] *= b[j];
+        s[j] += v[j];
+      }
+      if constexpr (PARTS > 0) {
+        CT* o = out + r * ldo + k;
+        if constexpr (PARTS == 2) {
+          float lo[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) lo[j] = v[j] - widen(narrow<CT>(v[j]));
-      store8(o + part, lo);
+          for (int j = 0; j < 8; ++j) split2(v[j], &v[j], &lo[j]);
+          store8(o + part, lo);
+        }
+        store8(o, v);
+      }
     }
   }
+  if (!sums) return;
+  __shared__ float sh[8][256];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sh[t / 32][t % 32 * 8 + j] = s[j];
+  __syncthreads();
+  const long long col = blockIdx.x % tiles * 256 + t;
+  if (col >= K) return;
+  float a = sh[0][t];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) a += sh[i][t];
+  sums[chunk * K + col] = scale * a;
+}
+// out[col] = sum over the chunks; 64 columns and four sets of chunks per workgroup
+__global__ __launch_bounds__(256) void add_chunks_kernel(const float* part, int chunks, long long F, float* out) {
+  __shared__ float sh[4][64];
+  const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
+  const long long col = blockIdx.x * 64LL + lane;
+  float s = 0.0f;
+  if (col < F)
+    for (int c = set; c < chunks; c += 4) s += part[c * F + col];
+  sh[set][lane] = s;
+  __syncthreads();
+  if (set == 0 && col < F) out[col] = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
 }
 
-template <typename CT> constexpr int slab_of() { return 128 / (int)sizeof(CT); }
+__global__ __launch_bounds__(256) void zero_kernel(float* out, long long n) {
+  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) out[i] = 0.0f;
+}
 
+inline size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+// Rows that a workgroup of lay_out_kernel takes: 64, and more where that makes over 256 chunks
+int span_of(long long rows) {
+  const long long n = (rows + 255) / 256;
+  return (int)(n <= 64 ? 64 : (n + 7) / 8 * 8);
+}
+int chunks_of(long long rows) { const int s = span_of(rows); return (int)((rows + s - 1) / s); }
+
+template <typename T, typename CT, int PARTS, bool HF>
+hipError_t lay_out(const void* p, const void* f, long long rows, long long K, void* out, long long ldo, float scale, float* sums, hipStream_t s) {
+  const long long tiles = ((PARTS ? ldo : K) + 255) / 256;
+  hipLaunchKernelGGL((lay_out_kernel<T, CT, PARTS, HF>), dim3((unsigned)(tiles * chunks_of(rows))), dim3(256), 0, s, static_cast<const T*>(p),
+                     static_cast<const T*>(f), rows, K, static_cast<CT*>(out), ldo, rows * ldo, span_of(rows), scale, sums);
+  return hipGetLastError();
+}
+// rows x K entries of `type`, with factors or without, as CT (bf16: with factors in two parts); out null: sums only
+hipError_t lay_out(const void* p, const void* f, int type, bool bf16, long long rows, long long K, void* out, long long ldo, float scale, float* sums,
+                   hipStream_t s) {
+  if (!out) {
+    if (type) return f ? lay_out<__bf16, __bf16, 0, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<__bf16, __bf16, 0, false>(p, f, rows, K, out, ldo, scale, sums, s);
+    return f ? lay_out<float, float, 0, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<float, float, 0, false>(p, f, rows, K, out, ldo, scale, sums, s);
+  }
+  if (bf16) return f ? lay_out<__bf16, __bf16, 2, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<__bf16, __bf16, 1, false>(p, f, rows, K, out, ldo, scale, sums, s);
+  if (type) return f ? lay_out<__bf16, float, 1, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<__bf16, float, 1, false>(p, f, rows, K, out, ldo, scale, sums, s);
+  return f ? lay_out<float, float, 1, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<float, float, 1, false>(p, f, rows, K, out, ldo, scale, sums, s);
+}
+
+// ---- which tiles, and what has to be laid out
+inline int slab_of(bool bf16) { return bf16 ? 64 : 32; }
+inline bool wide_sizes(long long I, long long J, long long Kc) {
+  const long long t128 = (I + 127) / 128 * ((J + 127) / 128);
+  return I >= 128 && J >= 128 && Kc >= 64 && t128 >= 16 && Kc <= (1LL << 20) && I <= (1LL << 22) && J <= (1LL << 22);
+}
 struct WidePlan {
   bool wide, bf16;
   int bt, slabs, passes, parts;       // parts: workgroups that share a tile's contraction
   bool copyA, copyB;
-  long long ldp;                      // entries from row to row of a laid out plane
+  long long ldA, ldB;                 // entries from row to row of a laid out plane
   size_t offB, offP, bytes;
 };
 inline bool in_place(const Operand& o, bool bf16, long long Kc) {
-  const int slab = bf16 ? 64 : 32;
-  return !o.kslow && !o.f && (o.type != 0) == bf16 && Kc % slab == 0 && o.ld == Kc;
+  if (o.f || (o.type != 0) != bf16) return false;
+  if (o.kslow) return o.ld % (bf16 ? 8 : 4) == 0;
+  return o.ld % slab_of(bf16) == 0 && (o.ld == Kc || o.padded);
+}
+// (row length of the copy: whole slabs along k; with k slow, whole 16-byte pieces, of which 8 entries are some)
+inline long long plane_ld(const Operand& o, bool bf16, long long rows, long long Kc) {
+  const long long m = o.kslow ? 8 : slab_of(bf16);
+  return ((o.kslow ? rows : Kc) + m - 1) / m * m;
 }
 WidePlan wide_plan(const Product& q) {
   WidePlan w = {};
-  const long long t128 = (q.I + 127) / 128 * ((q.J + 127) / 128);
-  w.wide = q.I >= 128 && q.J >= 128 && q.Kc >= 64 && t128 >= 16 && q.Kc <= (1LL << 20) && t128 < (1LL << 30);
+  w.wide = wide_sizes(q.I, q.J, q.Kc);
   if (!w.wide) return w;
   w.bf16 = q.A.type && q.B.type;
-  const int slab = w.bf16 ? 64 : 32;
-  const long long t256 = (q.I + 255) / 256 * ((q.J + 255) / 256);
+  const long long t128 = (q.I + 127) / 128 * ((q.J + 127) / 128), t256 = (q.I + 255) / 256 * ((q.J + 255) / 256);
   w.bt = t256 >= 192 ? 256 : 128;
-  w.passes = w.bf16 && q.A.f ? 2 : 1;
-  w.slabs = (int)((q.Kc + slab - 1) / slab);
-  w.ldp = (long long)w.slabs * slab;
+  w.passes = q.A.parts > 1 ? q.A.parts : w.bf16 && q.A.f ? 2 : 1;
+  w.slabs = (int)((q.Kc + slab_of(w.bf16) - 1) / slab_of(w.bf16));
   const long long tiles = w.bt == 256 ? t256 : t128;
   const int total = w.slabs * w.passes;
   long long parts = tiles >= 256 ? 1 : 512 / tiles;
@@ -563,41 +694,33 @@ WidePlan wide_plan(const Product& q) {
   w.parts = (int)parts;
   w.copyA = !in_place(q.A, w.bf16, q.Kc);
   w.copyB = !in_place(q.B, w.bf16, q.Kc);
+  w.ldA = plane_ld(q.A, w.bf16, q.I, q.Kc);
+  w.ldB = plane_ld(q.B, w.bf16, q.J, q.Kc);
   const size_t es = w.bf16 ? 2 : 4;
-  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  w.offB = w.copyA ? up((size_t)w.passes * q.I * w.ldp * es) : 0;
-  w.offP = w.offB + (w.copyB ? up((size_t)q.J * w.ldp * es) : 0);
+  w.offB = w.copyA ? up((size_t)w.passes * (q.A.kslow ? q.Kc : q.I) * w.ldA * es) : 0;
+  w.offP = w.offB + (w.copyB ? up((size_t)(q.B.kslow ? q.Kc : q.J) * w.ldB * es) : 0);
   w.bytes = w.offP + (w.parts > 1 ? (size_t)w.parts * q.I * q.J * sizeof(float) : 0);
   return w;
 }
-
-template <typename T, typename CT, int PARTS, bool HF>
-hipError_t lay_out(const Operand& o, long long rows, long long Kc, void* out, long long ldp, hipStream_t s) {
-  const dim3 grid((unsigned)((rows + 63) / 64 * ((ldp + 63) / 64)));
-  const T *p = static_cast<const T*>(o.p), *f = static_cast<const T*>(o.f);
-  if (o.kslow) hipLaunchKernelGGL((lay_out_kernel<T, CT, PARTS, HF, true>), grid, dim3(256), 0, s, p, f, o.ld, rows, Kc, static_cast<CT*>(out), ldp, rows * ldp);
-  else hipLaunchKernelGGL((lay_out_kernel<T, CT, PARTS, HF, false>), grid, dim3(256), 0, s, p, f, o.ld, rows, Kc, static_cast<CT*>(out), ldp, rows * ldp);
-  return hipGetLastError();
-}
-hipError_t lay_out(const Operand& o, bool bf16, long long rows, long long Kc, void* out, long long ldp, hipStream_t s) {
-  if (bf16) return o.f ? lay_out<__bf16, __bf16, 2, true>(o, rows, Kc, out, ldp, s) : lay_out<__bf16, __bf16, 1, false>(o, rows, Kc, out, ldp, s);
-  if (o.type) return o.f ? lay_out<__bf16, float, 1, true>(o, rows, Kc, out, ldp, s) : lay_out<__bf16, float, 1, false>(o, rows, Kc, out, ldp, s);
-  return o.f ? lay_out<float, float, 1, true>(o, rows, Kc, out, ldp, s) : lay_out<float, float, 1, false>(o, rows, Kc, out, ldp, s);
+hipError_t lay_out_operand(const Operand& o, bool bf16, long long rows, long long Kc, void* out, long long ldo, hipStream_t s) {
+  return o.kslow ? lay_out(o.p, o.f, o.type, bf16, Kc, rows, out, ldo, 1.0f, nullptr, s) : lay_out(o.p, o.f, o.type, bf16, rows, Kc, out, ldo, 1.0f, nullptr, s);
 }
 
-template <typename CT, int BT, typename OT>
+template <typename CT, int BT, typename OT, bool AS, bool BS>
 hipError_t launch_wide_tiles(const WideArgs& a, int parts, hipStream_t s) {
   static LdsOptIn opt;
   const size_t smem = 4 * BT * 128;
-  const hipError_t e = opt.raise(reinterpret_cast<const void*>(&product_wide_kernel<CT, BT, OT>), smem);
+  const hipError_t e = opt.raise(reinterpret_cast<const void*>(&product_wide_kernel<CT, BT, OT, AS, BS>), smem);
   if (e != hipSuccess) return e;
   const long long tiles = (a.I + BT - 1) / BT * ((a.J + BT - 1) / BT);
-  hipLaunchKernelGGL((product_wide_kernel<CT, BT, OT>), dim3((unsigned)tiles, (unsigned)parts), dim3(256), smem, s, a);
+  hipLaunchKernelGGL((product_wide_kernel<CT, BT, OT, AS, BS>), dim3((unsigned)tiles, (unsigned)parts), dim3(256), smem, s, a);
   return hipGetLastError();
 }
 template <typename CT, int BT>
-hipError_t launch_wide_out(const WideArgs& a, int parts, hipStream_t s) {
-  return a.e.otype ? launch_wide_tiles<CT, BT, __bf16>(a, parts, s) : launch_wide_tiles<CT, BT, float>(a, parts, s);
+hipError_t launch_wide_out(const WideArgs& a, bool as, bool bs, int parts, hipStream_t s) {
+  if (as) return launch_wide_tiles<CT, BT, float, true, true>(a, parts, s);            // dW is float
+  if (bs) return a.e.otype ? launch_wide_tiles<CT, BT, __bf16, false, true>(a, parts, s) : launch_wide_tiles<CT, BT, float, false, true>(a, parts, s);
+  return a.e.otype ? launch_wide_tiles<CT, BT, __bf16, false, false>(a, parts, s) : launch_wide_tiles<CT, BT, float, false, false>(a, parts, s);
 }
 
 hipError_t join_parts(const Product& q, const float* partial, int parts, hipStream_t s) {
@@ -610,50 +733,78 @@ hipError_t launch_wide_product(const Product& q, const WidePlan& w, void* ws, hi
   char* base = static_cast<char*>(ws);
   const long long es = w.bf16 ? 2 : 4;
   hipError_t e = hipSuccess;
-  if (w.copyA) e = lay_out(q.A, w.bf16, q.I, q.Kc, base, w.ldp, s);
-  if (e == hipSuccess && w.copyB) e = lay_out(q.B, w.bf16, q.J, q.Kc, base + w.offB, w.ldp, s);
+  if (w.copyA) e = lay_out_operand(q.A, w.bf16, q.I, q.Kc, base, w.ldA, s);
+  if (e == hipSuccess && w.copyB) e = lay_out_operand(q.B, w.bf16, q.J, q.Kc, base + w.offB, w.ldB, s);
   if (e != hipSuccess) return e;
   WideArgs a = {};
-  a.A = w.copyA ? Plane{base, w.ldp * es, q.I * w.ldp * es} : Plane{q.A.p, q.A.ld * es, 0};
-  a.B = w.copyB ? Plane{base + w.offB, w.ldp * es, 0} : Plane{q.B.p, q.B.ld * es, 0};
+  a.A = w.copyA ? Plane{base, w.ldA * es, (q.A.kslow ? q.Kc : q.I) * w.ldA * es} : Plane{static_cast<const char*>(q.A.p), q.A.ld * es, q.A.part * es};
+  a.B = w.copyB ? Plane{base + w.offB, w.ldB * es, 0} : Plane{static_cast<const char*>(q.B.p), q.B.ld * es, 0};
   a.e = q.e;
-  a.I = q.I; a.J = q.J;
+  a.I = q.I; a.J = q.J; a.Kc = q.Kc;
   a.slabs = w.slabs;
   a.passes = w.passes;
   a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;
   const int parts = (w.slabs * w.passes + a.per - 1) / a.per;          // none of them empty
   a.partial = parts > 1 ? reinterpret_cast<float*>(base + w.offP) : nullptr;
-  if (w.bf16) e = w.bt == 256 ? launch_wide_out<__bf16, 256>(a, parts, s) : launch_wide_out<__bf16, 128>(a, parts, s);
-  else e = w.bt == 256 ? launch_wide_out<float, 256>(a, parts, s) : launch_wide_out<float, 128>(a, parts, s);
+  if (w.bf16) e = w.bt == 256 ? launch_wide_out<__bf16, 256>(a, q.A.kslow, q.B.kslow, parts, s) : launch_wide_out<__bf16, 128>(a, q.A.kslow, q.B.kslow, parts, s);
+  else e = w.bt == 256 ? launch_wide_out<float, 256>(a, q.A.kslow, q.B.kslow, parts, s) : launch_wide_out<float, 128>(a, q.A.kslow, q.B.kslow, parts, s);
   if (e != hipSuccess || parts == 1) return e;
   return join_parts(q, a.partial, parts, s);
 }
 
-// ------------------------------------------------------------------------------------------ sums of columns
-// Workgroup (64 columns, chunk of rows): four wavefronts take every fourth row; then the chunks are added up.
-constexpr int CHUNK = 256;
-template <typename T>
-__global__ __launch_bounds__(256) void column_sum_kernel(const T* g, const T* f, long long M, long long F, float scale, float* out) {
-  __shared__ float part[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long col = blockIdx.x * 64LL + lane, m0 = blockIdx.y * (long long)CHUNK, m1 = m0 + CHUNK < M ? m0 + CHUNK : M;
-  float s = 0.0f;
-  if (col < F)
-    for (long long m = m0 + wave; m < m1; m += 4) s += f ? widen(g[m * F + col]) * widen(f[m * F + col]) : widen(g[m * F + col]);
-  part[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && col < F) out[blockIdx.y * F + col] = scale * ((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+// ---- the backward pass: G = dY * D is laid out once for both products where a large tile reads it and it is not there already
+Product input_product(const BackwardArgs& b) {
+  Product q = {};
+  q.A = Operand{b.dY, b.D, b.F, b.ytype, 0};
+  q.B = Operand{b.W, nullptr, b.K, b.wtype, 1};
+  q.e = Epilogue{0, 0, b.xtype, b.scale, nullptr, nullptr, b.dX, nullptr};
+  q.I = b.M; q.J = b.K; q.Kc = b.F;
+  return q;
 }
-__global__ __launch_bounds__(256) void add_chunks_kernel(const float* part, long long chunks, long long F, float* out) {
-  const long long col = blockIdx.x * 256LL + threadIdx.x;
-  if (col >= F) return;
-  float s = 0.0f;
-  for (long long c = 0; c < chunks; ++c) s += part[c * F + col];
-  out[col] = s;
+Product weight_product(const BackwardArgs& b) {
+  Product q = {};
+  q.A = Operand{b.dY, b.D, b.F, b.ytype, 1};
+  q.B = Operand{b.X, nullptr, b.K, b.xtype, 1};
+  q.e = Epilogue{0, 0, 0, b.scale, nullptr, nullptr, b.dW, nullptr};
+  q.I = b.F; q.J = b.K; q.Kc = b.M;
+  return q;
 }
-
-__global__ __launch_bounds__(256) void zero_kernel(float* out, long long n) {
-  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) out[i] = 0.0f;
+// A gradient plane: rows along F, padded to whole slabs
+struct GradientPlane {
+  bool use[2];                        // [bf16]
+  long long ld[2];
+  size_t off[2], bytes;
+};
+bool reads_plane(const Product& q, bool bf16) {
+  const WidePlan w = wide_plan(q);
+  return w.wide && w.bf16 == bf16 && w.copyA;
+}
+GradientPlane gradient_plane(const BackwardArgs& b, const Product& x, const Product& w) {
+  GradientPlane g = {};
+  for (int bf16 = 0; bf16 < 2; ++bf16) {
+    g.use[bf16] = (b.dX && reads_plane(x, bf16)) || (b.dW && reads_plane(w, bf16));
+    if (!g.use[bf16]) continue;
+    const int m = slab_of(bf16);
+    g.ld[bf16] = (b.F + m - 1) / m * m;
+    g.off[bf16] = g.bytes;
+    g.bytes += up((size_t)b.M * g.ld[bf16] * (bf16 ? (b.D ? 4 : 2) : 4));
+  }
+  return g;
+}
+// The product with its gradient operand from the plane
+Product from_plane(Product q, const BackwardArgs& b, const GradientPlane& g, char* ws) {
+  const WidePlan w = wide_plan(q);
+  if (!w.wide || !w.copyA) return q;
+  Operand o = {};
+  o.p = ws + g.off[w.bf16];
+  o.ld = g.ld[w.bf16];
+  o.type = w.bf16;
+  o.kslow = q.A.kslow;
+  o.padded = 1;
+  o.parts = w.bf16 && b.D ? 2 : 1;
+  o.part = b.M * g.ld[w.bf16];
+  q.A = o;
+  return q;
 }
 
 }  // namespace
@@ -678,27 +829,46 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
   return join_parts(q, partial, parts, s);
 }
 
-size_t column_sum_workspace(long long M, long long F) {
-  const long long chunks = (M + CHUNK - 1) / CHUNK;
-  return chunks > 1 ? (size_t)chunks * (size_t)F * sizeof(float) : 0;
+// What the calls with these sizes and types need, whichever outputs are wanted (the pointers say only whether one is there)
+size_t backward_workspace(const BackwardArgs& b) {
+  size_t n = 0;
+  for (int wanted = 1; wanted < 4; ++wanted) {
+    BackwardArgs a = b;
+    if (!(wanted & 1)) a.dX = nullptr;
+    if (!(wanted & 2)) a.dW = nullptr;
+    const Product x = input_product(a), w = weight_product(a);
+    const GradientPlane g = gradient_plane(a, x, w);
+    size_t m = 0;
+    if (a.dX) m = product_workspace(from_plane(x, a, g, nullptr));
+    if (a.dW) { const size_t k = product_workspace(from_plane(w, a, g, nullptr)); m = m > k ? m : k; }
+    m += g.bytes;
+    n = n > m ? n : m;
+  }
+  return up(n) + up((size_t)chunks_of(b.M) * (size_t)b.F * sizeof(float));
 }
 
-hipError_t launch_column_sum(const Operand& G, long long M, long long F, float scale, float* db, void* ws, hipStream_t s) {
-  const long long chunks = (M + CHUNK - 1) / CHUNK;
-  float* out = chunks > 1 ? static_cast<float*>(ws) : db;
-  // (a grid's second dimension ends at 65535 chunks: the rows of taller layers are handed over in several launches)
-  for (long long c = 0; c < chunks; c += 65535) {
-    const long long n = chunks - c < 65535 ? chunks - c : 65535, rows = M - c * CHUNK, at = c * CHUNK * F;
-    const dim3 grid((unsigned)((F + 63) / 64), (unsigned)n);
-    if (G.type)
-      hipLaunchKernelGGL(column_sum_kernel<__bf16>, grid, dim3(256), 0, s, static_cast<const __bf16*>(G.p) + at,
-                         G.f ? static_cast<const __bf16*>(G.f) + at : nullptr, rows, F, scale, out + c * F);
-    else
-      hipLaunchKernelGGL(column_sum_kernel<float>, grid, dim3(256), 0, s, static_cast<const float*>(G.p) + at,
-                         G.f ? static_cast<const float*>(G.f) + at : nullptr, rows, F, scale, out + c * F);
+hipError_t launch_backward(const BackwardArgs& b, void* ws, size_t bytes, hipStream_t s) {
+  char* base = static_cast<char*>(ws);
+  const Product x = input_product(b), w = weight_product(b);
+  const GradientPlane g = gradient_plane(b, x, w);
+  const int chunks = chunks_of(b.M);
+  const size_t sums = up((size_t)chunks * (size_t)b.F * sizeof(float));
+  float* part = chunks > 1 ? reinterpret_cast<float*>(base + bytes / 256 * 256 - sums) : b.db;
+  bool summed = !b.db;
+  hipError_t e = hipSuccess;
+  for (int bf16 = 0; bf16 < 2 && e == hipSuccess; ++bf16)
+    if (g.use[bf16]) {
+      e = lay_out(b.dY, b.D, b.ytype, bf16, b.M, b.F, base + g.off[bf16], g.ld[bf16], b.scale, summed ? nullptr : part, s);
+      summed = true;
+    }
+  if (e == hipSuccess && !summed) e = lay_out(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, b.scale, part, s);
+  if (e == hipSuccess && b.db && chunks > 1) {
+    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(256), 0, s, part, chunks, b.F, b.db);
+    e = hipGetLastError();
   }
-  if (chunks > 1) hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((F + 255) / 256)), dim3(256), 0, s, out, chunks, F, db);
-  return hipGetLastError();
+  if (e == hipSuccess && b.dX) e = launch_product(from_plane(x, b, g, base), base + g.bytes, s);
+  if (e == hipSuccess && b.dW) e = launch_product(from_plane(w, b, g, base), base + g.bytes, s);
+  return e;
 }
 
 hipError_t launch_zero(float* out, long long n, hipStream_t s) {

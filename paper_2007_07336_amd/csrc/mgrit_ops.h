@@ -12,6 +12,9 @@ struct Operand {
   long long ld;
   int type;                          // 0 float, 1 bf16
   int kslow;
+  // set for planes in the workspace: rows end in zeros up to ld, and the operand is the sum of `parts` planes, `part` entries apart
+  int padded, parts;
+  long long part;
 };
 // What becomes of a sum.  Forward (fwd): z = sum + bias, out = R + scale act(z), D = scale act'(z); else out = scale sum.
 struct Epilogue {
@@ -30,10 +33,18 @@ struct Product {
 
 size_t     product_workspace(const Product& q);
 hipError_t launch_product(const Product& q, void* ws, hipStream_t s);
-// db[f] = scale * sum over the rows of G(., f), G = dY or dY * D
-size_t     column_sum_workspace(long long M, long long F);
-hipError_t launch_column_sum(const Operand& G, long long M, long long F, float scale, float* db, void* ws, hipStream_t s);
 
+// The backward pass of an end layer: G = dY * D (D null: dY, with `scale` on every result), dX = G W, dW = G^T X, db = column
+// sums of G; dX, dW, db null where they are not wanted.
+struct BackwardArgs {
+  long long M, K, F;
+  int xtype, wtype, ytype;
+  float scale;
+  const void* X;  const void* W;  const void* D;  const void* dY;
+  void* dX;  float* dW;  float* db;
+};
+size_t     backward_workspace(const BackwardArgs& b);
+hipError_t launch_backward(const BackwardArgs& b, void* ws, size_t bytes, hipStream_t s);   // bytes: backward_workspace or more
 hipError_t launch_zero(float* out, long long n, hipStream_t s);
 
 struct LossArgs {

@@ -34,26 +34,9 @@ Product forward_product(const mgrit_affine_t* p, const void* X, const void* W, c
   q.I = p->M; q.J = p->F; q.Kc = p->K;
   return q;
 }
-Operand gradient(const mgrit_affine_t* p, const void* D, const void* dY, int kslow) {
-  return Operand{dY, D, p->F, p->ytype, kslow};
-}
-// the factors hold the layer's scale already
-inline float backward_scale(const mgrit_affine_t* p, const void* D) { return D ? 1.0f : p->scale; }
-Product input_product(const mgrit_affine_t* p, const void* W, const void* D, const void* dY, void* dX) {
-  Product q = {};
-  q.A = gradient(p, D, dY, 0);
-  q.B = Operand{W, nullptr, p->K, p->wtype, 1};
-  q.e = Epilogue{0, 0, p->xtype, backward_scale(p, D), nullptr, nullptr, dX, nullptr};
-  q.I = p->M; q.J = p->K; q.Kc = p->F;
-  return q;
-}
-Product weight_product(const mgrit_affine_t* p, const void* X, const void* D, const void* dY, float* dW) {
-  Product q = {};
-  q.A = gradient(p, D, dY, 1);
-  q.B = Operand{X, nullptr, p->K, p->xtype, 1};
-  q.e = Epilogue{0, 0, MGRIT_FP32, backward_scale(p, D), nullptr, nullptr, dW, nullptr};
-  q.I = p->F; q.J = p->K; q.Kc = p->M;
-  return q;
+BackwardArgs backward_args(const mgrit_affine_t* p, const void* X, const void* W, const void* D, const void* dY, void* dX, float* dW, float* db) {
+  // (the factors hold the layer's scale already)
+  return BackwardArgs{p->M, p->K, p->F, p->xtype, p->wtype, p->ytype, D ? 1.0f : p->scale, X, W, D, dY, dX, dW, db};
 }
 inline size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 
@@ -102,13 +85,11 @@ size_t mgrit_affine_workspace_bytes(const mgrit_affine_t* p) {
 
 size_t mgrit_affine_backward_workspace_bytes(const mgrit_affine_t* p) {
   if (check_affine(p) != MGRIT_OK || p->M == 0) return 0;
-  size_t n = 0;
-  for (int with = 0; with < 2; ++with) {       // with and without factors (only whether they are there is looked at)
-    const void* D = with ? static_cast<const void*>(p) : nullptr;
-    n = larger(n, product_workspace(input_product(p, nullptr, D, nullptr, nullptr)));
-    n = larger(n, product_workspace(weight_product(p, nullptr, D, nullptr, nullptr)));
-  }
-  return larger(n, column_sum_workspace(p->M, p->F));
+  // whether a call brings factors and what it wants is not known here: room for all of it (the pointers only say what is there)
+  void* there = const_cast<mgrit_affine_t*>(p);
+  float* also = static_cast<float*>(there);
+  const size_t with = backward_workspace(backward_args(p, there, there, there, there, there, also, also));
+  return larger(with, backward_workspace(backward_args(p, there, there, nullptr, there, there, also, also)));
 }
 
 int32_t mgrit_affine_forward(const mgrit_affine_t* p, const void* X, const void* W, const float* b, const void* R, void* Y,
@@ -144,9 +125,7 @@ int32_t mgrit_affine_backward(const mgrit_affine_t* p, const void* X, const void
   for (const void* q : {X, W, D, dY, static_cast<const void*>(dX), static_cast<const void*>(workspace)})
     if (!aligned_to(q, 16)) return MGRIT_ERR_POINTER;
   if (workspace_bytes < need) return MGRIT_ERR_WORKSPACE;
-  if (dX) e = launch_product(input_product(p, W, D, dY, dX), workspace, s);
-  if (e == hipSuccess && dW) e = launch_product(weight_product(p, X, D, dY, dW), workspace, s);
-  if (e == hipSuccess && db) e = launch_column_sum(gradient(p, D, dY, 1), p->M, p->F, backward_scale(p, D), db, workspace, s);
+  if (dX || dW || db) e = launch_backward(backward_args(p, X, W, D, dY, dX, dW, db), workspace, need, s);
   return e == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
 }
 
