@@ -280,42 +280,65 @@ MGRIT_FP32, MGRIT_BF16 = 0, 1
 MGRIT_LOSS_SUM, MGRIT_LOSS_MEAN = 0, 1
 
 
-def _torch_type(t: int):
-    import torch
-    return {MGRIT_FP32: torch.float32, MGRIT_BF16: torch.bfloat16}.get(t)
+_TYPES = []                                      # torch types by their number here, filled at the first use (torch is imported late)
 
 
-def _check(where, **tensors):
-    """tensors: name = (tensor or None, number of values, torch type).  What the C side cannot see of a tensor: that it
-    has this many values of this type one behind the other, on the GPU of the others.  Returns that GPU, which the call
-    runs on whatever the current one is."""
-    given = [(name, v) for name, v in tensors.items() if v[0] is not None]
-    for name, (t, count, dtype) in given:
-        if dtype is None or t.dtype != dtype:
+def _torch_types():
+    if not _TYPES:
+        import torch
+        _TYPES.extend((torch.float32, torch.bfloat16, torch.int64, torch.cuda, torch._C._cuda_getCurrentRawStream))
+    return _TYPES
+
+
+def _type(types, kind):
+    return types[kind] if kind in (MGRIT_FP32, MGRIT_BF16) else None
+
+
+def _check(where, items):
+    """items: (name, tensor or None, number of values or None, torch type or None).  What the C side cannot see of a tensor: that it
+    has this many values of this type one behind the other, on the GPU of the others.  Returns the index of that GPU, which the
+    call runs on whatever the current one is; None if there is no tensor."""
+    device = None
+    for name, t, count, dtype in items:
+        if t is None:
+            continue
+        d = t.get_device()
+        if device is None:
+            device = d
+        if d < 0 or d != device or t.dtype is not dtype or (count is not None and t.numel() != count) or not t.is_contiguous():
+            break
+    else:
+        return device
+    given = [i for i in items if i[1] is not None]
+    for name, t, count, dtype in given:          # something does not fit: say what
+        if t.dtype is not dtype:
             raise ValueError(f"{where}: {name} has type {t.dtype}, not {dtype}")
         if count is not None and t.numel() != count:
             raise ValueError(f"{where}: {name} has {t.numel()} values, not {count}")
         if not t.is_contiguous():
             raise ValueError(f"{where}: {name} is not contiguous")
-    device = None
-    for name, (t, _, _) in given:
+    for name, t, _, _ in given:
         if not t.is_cuda:
             raise ValueError(f"{where}: {name} is not on a GPU")
-        if device is not None and t.device != device:
-            raise ValueError(f"{where}: {name} is on {t.device}, others on {device}")
-        device = t.device
-    return device
+        raise_on = [n for n, u, _, _ in given if u.device != t.device]
+        if raise_on:
+            raise ValueError(f"{where}: {name} is on {t.device}, {raise_on[0]} is not")
+    raise ValueError(f"{where}: tensors that do not fit")
 
 
 def _call(where, device, stream, check, call):
-    """call(stream handle) on `device`, on `stream` or that device's current stream."""
-    import torch
+    """call(stream handle) with GPU `device` the current one, on `stream` or that GPU's current stream."""
     if device is None:
         raise ValueError(f"{where}: no tensor given")
-    if stream is not None and stream.device != device:
-        raise ValueError(f"{where}: the stream is on {stream.device}, the tensors on {device}")
-    with torch.cuda.device(device):
-        rc = call(_stream(stream))
+    cuda, raw_stream = _torch_types()[3:5]
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"{where}: the stream is on GPU {stream.device_index}, the tensors on GPU {device}")
+    handle = (raw_stream(device) if stream is None else stream.cuda_stream) or None
+    if cuda.current_device() == device:
+        rc = call(handle)
+    else:
+        with cuda.device(device):
+            rc = call(handle)
     if check and rc != MGRIT_OK:
         raise MgritError(rc, where)
     return rc
@@ -337,23 +360,28 @@ def mgrit_affine_backward_workspace_bytes(p: mgrit_affine_t) -> int:
     return int(lib().mgrit_affine_backward_workspace_bytes(ctypes.byref(p)))
 
 
+def _workspace(t):
+    return "workspace", t, None, None if t is None else t.dtype
+
+
 def mgrit_affine_forward(p: mgrit_affine_t, X, W, b, R, Y, D, workspace, *, stream=None, check=True):
     """Y = R + scale act(X W^T + b), D = scale act'(..): b, R, D may be None, and the workspace where none is needed."""
-    where, (x, w, y) = "mgrit_affine_forward", map(_torch_type, (p.xtype, p.wtype, p.ytype))
-    device = _check(where, X=(X, p.M * p.K, x), W=(W, p.F * p.K, w), b=(b, p.F, _torch_type(0)), R=(R, p.M * p.F, y),
-                    Y=(Y, p.M * p.F, y), D=(D, p.M * p.F, y), workspace=(workspace, None, workspace is not None and workspace.dtype))
+    where, T = "mgrit_affine_forward", _torch_types()
+    M, K, F, y = p.M, p.K, p.F, _type(T, p.ytype)
+    device = _check(where, (("X", X, M * K, _type(T, p.xtype)), ("W", W, F * K, _type(T, p.wtype)), ("b", b, F, T[0]), ("R", R, M * F, y),
+                            ("Y", Y, M * F, y), ("D", D, M * F, y), _workspace(workspace)))
     return _call(where, device, stream, check, lambda s: lib().mgrit_affine_forward(
-        ctypes.byref(p), _ptr(X), _ptr(W), _ptr(b), _ptr(R), _ptr(Y), _ptr(D), _ptr(workspace), _size(workspace), s))
+        p, _ptr(X), _ptr(W), _ptr(b), _ptr(R), _ptr(Y), _ptr(D), _ptr(workspace), _size(workspace), s))
 
 
 def mgrit_affine_backward(p: mgrit_affine_t, X, W, D, dY, dX, dW, db, workspace, *, stream=None, check=True):
     """With G = dY * D (D None, identity only: scale dY): dX = G W, dW = G^T X, db = column sums of G; each may be None."""
-    where, (x, w, y) = "mgrit_affine_backward", map(_torch_type, (p.xtype, p.wtype, p.ytype))
-    f = _torch_type(0)
-    device = _check(where, X=(X, p.M * p.K, x), W=(W, p.F * p.K, w), D=(D, p.M * p.F, y), dY=(dY, p.M * p.F, y), dX=(dX, p.M * p.K, x),
-                    dW=(dW, p.F * p.K, f), db=(db, p.F, f), workspace=(workspace, None, workspace is not None and workspace.dtype))
+    where, T = "mgrit_affine_backward", _torch_types()
+    M, K, F, x, y = p.M, p.K, p.F, _type(T, p.xtype), _type(T, p.ytype)
+    device = _check(where, (("X", X, M * K, x), ("W", W, F * K, _type(T, p.wtype)), ("D", D, M * F, y), ("dY", dY, M * F, y), ("dX", dX, M * K, x),
+                            ("dW", dW, F * K, T[0]), ("db", db, F, T[0]), _workspace(workspace)))
     return _call(where, device, stream, check, lambda s: lib().mgrit_affine_backward(
-        ctypes.byref(p), _ptr(X), _ptr(W), _ptr(D), _ptr(dY), _ptr(dX), _ptr(dW), _ptr(db), _ptr(workspace), _size(workspace), s))
+        p, _ptr(X), _ptr(W), _ptr(D), _ptr(dY), _ptr(dX), _ptr(dW), _ptr(db), _ptr(workspace), _size(workspace), s))
 
 
 def make_loss(*, B, V, dtype=MGRIT_FP32, reduction=MGRIT_LOSS_MEAN, scale=1.0) -> mgrit_loss_t:
@@ -366,33 +394,32 @@ def mgrit_cross_entropy_workspace_bytes(p: mgrit_loss_t) -> int:
 
 def mgrit_cross_entropy(p: mgrit_loss_t, logits, labels, loss, row_loss, grad, workspace, *, stream=None, check=True):
     """loss (1 value), row_loss (B) and grad (like logits, may be logits) may each be None; labels are int64."""
-    import torch
-    where, t, f = "mgrit_cross_entropy", _torch_type(p.dtype), torch.float32
-    device = _check(where, logits=(logits, p.B * p.V, t), labels=(labels, p.B, torch.int64), loss=(loss, 1, f), row_loss=(row_loss, p.B, f),
-                    grad=(grad, p.B * p.V, t), workspace=(workspace, None, workspace is not None and workspace.dtype))
+    where, T = "mgrit_cross_entropy", _torch_types()
+    t, B, V = _type(T, p.dtype), p.B, p.V
+    device = _check(where, (("logits", logits, B * V, t), ("labels", labels, B, T[2]), ("loss", loss, 1, T[0]), ("row_loss", row_loss, B, T[0]),
+                            ("grad", grad, B * V, t), _workspace(workspace)))
     return _call(where, device, stream, check, lambda s: lib().mgrit_cross_entropy(
-        ctypes.byref(p), _ptr(logits), _ptr(labels), _ptr(loss), _ptr(row_loss), _ptr(grad), _ptr(workspace), _size(workspace), s))
+        p, _ptr(logits), _ptr(labels), _ptr(loss), _ptr(row_loss), _ptr(grad), _ptr(workspace), _size(workspace), s))
 
 
 class TensorList:
     """Tensors to clip: the descriptors handed to the library, and the tensors, which are kept alive."""
 
     def __init__(self, src: Sequence, dst: Optional[Sequence] = None):
-        where, dst = "make_tensor_list", list(src) if dst is None else list(dst)
+        where, dst, T = "make_tensor_list", list(src) if dst is None else list(dst), _torch_types()
         self.src, self.dst = list(src), dst
         if len(self.src) != len(self.dst):
             raise ValueError(f"{where}: {len(self.src)} tensors, {len(self.dst)} results")
         self.array = (mgrit_tensor_t * max(1, len(self.src)))()
         self.device = None
         for i, (a, b) in enumerate(zip(self.src, self.dst)):
-            kind = [k for k in (MGRIT_FP32, MGRIT_BF16) if _torch_type(k) == a.dtype]
-            if not kind:
+            if a.dtype not in T[:2]:
                 raise ValueError(f"{where}: tensor {i} has type {a.dtype}")
-            device = _check(where, **{f"tensor {i}": (a, None, a.dtype), f"result {i}": (b, a.numel(), a.dtype)})
+            device = _check(where, ((f"tensor {i}", a, None, a.dtype), (f"result {i}", b, a.numel(), a.dtype)))
             if self.device is not None and device != self.device:
-                raise ValueError(f"{where}: tensor {i} is on {device}, others on {self.device}")
+                raise ValueError(f"{where}: tensor {i} is on GPU {device}, others on GPU {self.device}")
             self.device = device
-            self.array[i] = mgrit_tensor_t(src=_ptr(a), dst=_ptr(b), count=a.numel(), dtype=kind[0])
+            self.array[i] = mgrit_tensor_t(src=_ptr(a), dst=_ptr(b), count=a.numel(), dtype=T.index(a.dtype))
 
     def __len__(self):
         return len(self.src)
@@ -410,14 +437,15 @@ def mgrit_clip_workspace_bytes(tensors: TensorList) -> int:
 def mgrit_clip_gradients(tensors: TensorList, max_norm: float, norm, workspace, *, want_norm=False, stream=None, check=True):
     """dst = src * min(1, max_norm / norm).  norm: one float on the GPU or None.  Returns (return code, the norm if want_norm, which
     waits for the GPU)."""
-    import torch
-    where, host = "mgrit_clip_gradients", ctypes.c_double(0.0)
-    device = _check(where, norm=(norm, 1, torch.float32), workspace=(workspace, None, workspace is not None and workspace.dtype))
-    if device is not None and tensors.device is not None and device != tensors.device:
-        raise ValueError(f"{where}: norm or workspace on {device}, the tensors on {tensors.device}")
-    rc = _call(where, device or tensors.device, stream, check, lambda s: lib().mgrit_clip_gradients(
-        tensors.array, len(tensors), max_norm, _ptr(norm), ctypes.byref(host) if want_norm else None, _ptr(workspace), _size(workspace), s))
-    return rc, host.value if want_norm else None
+    where, host, T = "mgrit_clip_gradients", ctypes.c_double(0.0) if want_norm else None, _torch_types()
+    device = _check(where, (("norm", norm, 1, T[0]), _workspace(workspace)))
+    if device is None:
+        device = tensors.device
+    elif tensors.device is not None and device != tensors.device:
+        raise ValueError(f"{where}: norm or workspace on GPU {device}, the tensors on GPU {tensors.device}")
+    rc = _call(where, device, stream, check, lambda s: lib().mgrit_clip_gradients(
+        tensors.array, len(tensors), max_norm, _ptr(norm), None if host is None else ctypes.byref(host), _ptr(workspace), _size(workspace), s))
+    return rc, None if host is None else host.value
 
 
 TRACE_CLASSES = ("dense_step_kernel<float,64,64>", "dense_step_kernel<float,128,128>",

@@ -122,6 +122,19 @@ __device__ __forceinline__ void finish8(const Epilogue& e, long long at, float (
   if (e.D) put8(static_cast<OT*>(e.D) + at, d, whole, left);
 }
 
+// ------------------------------------------------------------------------------------------ from memory to LDS
+typedef __attribute__((address_space(3))) void LdsPtr;
+// 16 bytes per lane from base + each lane's offset + along to LDS address `to` and the 1008 bytes behind it, in lane order; zeros from
+// base + room on.  In assembly so that the compiler does not see a load that writes LDS: it would hold back every transposing read
+// until all loads have arrived (backward pass of 8192 x 4096 x 4096 bf16: 1781 us).  There is no result register, and what is
+// waited for stands in the kernel.
+typedef int int4v __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void to_lds(const char* base, int offset, int along, unsigned room, unsigned to) {
+  const unsigned long long b = reinterpret_cast<unsigned long long>(base);
+  const int4v rsrc = {(int)(unsigned)b, (int)(unsigned)(b >> 32), (int)room, 0x00020000};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(to), "v"(offset), "s"(rsrc), "s"(along) : "memory");
+}
+
 // ------------------------------------------------------------------------------------------ any size, any order
 // Tile of 64 x 64 outputs, four wavefronts with 32 x 32 of them each; slabs of the contraction go through registers (the
 // next one is in flight while this one is multiplied) into LDS, rows along k.  With float operands on the float matrix
@@ -300,23 +313,419 @@ hipError_t launch_types(const Product& q, float* partial, int parts, hipStream_t
   return launch_tiles<float, float, float, HF, AS, BS>(q, partial, parts, s);
 }
 
+// ------------------------------------------------------------------------------------------ few rows on one side
+// At most 64 rows of one operand (the few) against many of the other (the stream), both with k contiguous: a head's classes, or a
+// serving batch on wide weights.  Bound by reading the stream once: a workgroup has SB blocks of 16 stream rows and all of the
+// few's, its wavefronts share the contraction, each with slabs of its own in LDS, D of them in flight, and no barrier but the one
+// before the sums.  Through LDS because the 16 x 16 matrix instructions want 16 rows in 16 consecutive lanes, and loads are only
+// fast if consecutive lanes read one row (64 rows x 4096 x 4096 bf16: 62 cache accesses a load straight into registers, 22 us).
+// Rows that are no multiples of 16 bytes, and what is left of the contraction, go straight into registers all the same.
+typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T, typename CT> struct Row8;                  // eight k of a row
+template <> struct Row8<__bf16, __bf16> {
+  bf16x8 v;
+  __device__ __forceinline__ void load(const __bf16* p) { v = *reinterpret_cast<const bf16x8u*>(p); }
+  __device__ __forceinline__ void load(const __bf16* p, long long n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : __bf16(0.0f);
+  }
+  __device__ __forceinline__ bf16x8 all() const { return v; }
+};
+template <> struct Row8<__bf16, float> : Row8<__bf16, __bf16> {
+  __device__ __forceinline__ float at(int j) const { return widen(v[j]); }
+};
+template <> struct Row8<float, float> {
+  floatx4 v[2];
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = *reinterpret_cast<const floatx4u*>(p);
+    v[1] = *reinterpret_cast<const floatx4u*>(p + 4);
+  }
+  __device__ __forceinline__ void load(const float* p, long long n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j / 4][j % 4] = j < n ? p[j] : 0.0f;
+  }
+  __device__ __forceinline__ float at(int j) const { return v[j / 4][j % 4]; }
+};
+__device__ __forceinline__ void multiply16(const Row8<__bf16, __bf16>& a, const Row8<__bf16, __bf16>& b, floatx4& c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.all(), b.all(), c, 0, 0, 0);
+}
+template <typename A, typename B> __device__ __forceinline__ void multiply16(const A& a, const B& b, floatx4& c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.at(j), b.at(j), c, 0, 0, 0);
+}
+
+// A slab of 16 rows in LDS: panels of 128 bytes a row, 16-byte pieces in the order piece ^ (row / 2 & 7).  Eight k of a row:
+// step `st` of 32 k, quarter g.
+template <typename T, typename CT> __device__ __forceinline__ void from_slab(Row8<T, CT>& r, const unsigned char* block, int st, int r16, int g) {
+  const int turn = (r16 >> 1) & 7;
+  if constexpr (sizeof(T) == 2) {
+    r.v = *reinterpret_cast<const bf16x8*>(block + r16 * 128 + (((st * 4 + g) ^ turn) << 4));
+  } else {
+    block += st * 2048 + r16 * 128;
+    r.v[0] = *reinterpret_cast<const floatx4*>(block + (((2 * g) ^ turn) << 4));
+    r.v[1] = *reinterpret_cast<const floatx4*>(block + (((2 * g + 1) ^ turn) << 4));
+  }
+}
+template <typename TS, typename TF, int SB, int FB> struct FewShape {
+  static constexpr int K = sizeof(TS) == 2 || sizeof(TF) == 2 ? 64 : 32;       // of a slab
+  static constexpr int PS = K * (int)sizeof(TS) / 128, PF = K * (int)sizeof(TF) / 128, SLAB = (SB * PS + FB * PF) * 2048;   // panels; bytes
+  static constexpr int ROOM = 152 * 1024, W = 8 * 2 * SLAB <= ROOM ? 8 : 4;     // wavefronts
+  static constexpr int FIT = ROOM / (W * SLAB), D = FIT > 4 ? 4 : FIT;         // slabs
+  static_assert(D >= 2, "two slabs in turn");
+};
+
+// SWAP: the stream is A (out's rows), the few are B (out's columns); otherwise the other way round.
+template <typename TS, typename TF, typename CT, int SB, int FB, bool SWAP>
+__global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_few_kernel(Product q, long long kpart, float* partial, int slabs_in_lds) {
+  typedef FewShape<TS, TF, SB, FB> Sh;
+  constexpr int NS = SB * 16, NF = FB * 16, PITCH = SWAP ? NF + 1 : NS + 4, U = FB >= 4 ? 1 : 2, FEW_WAVES = Sh::W;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  float* sums = reinterpret_cast<float*>(lds);
+  constexpr int SUMS = (SWAP ? NS : NF) * PITCH;                               // of one wavefront
+  static_assert(FEW_WAVES * SUMS * 4 <= Sh::W * Sh::SLAB * Sh::D, "the sums take the slabs' place");
+  const Operand &so = SWAP ? q.A : q.B, &fo = SWAP ? q.B : q.A;
+  const long long ns = SWAP ? q.I : q.J, nf = SWAP ? q.J : q.I, s0 = (long long)logical_block() * NS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, k8 = (lane >> 4) * 8;
+  const long long p0 = blockIdx.y * kpart, p1 = p0 + kpart < q.Kc ? p0 + kpart : q.Kc;
+  const long long kw = ((p1 - p0 + FEW_WAVES - 1) / FEW_WAVES + 31) / 32 * 32;
+  long long k = p0 + wave * kw;
+  const long long kend = k + kw < p1 ? k + kw : p1;
+  const TS* ps[SB];
+  const TF* pf[FB];
+#pragma unroll
+  for (int i = 0; i < SB; ++i) { const long long r = s0 + i * 16 + r16; ps[i] = static_cast<const TS*>(so.p) + (r < ns ? r : ns - 1) * so.ld + k8; }
+#pragma unroll
+  for (int i = 0; i < FB; ++i) { const long long r = i * 16 + r16; pf[i] = static_cast<const TF*>(fo.p) + (r < nf ? r : nf - 1) * fo.ld + k8; }
+  floatx4 acc[SB][FB];
+#pragma unroll
+  for (int i = 0; i < SB; ++i)
+#pragma unroll
+    for (int j = 0; j < FB; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (slabs_in_lds) {
+    // (offsets from the first row of the workgroup and of the few; instruction h of a block takes its rows 8 h .. 8 h + 7)
+    int offS[SB][2], offF[FB][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = 8 * h + (lane >> 3), piece = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+#pragma unroll
+      for (int i = 0; i < SB; ++i) offS[i][h] = (int)((s0 + i * 16 + r < ns ? i * 16 + r : ns - 1 - s0) * so.ld * (int)sizeof(TS)) + piece;
+#pragma unroll
+      for (int j = 0; j < FB; ++j) offF[j][h] = (int)((j * 16 + r < nf ? j * 16 + r : nf - 1) * fo.ld * (int)sizeof(TF)) + piece;
+    }
+    const char* baseS = static_cast<const char*>(so.p) + s0 * so.ld * (int)sizeof(TS);
+    const char* baseF = static_cast<const char*>(fo.p);
+    const int n = kend > k ? (int)((kend - k) / Sh::K) : 0;
+    const unsigned mine = (unsigned)(unsigned long long)(LdsPtr*)lds + wave * Sh::D * Sh::SLAB;
+    const unsigned char* my = lds + wave * Sh::D * Sh::SLAB;
+    constexpr int LOADS = 2 * (SB * Sh::PS + FB * Sh::PF);
+    auto issue = [&](int t) {                       // slab t to its place; behind the last one the last again, so that the count of loads is the same
+      const long long at = k + (long long)(t < n ? t : n - 1) * Sh::K;
+      const unsigned to = mine + t % Sh::D * Sh::SLAB;
+#pragma unroll
+      for (int i = 0; i < SB; ++i)
+#pragma unroll
+        for (int x = 0; x < Sh::PS; ++x)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) to_lds(baseS, offS[i][h], (int)(at * (int)sizeof(TS)) + x * 128, 0xffffffffu, to + (i * Sh::PS + x) * 2048 + h * 1024);
+#pragma unroll
+      for (int j = 0; j < FB; ++j)
+#pragma unroll
+        for (int x = 0; x < Sh::PF; ++x)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            to_lds(baseF, offF[j][h], (int)(at * (int)sizeof(TF)) + x * 128, 0xffffffffu, to + ((SB * Sh::PS) + j * Sh::PF + x) * 2048 + h * 1024);
+    };
+    if (n > 0) {
+#pragma unroll
+      for (int t = 0; t < Sh::D - 1; ++t) issue(t);
+      for (int t = 0; t < n; ++t) {
+        // what was read from the place that is filled next has arrived; then all but the last D - 1 slabs' loads
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue(t + Sh::D - 1);
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS * (Sh::D - 1)) : "memory");
+        const unsigned char* slab = my + t % Sh::D * Sh::SLAB;
+#pragma unroll
+        for (int st = 0; st < Sh::K / 32; ++st) {
+          Row8<TS, CT> a[SB];
+          Row8<TF, CT> b[FB];
+#pragma unroll
+          for (int i = 0; i < SB; ++i) from_slab(a[i], slab + i * Sh::PS * 2048, st, r16, lane >> 4);
+#pragma unroll
+          for (int j = 0; j < FB; ++j) from_slab(b[j], slab + (SB * Sh::PS + j * Sh::PF) * 2048, st, r16, lane >> 4);
+#pragma unroll
+          for (int i = 0; i < SB; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) multiply16(a[i], b[j], acc[i][j]);
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      k += (long long)n * Sh::K;
+    }
+  }
+  // two sets of registers: one is on its way while the other is multiplied
+  Row8<TS, CT> a[2][U][SB];
+  Row8<TF, CT> b[2][U][FB];
+  auto load = [&](int set, long long at) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int i = 0; i < SB; ++i) a[set][u][i].load(ps[i] + at + 32 * u);
+#pragma unroll
+      for (int j = 0; j < FB; ++j) b[set][u][j].load(pf[j] + at + 32 * u);
+    }
+  };
+  auto multiply = [&](int set) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < SB; ++i)
+#pragma unroll
+        for (int j = 0; j < FB; ++j) multiply16(a[set][u][i], b[set][u][j], acc[i][j]);
+  };
+  const int whole = kend > k ? (int)((kend - k) / (32 * U)) : 0;
+  if (whole) load(0, k);
+  int n = 0;
+  for (; n + 2 <= whole; n += 2, k += 64 * U) {
+    load(1, k + 32 * U);
+    multiply(0);
+    if (n + 2 < whole) load(0, k + 64 * U);
+    multiply(1);
+  }
+  if (n < whole) { multiply(0); k += 32 * U; }
+  for (; k < kend; k += 32) {
+    const long long left = kend - k - k8;
+#pragma unroll
+    for (int i = 0; i < SB; ++i) a[0][0][i].load(ps[i] + k, left);
+#pragma unroll
+    for (int j = 0; j < FB; ++j) b[0][0][j].load(pf[j] + k, left);
+#pragma unroll
+    for (int i = 0; i < SB; ++i)
+#pragma unroll
+      for (int j = 0; j < FB; ++j) multiply16(a[0][0][i], b[0][0][j], acc[i][j]);
+  }
+  __syncthreads();
+  // lane: row r16 of the few, four rows of the stream
+#pragma unroll
+  for (int i = 0; i < SB; ++i)
+#pragma unroll
+    for (int j = 0; j < FB; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int s = i * 16 + (lane >> 4) * 4 + r, f = j * 16 + r16;
+        sums[wave * SUMS + (SWAP ? s * PITCH + f : f * PITCH + s)] = acc[i][j][r];
+      }
+  __syncthreads();
+  for (int n = threadIdx.x; n < NS * NF; n += 64 * FEW_WAVES) {
+    const int s = SWAP ? n / NF : n % NS, f = SWAP ? n % NF : n / NS;
+    if (s0 + s >= ns || f >= nf) continue;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) v += sums[w * SUMS + (SWAP ? s * PITCH + f : f * PITCH + s)];
+    const long long col = SWAP ? f : s0 + s, at = (SWAP ? s0 + s : f) * q.J + col;
+    if (partial) partial[blockIdx.y * q.I * q.J + at] = v;
+    else if (q.e.otype) finish<__bf16>(q.e, at, col, v);
+    else finish<float>(q.e, at, col, v);
+  }
+}
+
+struct FewPlan {
+  bool few, swap;
+  int sb, fb, parts;
+  long long kpart;
+};
+// Where one side has at most 64 rows.  Workgroups: one for 16 stream rows, for 32 from 16384 on against at most 16; the contraction is shared between
+// workgroups where there are fewer than two for each of the 256 compute units, down to 1024 a part (128 for each wavefront).
+FewPlan few_plan(const Product& q) {
+  FewPlan p = {};
+  const long long few = q.I < q.J ? q.I : q.J, many = q.I < q.J ? q.J : q.I;
+  p.few = !q.A.kslow && !q.B.kslow && !q.A.f && few <= 64 && many <= (1LL << 31);
+  if (!p.few) return p;
+  p.swap = q.I >= q.J;
+  p.fb = few <= 16 ? 1 : few <= 32 ? 2 : 4;
+  p.sb = p.fb == 1 && many >= 16384 ? 2 : 1;
+  const long long wgs = (many + 16 * p.sb - 1) / (16 * p.sb);
+  long long parts = wgs >= 256 ? 1 : (512 + wgs - 1) / wgs;
+  if (parts > q.Kc / 1024) parts = q.Kc / 1024 > 1 ? q.Kc / 1024 : 1;
+  p.kpart = ((q.Kc + parts - 1) / parts + 31) / 32 * 32;
+  p.parts = (int)((q.Kc + p.kpart - 1) / p.kpart);
+  return p;
+}
+template <typename TS, typename TF, typename CT, int SB, int FB, bool SWAP>
+hipError_t launch_few_kernel(const Product& q, const FewPlan& p, float* partial, hipStream_t s) {
+  typedef FewShape<TS, TF, SB, FB> Sh;
+  static LdsOptIn opt;
+  const long long many = SWAP ? q.I : q.J;
+  const size_t smem = Sh::W * Sh::D * Sh::SLAB;
+  const hipError_t e = opt.raise(reinterpret_cast<const void*>(&product_few_kernel<TS, TF, CT, SB, FB, SWAP>), smem);
+  if (e != hipSuccess) return e;
+  // (16-byte pieces of rows; offsets within the few's 64 rows and along a row are 31 bits)
+  const Operand &so = SWAP ? q.A : q.B, &fo = SWAP ? q.B : q.A;
+  const int in_lds = so.ld * sizeof(TS) % 16 == 0 && fo.ld * sizeof(TF) % 16 == 0 && q.Kc <= (1LL << 22);
+  hipLaunchKernelGGL((product_few_kernel<TS, TF, CT, SB, FB, SWAP>), dim3((unsigned)((many + 16 * SB - 1) / (16 * SB)), (unsigned)p.parts), dim3(64 * Sh::W),
+                     smem, s, q, p.kpart, p.parts > 1 ? partial : nullptr, in_lds);
+  return hipGetLastError();
+}
+template <typename TS, typename TF, typename CT, int SB, int FB>
+hipError_t launch_few_swap(const Product& q, const FewPlan& p, float* partial, hipStream_t s) {
+  return p.swap ? launch_few_kernel<TS, TF, CT, SB, FB, true>(q, p, partial, s) : launch_few_kernel<TS, TF, CT, SB, FB, false>(q, p, partial, s);
+}
+template <typename TS, typename TF, typename CT>
+hipError_t launch_few_sizes(const Product& q, const FewPlan& p, float* partial, hipStream_t s) {
+  if (p.sb == 2) return launch_few_swap<TS, TF, CT, 2, 1>(q, p, partial, s);
+  return p.fb == 1 ? launch_few_swap<TS, TF, CT, 1, 1>(q, p, partial, s)
+       : p.fb == 2 ? launch_few_swap<TS, TF, CT, 1, 2>(q, p, partial, s) : launch_few_swap<TS, TF, CT, 1, 4>(q, p, partial, s);
+}
+hipError_t launch_few(const Product& q, const FewPlan& p, float* partial, hipStream_t s) {
+  const int ts = p.swap ? q.A.type : q.B.type, tf = p.swap ? q.B.type : q.A.type;
+  if (ts && tf) return launch_few_sizes<__bf16, __bf16, __bf16>(q, p, partial, s);
+  if (ts) return launch_few_sizes<__bf16, float, float>(q, p, partial, s);
+  if (tf) return launch_few_sizes<float, __bf16, float>(q, p, partial, s);
+  return launch_few_sizes<float, float, float>(q, p, partial, s);
+}
+
+// ------------------------------------------------------------------------------------------ thin gradients
+// The backward pass where G has at most 16 columns (a head's classes) or rows (samples): both of its products in one pass over
+// the large operand S, whose rows go with G's long side:
+//   outS[r][k] = sum_t G(r, t) T[t][k],   outT[t][k] = sum_r G(r, t) S[r][k]
+// (few classes: S = X, T = W, outS = dX, outT = dW; few samples: S = W, T = X, outS = dW, outT = dX).  Bound by reading S and writing
+// outS: 2 NT multiplications for two values that pass are within what the vector unit does at that rate.  Workgroup: 256 k by a chunk of
+// rows, a wavefront every fourth row; a lane has four k of all of T and of outT in registers, G lies in LDS.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Any4 { T v[4]; };
+template <typename T> __device__ __forceinline__ floatx4 load4(const T* p, long long n) {       // n of them exist
+  floatx4 r = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (n >= 4) {
+    const Any4<T> a = *reinterpret_cast<const Any4<T>*>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = widen(a.v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) r[j] = widen(p[j]);
+  }
+  return r;
+}
+template <typename T> __device__ __forceinline__ void store4(T* p, floatx4 v, long long n) {
+  if (n >= 4) {
+    Any4<T> a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a.v[j] = narrow<T>(v[j]);
+    *reinterpret_cast<Any4<T>*>(p) = a;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) p[j] = narrow<T>(v[j]);
+  }
+}
+struct ThinArgs {
+  const void* S;  const void* T;  const void* g;  const void* f;
+  void* outS;  void* outT;            // outT: float sums of every chunk if there are several
+  float* sum;                         // db: of every chunk if there are several (few classes), or of the chunk's rows (few samples)
+  long long rows, K, F;
+  int nt, by_column;                  // by_column: G(r, t) = g[r F + t] (few classes), else g[t F + r] (few samples)
+  int chunk, chunks;                  // rows of a workgroup, at most THIN_ROWS
+  int outS_type, outT_type;
+  float scale;
+};
+constexpr int THIN_ROWS = 256;
+
+template <typename TS, typename TT, typename TY, int NT>
+__global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
+  __shared__ float G[THIN_ROWS][NT];
+  __shared__ floatx4 half[2][NT][64];
+  const long long blocks = (a.K + 255) / 256;
+  const long long L = logical_block(), c = L / blocks, r0 = c * a.chunk;
+  const int n = (int)(a.rows - r0 < a.chunk ? a.rows - r0 : a.chunk);
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const long long k = L % blocks * 256 + lane * 4, left = a.K - k;
+  const TY *g = static_cast<const TY*>(a.g), *f = static_cast<const TY*>(a.f);
+  for (int i = t; i < n * NT; i += 256) {
+    const int r = a.by_column ? i / NT : i % n, e = a.by_column ? i % NT : i / n;
+    float v = 0.0f;
+    if (e < a.nt) {
+      const long long at = a.by_column ? (r0 + r) * a.F + e : e * a.F + r0 + r;
+      v = f ? widen(g[at]) * widen(f[at]) : a.scale * widen(g[at]);
+    }
+    G[r][e] = v;
+  }
+  floatx4 w[NT], s[NT];
+#pragma unroll
+  for (int e = 0; e < NT; ++e) {
+    w[e] = s[e] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (a.outS && e < a.nt) w[e] = load4(static_cast<const TT*>(a.T) + e * a.K + k, left);
+  }
+  __syncthreads();
+  constexpr int U = 4;
+  for (int r = wave; r < n; r += 4 * U) {
+    floatx4 x[U];
+    if (a.outT) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = load4(static_cast<const TS*>(a.S) + (r0 + r + 4 * u) * a.K + k, r + 4 * u < n ? left : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = r + 4 * u < n;
+      const float* q = G[in ? r + 4 * u : 0];          // (x is zero behind the last row)
+      if (a.outS && in) {
+        floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < NT; ++e) o += q[e] * w[e];
+        const long long at = (r0 + r + 4 * u) * a.K + k;
+        if (a.outS_type) store4(static_cast<__bf16*>(a.outS) + at, o, left);
+        else store4(static_cast<float*>(a.outS) + at, o, left);
+      }
+      if (a.outT) {
+#pragma unroll
+        for (int e = 0; e < NT; ++e) s[e] += q[e] * x[u];
+      }
+    }
+  }
+  if (a.sum && L % blocks == 0) {
+    if (a.by_column) {                 // sums of the chunk's columns
+      if (t < a.nt) {
+        float v = 0.0f;
+        for (int r = 0; r < n; ++r) v += G[r][t];
+        a.sum[c * a.F + t] = v;
+      }
+    } else {
+      for (int r = t; r < n; r += 256) {
+        float v = 0.0f;
+        for (int e = 0; e < a.nt; ++e) v += G[r][e];
+        a.sum[r0 + r] = v;
+      }
+    }
+  }
+  if (!a.outT) return;
+  // the four wavefronts' sums, two by two
+#pragma unroll
+  for (int from = 2; from; from >>= 1) {
+    if (wave >= from && wave < 2 * from) {
+#pragma unroll
+      for (int e = 0; e < NT; ++e) half[wave - from][e][lane] = s[e];
+    }
+    __syncthreads();
+    if (wave < from) {
+#pragma unroll
+      for (int e = 0; e < NT; ++e) s[e] += half[wave][e][lane];
+    }
+    __syncthreads();
+  }
+  if (wave) return;
+#pragma unroll
+  for (int e = 0; e < NT; ++e) {
+    const long long at = e * a.K + k;
+    if (e >= a.nt) continue;
+    if (a.chunks > 1) store4(static_cast<float*>(a.outT) + c * a.nt * a.K + at, s[e], left);
+    else if (a.outT_type) store4(static_cast<__bf16*>(a.outT) + at, s[e], left);
+    else store4(static_cast<float*>(a.outT) + at, s[e], left);
+  }
+}
+
 // ------------------------------------------------------------------------------------------ large products
 // Operands as planes of CT in memory, 16-byte pieces: rows along k, padded with zeros to whole slabs (64 bf16 or 32 float), or
 // with k slow, as the backward pass meets its operands, rows of any multiple of 16 bytes.  What the caller has in this form is read
 // in place; anything else -- ragged, with a factor, of another type -- is laid out in the workspace first, which costs a pass
 // over the operand and keeps the multiplying loop free of everything but multiplications.
-typedef __attribute__((address_space(3))) void LdsPtr;
-// 16 bytes per lane from base + each lane's offset + along to LDS address `to` and the 1008 bytes behind it, in lane order; zeros from
-// base + room on.  In assembly so that the compiler does not see a load that writes LDS: it would hold back every transposing read
-// until all loads have arrived (backward pass of 8192 x 4096 x 4096 bf16: 1781 us).  There is no result register, and what is
-// waited for stands in the kernel.
-typedef int int4v __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void to_lds(const char* base, int offset, int along, unsigned room, unsigned to) {
-  const unsigned long long b = reinterpret_cast<unsigned long long>(base);
-  const int4v rsrc = {(int)(unsigned)b, (int)(unsigned)(b >> 32), (int)room, 0x00020000};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(to), "v"(offset), "s"(rsrc), "s"(along) : "memory");
-}
-
 template <typename CT> struct Mma;
 template <> struct Mma<__bf16> {
   typedef bf16x8 Frag;
@@ -807,9 +1216,79 @@ Product from_plane(Product q, const BackwardArgs& b, const GradientPlane& g, cha
   return q;
 }
 
+// ---- thin gradients: at most 16 columns or rows of G
+struct ThinPlan {
+  bool thin, by_column;
+  int chunk, chunks;
+  size_t bytes, sums;                 // of the chunks' sums; where those of db begin
+};
+// Chunks of the long side: about a thousand workgroups with the blocks of 256 k, and no fewer than 32 rows each, 8 per wavefront.
+ThinPlan thin_plan(const BackwardArgs& b) {
+  ThinPlan p = {};
+  const long long nt = b.F < b.M ? b.F : b.M, rows = b.F < b.M ? b.M : b.F, blocks = (b.K + 255) / 256;
+  p.thin = nt <= 16;
+  if (!p.thin) return p;
+  p.by_column = b.F < b.M;
+  long long chunks = blocks >= 1024 ? 1 : 1024 / blocks;
+  if (chunks > (rows + 31) / 32) chunks = (rows + 31) / 32;
+  long long chunk = ((rows + chunks - 1) / chunks + 3) / 4 * 4;
+  if (chunk > THIN_ROWS) chunk = THIN_ROWS;
+  p.chunk = (int)chunk;
+  p.chunks = (int)((rows + chunk - 1) / chunk);
+  if (p.chunks > 1) {
+    p.sums = up((size_t)p.chunks * nt * b.K * sizeof(float));
+    p.bytes = p.sums + (p.by_column ? up((size_t)p.chunks * b.F * sizeof(float)) : 0);
+  }
+  return p;
+}
+template <typename TS, typename TT, typename TY>
+hipError_t launch_thin_sizes(const ThinArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.K + 255) / 256 * a.chunks));
+  if (a.nt <= 4) hipLaunchKernelGGL((thin_backward_kernel<TS, TT, TY, 4>), grid, dim3(256), 0, s, a);
+  else if (a.nt <= 8) hipLaunchKernelGGL((thin_backward_kernel<TS, TT, TY, 8>), grid, dim3(256), 0, s, a);
+  else if (a.nt <= 12) hipLaunchKernelGGL((thin_backward_kernel<TS, TT, TY, 12>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((thin_backward_kernel<TS, TT, TY, 16>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename TS, typename TT>
+hipError_t launch_thin_y(const ThinArgs& a, int ytype, hipStream_t s) {
+  return ytype ? launch_thin_sizes<TS, TT, __bf16>(a, s) : launch_thin_sizes<TS, TT, float>(a, s);
+}
+hipError_t launch_thin(const BackwardArgs& b, const ThinPlan& p, char* ws, hipStream_t s) {
+  ThinArgs a = {};
+  const bool c = p.by_column;
+  a.S = c ? b.X : b.W;  a.T = c ? b.W : b.X;  a.g = b.dY;  a.f = b.D;
+  void* outT = c ? static_cast<void*>(b.dW) : b.dX;
+  a.outS = c ? b.dX : static_cast<void*>(b.dW);
+  a.outT = outT && p.chunks > 1 ? ws : outT;
+  a.sum = b.db && c && p.chunks > 1 ? reinterpret_cast<float*>(ws + p.sums) : b.db;
+  a.rows = c ? b.M : b.F;  a.K = b.K;  a.F = b.F;
+  a.nt = (int)(c ? b.F : b.M);  a.by_column = c;
+  a.chunk = p.chunk;  a.chunks = p.chunks;
+  a.outS_type = c ? b.xtype : 0;  a.outT_type = c ? 0 : b.xtype;
+  a.scale = b.scale;
+  const int ts = c ? b.xtype : b.wtype, tt = c ? b.wtype : b.xtype;
+  hipError_t e = ts ? (tt ? launch_thin_y<__bf16, __bf16>(a, b.ytype, s) : launch_thin_y<__bf16, float>(a, b.ytype, s))
+                    : (tt ? launch_thin_y<float, __bf16>(a, b.ytype, s) : launch_thin_y<float, float>(a, b.ytype, s));
+  if (e != hipSuccess || p.chunks == 1) return e;
+  if (outT) {
+    Product q = {};
+    q.e = Epilogue{0, 0, a.outT_type, 1.0f, nullptr, nullptr, outT, nullptr};
+    q.I = a.nt; q.J = b.K;
+    e = join_parts(q, static_cast<const float*>(a.outT), p.chunks, s);
+  }
+  if (e == hipSuccess && b.db && c) {
+    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(256), 0, s, a.sum, p.chunks, b.F, b.db);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
 }  // namespace
 
 size_t product_workspace(const Product& q) {
+  const FewPlan f = few_plan(q);
+  if (f.few) return f.parts > 1 ? (size_t)f.parts * (size_t)q.I * (size_t)q.J * sizeof(float) : 0;
   const WidePlan w = wide_plan(q);
   if (w.wide) return w.bytes;
   const int parts = parts_of(q);
@@ -817,6 +1296,11 @@ size_t product_workspace(const Product& q) {
 }
 
 hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
+  const FewPlan f = few_plan(q);
+  if (f.few) {
+    const hipError_t e = launch_few(q, f, static_cast<float*>(ws), s);
+    return e != hipSuccess || f.parts == 1 ? e : join_parts(q, static_cast<float*>(ws), f.parts, s);
+  }
   const WidePlan w = wide_plan(q);
   if (w.wide) return launch_wide_product(q, w, ws, s);
   const int parts = parts_of(q);
@@ -831,6 +1315,8 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
 
 // What the calls with these sizes and types need, whichever outputs are wanted (the pointers say only whether one is there)
 size_t backward_workspace(const BackwardArgs& b) {
+  const ThinPlan t = thin_plan(b);
+  if (t.thin) return t.bytes;
   size_t n = 0;
   for (int wanted = 1; wanted < 4; ++wanted) {
     BackwardArgs a = b;
@@ -849,6 +1335,8 @@ size_t backward_workspace(const BackwardArgs& b) {
 
 hipError_t launch_backward(const BackwardArgs& b, void* ws, size_t bytes, hipStream_t s) {
   char* base = static_cast<char*>(ws);
+  const ThinPlan t = thin_plan(b);
+  if (t.thin) return launch_thin(b, t, base, s);
   const Product x = input_product(b), w = weight_product(b);
   const GradientPlane g = gradient_plane(b, x, w);
   const int chunks = chunks_of(b.M);
