@@ -370,7 +370,8 @@ template <typename T, typename CT> __device__ __forceinline__ void from_slab(Row
 template <typename TS, typename TF, int SB, int FB> struct FewShape {
   static constexpr int K = sizeof(TS) == 2 || sizeof(TF) == 2 ? 64 : 32;       // of a slab
   static constexpr int PS = K * (int)sizeof(TS) / 128, PF = K * (int)sizeof(TF) / 128, SLAB = (SB * PS + FB * PF) * 2048;   // panels; bytes
-  static constexpr int ROOM = 152 * 1024, W = 8 * 2 * SLAB <= ROOM ? 8 : 4;     // wavefronts
+  // two blocks of stream rows are taken where there are many workgroups: two of them share a compute unit then, if they fit
+  static constexpr int ROOM = (SB == 2 && 4 * 2 * SLAB <= 76 * 1024 ? 76 : 152) * 1024, W = 8 * 2 * SLAB <= ROOM ? 8 : 4 * 2 * SLAB <= ROOM ? 4 : 2;     // wavefronts
   static constexpr int FIT = ROOM / (W * SLAB), D = FIT > 4 ? 4 : FIT;         // slabs
   static_assert(D >= 2, "two slabs in turn");
 };
@@ -529,6 +530,7 @@ __global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_fe
   }
 }
 
+constexpr long long FEW_MANY = 8192;
 struct FewPlan {
   bool few, swap;
   int sb, fb, parts;
@@ -543,7 +545,7 @@ FewPlan few_plan(const Product& q) {
   if (!p.few) return p;
   p.swap = q.I >= q.J;
   p.fb = few <= 16 ? 1 : few <= 32 ? 2 : 4;
-  p.sb = p.fb == 1 && many >= 16384 ? 2 : 1;
+  p.sb = many >= FEW_MANY ? 2 : 1;
   const long long wgs = (many + 16 * p.sb - 1) / (16 * p.sb);
   long long parts = wgs >= 256 ? 1 : (512 + wgs - 1) / wgs;
   if (parts > q.Kc / 1024) parts = q.Kc / 1024 > 1 ? q.Kc / 1024 : 1;
@@ -572,7 +574,8 @@ hipError_t launch_few_swap(const Product& q, const FewPlan& p, float* partial, h
 }
 template <typename TS, typename TF, typename CT>
 hipError_t launch_few_sizes(const Product& q, const FewPlan& p, float* partial, hipStream_t s) {
-  if (p.sb == 2) return launch_few_swap<TS, TF, CT, 2, 1>(q, p, partial, s);
+  if (p.sb == 2) return p.fb == 1 ? launch_few_swap<TS, TF, CT, 2, 1>(q, p, partial, s)
+                      : p.fb == 2 ? launch_few_swap<TS, TF, CT, 2, 2>(q, p, partial, s) : launch_few_swap<TS, TF, CT, 2, 4>(q, p, partial, s);
   return p.fb == 1 ? launch_few_swap<TS, TF, CT, 1, 1>(q, p, partial, s)
        : p.fb == 2 ? launch_few_swap<TS, TF, CT, 1, 2>(q, p, partial, s) : launch_few_swap<TS, TF, CT, 1, 4>(q, p, partial, s);
 }
