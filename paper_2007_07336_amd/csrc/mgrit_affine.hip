@@ -313,6 +313,22 @@ hipError_t launch_types(const Product& q, float* partial, int parts, hipStream_t
   return launch_tiles<float, float, float, HF, AS, BS>(q, partial, parts, s);
 }
 
+hipError_t join_parts(const Product& q, const float* partial, int parts, hipStream_t s) {
+  const long long n = q.I * q.J, blocks = (n + 255) / 256;
+  hipLaunchKernelGGL(join_parts_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, q.e, partial, parts, n, q.J);
+  return hipGetLastError();
+}
+// (for operands beyond the 32-bit offsets of the tiles below)
+hipError_t launch_any_product(const Product& q, void* ws, hipStream_t s) {
+  const int parts = parts_of(q);
+  float* partial = static_cast<float*>(ws);
+  hipError_t e;
+  if (!q.A.kslow && !q.B.kslow) e = launch_types<false, false, false>(q, partial, parts, s);
+  else if (!q.A.kslow) e = q.A.f ? launch_types<true, false, true>(q, partial, parts, s) : launch_types<false, false, true>(q, partial, parts, s);
+  else e = q.A.f ? launch_types<true, true, true>(q, partial, parts, s) : launch_types<false, true, true>(q, partial, parts, s);
+  return e != hipSuccess || parts == 1 ? e : join_parts(q, partial, parts, s);
+}
+
 // ------------------------------------------------------------------------------------------ few rows on one side
 // At most 64 rows of one operand (the few) against many of the other (the stream), both with k contiguous: a head's classes, or a
 // serving batch on wide weights.  Bound by reading the stream once: a workgroup has SB blocks of 16 stream rows and all of the
@@ -772,6 +788,8 @@ struct Stream {
   int along, offset[NL];
   int at[KS ? T : 4];          // where this lane reads: per tile (k slow) or per step
 
+  // which pieces of row k change places (k slow)
+  static __device__ __forceinline__ int turn(int k) { return ES == 4 ? (k >> 2 & 1) << 3 : BT == 64 ? (k >> 1 & 1) << 2 : (k & 3) << 2; }
   // rows r0.. of `rows`; skip: slabs before the first one; side: which half of the tile this wavefront reads
   __device__ __forceinline__ void init(const Plane& p, long long r0, long long rows, long long Kc, int part, int skip, int wave, int lane, int side) {
     const int c = lane & 31, g = lane >> 5;
@@ -782,7 +800,7 @@ struct Stream {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int byte = (wave * NL + i) * 1024 + lane * 16, k = byte / ROW, piece = byte % ROW / 16;
-        const int from = ES == 2 ? piece ^ ((k & 3) << 2) : piece ^ ((k >> 2 & 1) << 3);
+        const int from = piece ^ turn(k);
         offset[i] = (int)(k * p.ld) + from * 16;
       }
 #pragma unroll
@@ -790,10 +808,10 @@ struct Stream {
         const int first = side * (BT / 2) + i * 32;
         if (ES == 2) {
           const int l16 = lane & 15, k = 8 * g + (l16 >> 2), col = first + 16 * (c >> 4) + 4 * (l16 & 3);
-          at[i] = k * ROW + (((col >> 3) ^ ((k & 3) << 2)) << 4) + (col & 7) * 2;
+          at[i] = k * ROW + (((col >> 3) ^ turn(k)) << 4) + (col & 7) * 2;
         } else {
           const int col = first + c;
-          at[i] = 4 * g * ROW + (((col >> 2) ^ (g << 3)) << 4) + (col & 3) * 4;
+          at[i] = 4 * g * ROW + (((col >> 2) ^ turn(4 * g)) << 4) + (col & 3) * 4;
         }
       }
     } else {
@@ -847,7 +865,7 @@ struct Stream {
 // is multiplied in four steps, the next one is on its way.  Behind the last step's reads a barrier says that nobody needs the old slab
 // any more and that the next one has arrived; the loads of the one after go out at once and have a whole slab's time.
 template <typename CT, int BT, typename OT, bool AS, bool BS>
-__global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(WideArgs a) {
+__global__ __launch_bounds__(256, BT == 256 ? 1 : BT == 128 ? 2 : 4) void product_wide_kernel(WideArgs a) {
   typedef typename Mma<CT>::Frag Frag;
   constexpr int T = BT / 64, NL = BT / 32, SLAB = BT * 128;       // 32 x 32 tiles along a wavefront's side; loads per operand and slab
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -889,28 +907,29 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
     for (int j = 0; j < T; ++j) acc[i][j] = zero16();
 
   // One slab.  In every step the reads of the next one are spread over the first half of the multiplications; the order is fixed
-  // in groups of T / 2 multiplications.  The loads of the slab after the next begin behind the barrier and are spread over SPREAD
+  // in NG groups of MG multiplications.  The loads of the slab after the next begin behind the barrier and are spread over SPREAD
   // steps: the address unit takes 16 cycles for one, and a wavefront that waits for it multiplies nothing.
-  constexpr int SPREAD = 3, PER = (2 * NL + 2 * T * SPREAD - 1) / (2 * T * SPREAD);       // loads in a group
+  constexpr int NG = T == 1 ? 1 : 2 * T, MG = T * T / NG;
+  constexpr int SPREAD = 3, PER = (2 * NL + NG * SPREAD - 1) / (NG * SPREAD);             // loads in a group
   auto multiply = [&](int buf, auto rest, auto more, auto last) {
 #pragma unroll
     for (int step = 0; step < 4; ++step) {
       if (step == 3) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-      for (int n = 0; n < 2 * T; ++n) {
+      for (int n = 0; n < NG; ++n) {
         if (n < T && !(step == 3 && last)) {
           read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n);
           read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n + 1);
         }
-        const int group = (step + 1) % 4 * 2 * T + n;
+        const int group = (step + 1) % 4 * NG + n;
 #pragma unroll
         for (int k = group * PER; k < (group + 1) * PER && k < 2 * NL; ++k) {
           if (step == 3 && more) load(buf, k);
           if (step < 3 && rest) load(buf ^ 1, k);
         }
 #pragma unroll
-        for (int k = 0; k < T / 2; ++k) {
-          const int m = n * (T / 2) + k;
+        for (int k = 0; k < MG; ++k) {
+          const int m = n * MG + k;
           Mma<CT>::go(fa[step & 1][m / T], fb[step & 1][m % T], acc[m / T][m % T]);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -926,7 +945,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   if (t0 + 1 < t1) {
 #pragma unroll
-    for (int i = 0; i < 2 * T * PER && i < 2 * NL; ++i) load(1, i);
+    for (int i = 0; i < NG * PER && i < 2 * NL; ++i) load(1, i);
   }
 #pragma unroll
   for (int n = 0; n < 2 * T; ++n) read(0, 0, n);
@@ -969,13 +988,23 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_wide_kernel(Wi
 // Operand -> planes of CT: rows x (k padded to ldo with zeros), PARTS of them: 1 as it is (or widened); 2: the product of two bf16
 // values, which has 16 significant bits, as the sum of two.  A thread has eight columns of every eighth row of a workgroup's
 // span x 256 entries.  With `sums` the columns' sums over the span as well (of the gradient, for the bias), and PARTS = 0 is
-// those alone.  Bound by memory: 8192 x 4096 bf16 with factors into two planes, 256 MB, with sums: see the table of cases.
+// those alone.  Bound by memory.  All that a call lays out goes in one launch, one job for each array.
+struct LayJob {
+  const void* p;  const void* f;
+  void* out;  float* sums;
+  long long rows, K, ldo;
+  int span, kind;                     // kind: type + 2 * (CT is bf16) + 4 * (there are factors) + 8 * (no planes, sums only)
+  float scale;
+  unsigned first;                     // workgroup
+};
+struct LayJobs { LayJob j[4]; int n; };
 template <typename T, typename CT, int PARTS, bool HF>
-__global__ __launch_bounds__(256) void lay_out_kernel(const T* p, const T* f, long long rows, long long K, CT* out, long long ldo, long long part, int span,
-                                                      float scale, float* sums) {
-  const long long tiles = ((PARTS ? ldo : K) + 255) / 256, chunk = blockIdx.x / tiles;
+__device__ __forceinline__ void lay_out(const LayJob& a, float (&sh)[8][256]) {
+  const T *p = static_cast<const T*>(a.p), *f = static_cast<const T*>(a.f);
+  CT* out = static_cast<CT*>(a.out);
+  const long long K = a.K, ldo = a.ldo, tiles = ((PARTS ? ldo : K) + 255) / 256, L = blockIdx.x - a.first, chunk = L / tiles;
   const int t = threadIdx.x;
-  const long long k = blockIdx.x % tiles * 256 + t % 32 * 8, r0 = chunk * span, r1 = r0 + span < rows ? r0 + span : rows;
+  const long long k = L % tiles * 256 + t % 32 * 8, r0 = chunk * a.span, r1 = r0 + a.span < a.rows ? r0 + a.span : a.rows;
   const long long left = K - k;
   const bool whole = K % 8 == 0 && left >= 8;
   float s[8] = {};
@@ -1004,35 +1033,55 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T* p, const T* f, lo
           float lo[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) split2(v[j], &v[j], &lo[j]);
-          store8(o + part, lo);
+          store8(o + a.rows * ldo, lo);
         }
         store8(o, v);
       }
     }
   }
-  if (!sums) return;
-  __shared__ float sh[8][256];
+  if (!a.sums) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sh[t / 32][t % 32 * 8 + j] = s[j];
   __syncthreads();
-  const long long col = blockIdx.x % tiles * 256 + t;
+  const long long col = L % tiles * 256 + t;
   if (col >= K) return;
-  float a = sh[0][t];
+  float x = sh[0][t];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) a += sh[i][t];
-  sums[chunk * K + col] = scale * a;
+  for (int i = 1; i < 8; ++i) x += sh[i][t];
+  a.sums[chunk * K + col] = a.scale * x;
 }
-// out[col] = sum over the chunks; 64 columns and four sets of chunks per workgroup
-__global__ __launch_bounds__(256) void add_chunks_kernel(const float* part, int chunks, long long F, float* out) {
-  __shared__ float sh[4][64];
+__global__ __launch_bounds__(256) void lay_out_kernel(LayJobs jobs) {
+  __shared__ float sh[8][256];
+  int i = 0;
+  while (i + 1 < jobs.n && blockIdx.x >= jobs.j[i + 1].first) ++i;
+  const LayJob a = jobs.j[i];
+  switch (a.kind) {
+    case 0: lay_out<float, float, 1, false>(a, sh); break;
+    case 1: lay_out<__bf16, float, 1, false>(a, sh); break;
+    case 3: lay_out<__bf16, __bf16, 1, false>(a, sh); break;
+    case 4: lay_out<float, float, 1, true>(a, sh); break;
+    case 5: lay_out<__bf16, float, 1, true>(a, sh); break;
+    case 7: lay_out<__bf16, __bf16, 2, true>(a, sh); break;
+    case 8: lay_out<float, float, 0, false>(a, sh); break;
+    case 9: lay_out<__bf16, float, 0, false>(a, sh); break;
+    case 12: lay_out<float, float, 0, true>(a, sh); break;
+    case 13: lay_out<__bf16, float, 0, true>(a, sh); break;
+  }
+}
+// out[col] = sum over the chunks; 64 columns and sixteen sets of chunks per workgroup
+__global__ __launch_bounds__(1024) void add_chunks_kernel(const float* part, int chunks, long long F, float* out) {
+  __shared__ float sh[16][64];
   const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
   const long long col = blockIdx.x * 64LL + lane;
   float s = 0.0f;
   if (col < F)
-    for (int c = set; c < chunks; c += 4) s += part[c * F + col];
+    for (int c = set; c < chunks; c += 16) s += part[c * F + col];
   sh[set][lane] = s;
   __syncthreads();
-  if (set == 0 && col < F) out[col] = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+  if (set || col >= F) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += sh[i][lane];
+  out[col] = s;
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(float* out, long long n) {
@@ -1041,81 +1090,96 @@ __global__ __launch_bounds__(256) void zero_kernel(float* out, long long n) {
 
 inline size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
-// Rows that a workgroup of lay_out_kernel takes: 64, and more where that makes over 256 chunks
-int span_of(long long rows) {
-  const long long n = (rows + 255) / 256;
-  return (int)(n <= 64 ? 64 : (n + 7) / 8 * 8);
-}
-int chunks_of(long long rows) { const int s = span_of(rows); return (int)((rows + s - 1) / s); }
-
-template <typename T, typename CT, int PARTS, bool HF>
-hipError_t lay_out(const void* p, const void* f, long long rows, long long K, void* out, long long ldo, float scale, float* sums, hipStream_t s) {
-  const long long tiles = ((PARTS ? ldo : K) + 255) / 256;
-  hipLaunchKernelGGL((lay_out_kernel<T, CT, PARTS, HF>), dim3((unsigned)(tiles * chunks_of(rows))), dim3(256), 0, s, static_cast<const T*>(p),
-                     static_cast<const T*>(f), rows, K, static_cast<CT*>(out), ldo, rows * ldo, span_of(rows), scale, sums);
-  return hipGetLastError();
-}
-// rows x K entries of `type`, with factors or without, as CT (bf16: with factors in two parts); out null: sums only
-hipError_t lay_out(const void* p, const void* f, int type, bool bf16, long long rows, long long K, void* out, long long ldo, float scale, float* sums,
-                   hipStream_t s) {
-  if (!out) {
-    if (type) return f ? lay_out<__bf16, __bf16, 0, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<__bf16, __bf16, 0, false>(p, f, rows, K, out, ldo, scale, sums, s);
-    return f ? lay_out<float, float, 0, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<float, float, 0, false>(p, f, rows, K, out, ldo, scale, sums, s);
-  }
-  if (bf16) return f ? lay_out<__bf16, __bf16, 2, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<__bf16, __bf16, 1, false>(p, f, rows, K, out, ldo, scale, sums, s);
-  if (type) return f ? lay_out<__bf16, float, 1, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<__bf16, float, 1, false>(p, f, rows, K, out, ldo, scale, sums, s);
-  return f ? lay_out<float, float, 1, true>(p, f, rows, K, out, ldo, scale, sums, s) : lay_out<float, float, 1, false>(p, f, rows, K, out, ldo, scale, sums, s);
+// Rows of a chunk of sums: 8, and more where that makes over 256 chunks
+int sum_span(long long rows) { const long long n = (rows + 255) / 256; return (int)((n + 7) / 8 * 8); }
+int chunks_of(long long rows) { const int s = sum_span(rows); return (int)((rows + s - 1) / s); }
+// ... and of an array that is laid out alone: 8, up to 64 where that still makes two thousand workgroups
+int lay_span(long long rows, long long tiles) {
+  const long long n = rows * tiles / 2048 / 8 * 8;
+  return (int)(n < 8 ? 8 : n > 64 ? 64 : n);
 }
 
-// ---- which tiles, and what has to be laid out
+// ---- which operands have to be laid out
 inline int slab_of(bool bf16) { return bf16 ? 64 : 32; }
-inline bool wide_sizes(long long I, long long J, long long Kc) {
-  const long long t128 = (I + 127) / 128 * ((J + 127) / 128);
-  return I >= 128 && J >= 128 && Kc >= 64 && t128 >= 16 && Kc <= (1LL << 20) && I <= (1LL << 22) && J <= (1LL << 22);
-}
-struct WidePlan {
-  bool wide, bf16;
-  int bt, slabs, passes, parts;       // parts: workgroups that share a tile's contraction
-  bool copyA, copyB;
-  long long ldA, ldB;                 // entries from row to row of a laid out plane
-  size_t offB, offP, bytes;
-};
 inline bool in_place(const Operand& o, bool bf16, long long Kc) {
   if (o.f || (o.type != 0) != bf16) return false;
   if (o.kslow) return o.ld % (bf16 ? 8 : 4) == 0;
   return o.ld % slab_of(bf16) == 0 && (o.ld == Kc || o.padded);
 }
-// (row length of the copy: whole slabs along k; with k slow, whole 16-byte pieces, of which 8 entries are some)
-inline long long plane_ld(const Operand& o, bool bf16, long long rows, long long Kc) {
-  const long long m = o.kslow ? 8 : slab_of(bf16);
-  return ((o.kslow ? rows : Kc) + m - 1) / m * m;
+// The launch that lays out, as it comes together, and what it takes of the workspace
+struct Layout {
+  LayJobs jobs;
+  char* base;
+  size_t bytes;
+  long long blocks;
+
+  char* take(size_t n) { char* p = base + bytes; bytes += up(n); return p; }
+  void add(const void* p, const void* f, int type, bool bf16, long long rows, long long K, void* out, long long ldo, int span, float scale, float* sums) {
+    LayJob& j = jobs.j[jobs.n++];
+    j = LayJob{p, f, out, sums, rows, K, ldo, span, type + 2 * (out && bf16) + (f ? 4 : 0) + (out ? 0 : 8), scale, (unsigned)blocks};
+    blocks += ((out ? ldo : K) + 255) / 256 * ((rows + span - 1) / span);
+  }
+  // the operand itself, or its plane in the workspace
+  Operand plane(const Operand& o, bool bf16, long long rows, long long Kc) {
+    if (in_place(o, bf16, Kc)) return o;
+    // (row length: whole slabs along k; with k slow whole 16-byte pieces, of which 8 entries are some)
+    const long long m = o.kslow ? 8 : slab_of(bf16), r = o.kslow ? Kc : rows, k = o.kslow ? rows : Kc, ld = (k + m - 1) / m * m;
+    Operand n = {};
+    n.parts = bf16 && o.f ? 2 : 1;
+    n.p = take((size_t)n.parts * r * ld * (bf16 ? 2 : 4));
+    n.ld = ld; n.type = bf16; n.kslow = o.kslow; n.padded = 1; n.part = r * ld;
+    add(o.p, o.f, o.type, bf16, r, k, const_cast<void*>(n.p), ld, lay_span(r, (ld + 255) / 256), 1.0f, nullptr);
+    return n;
+  }
+  hipError_t launch(hipStream_t s) const {
+    if (jobs.n) hipLaunchKernelGGL(lay_out_kernel, dim3((unsigned)blocks), dim3(256), 0, s, jobs);
+    return hipGetLastError();
+  }
+};
+
+// ---- which tiles
+// (32-bit offsets within a tile's rows, or within a slab's where k is slow)
+inline bool wide_sizes(const Product& q) {
+  const long long most = 1LL << 20;
+  return (q.A.kslow ? q.I <= 4 * most : q.Kc <= most) && (q.B.kslow ? q.J <= 4 * most : q.Kc <= most) && q.Kc <= (1LL << 30) &&
+         (q.I + 63) / 64 * ((q.J + 63) / 64) < (1LL << 30);
 }
+struct WidePlan {
+  bool bf16;
+  int bt, slabs, passes, parts;       // parts: workgroups that share a tile's contraction
+  size_t bytes;                       // of their sums
+};
+// The tile and the number of parts whose time is estimated lowest: tiles run one to a compute unit at a time or share it without
+// getting faster; us for a slab by what the loop reaches (256: 1380 TFLOP/s bf16, 150 float), the start and end of a tile, and the
+// launch and the traffic that join the parts.
 WidePlan wide_plan(const Product& q) {
   WidePlan w = {};
-  w.wide = wide_sizes(q.I, q.J, q.Kc);
-  if (!w.wide) return w;
   w.bf16 = q.A.type && q.B.type;
-  const long long t128 = (q.I + 127) / 128 * ((q.J + 127) / 128), t256 = (q.I + 255) / 256 * ((q.J + 255) / 256);
-  w.bt = t256 >= 192 ? 256 : 128;
   w.passes = q.A.parts > 1 ? q.A.parts : w.bf16 && q.A.f ? 2 : 1;
   w.slabs = (int)((q.Kc + slab_of(w.bf16) - 1) / slab_of(w.bf16));
-  const long long tiles = w.bt == 256 ? t256 : t128;
   const int total = w.slabs * w.passes;
-  long long parts = tiles >= 256 ? 1 : 512 / tiles;
-  if (parts > total / 8) parts = total / 8 > 0 ? total / 8 : 1;
-  w.parts = (int)parts;
-  w.copyA = !in_place(q.A, w.bf16, q.Kc);
-  w.copyB = !in_place(q.B, w.bf16, q.Kc);
-  w.ldA = plane_ld(q.A, w.bf16, q.I, q.Kc);
-  w.ldB = plane_ld(q.B, w.bf16, q.J, q.Kc);
-  const size_t es = w.bf16 ? 2 : 4;
-  w.offB = w.copyA ? up((size_t)w.passes * (q.A.kslow ? q.Kc : q.I) * w.ldA * es) : 0;
-  w.offP = w.offB + (w.copyB ? up((size_t)(q.B.kslow ? q.Kc : q.J) * w.ldB * es) : 0);
-  w.bytes = w.offP + (w.parts > 1 ? (size_t)w.parts * q.I * q.J * sizeof(float) : 0);
+  double best = 0.0;
+  for (int bt = 256; bt >= 64; bt /= 2) {
+    const long long tiles = (q.I + bt - 1) / bt * ((q.J + bt - 1) / bt);
+    const double slab = w.bf16 ? (bt == 256 ? 1.6 : bt == 128 ? 0.55 : 0.2) : (bt == 256 ? 7.2 : bt == 128 ? 1.9 : 0.55), ends = bt == 256 ? 6.0 : bt == 128 ? 3.0 : 2.0;
+    for (int parts = 1; parts <= 32 && (parts == 1 || (2 * parts <= total && tiles * parts <= 2048)); ++parts) {
+      const int per = (total + parts - 1) / parts;
+      if (parts > 1 && (total + per - 1) / per != parts) continue;
+      const long long rounds = (tiles * parts + 255) / 256;
+      const double join = parts > 1 ? 4.0 + (double)q.I * q.J * 4.0 * (2 * parts) / 4.0e6 : 0.0;
+      const double us = (double)rounds * (per * slab + (bt == 256 ? ends : 0.0)) + (bt == 256 ? 0.0 : ends) + join;
+      if (best == 0.0 || us < best) { best = us; w.bt = bt; w.parts = parts; }
+    }
+  }
+  w.bytes = w.parts > 1 ? (size_t)w.parts * q.I * q.J * sizeof(float) : 0;
   return w;
 }
-hipError_t lay_out_operand(const Operand& o, bool bf16, long long rows, long long Kc, void* out, long long ldo, hipStream_t s) {
-  return o.kslow ? lay_out(o.p, o.f, o.type, bf16, Kc, rows, out, ldo, 1.0f, nullptr, s) : lay_out(o.p, o.f, o.type, bf16, rows, Kc, out, ldo, 1.0f, nullptr, s);
+
+// Room for the sums of the parts of a product whose operands are where they will be read
+size_t parts_workspace(const Product& q) {
+  if (wide_sizes(q)) return wide_plan(q).bytes;
+  const int parts = parts_of(q);
+  return parts > 1 ? (size_t)parts * (size_t)q.I * (size_t)q.J * sizeof(float) : 0;
 }
 
 template <typename CT, int BT, typename OT, bool AS, bool BS>
@@ -1135,33 +1199,26 @@ hipError_t launch_wide_out(const WideArgs& a, bool as, bool bs, int parts, hipSt
   return a.e.otype ? launch_wide_tiles<CT, BT, __bf16, false, false>(a, parts, s) : launch_wide_tiles<CT, BT, float, false, false>(a, parts, s);
 }
 
-hipError_t join_parts(const Product& q, const float* partial, int parts, hipStream_t s) {
-  const long long n = q.I * q.J, blocks = (n + 255) / 256;
-  hipLaunchKernelGGL(join_parts_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, q.e, partial, parts, n, q.J);
-  return hipGetLastError();
-}
-
-hipError_t launch_wide_product(const Product& q, const WidePlan& w, void* ws, hipStream_t s) {
-  char* base = static_cast<char*>(ws);
+// The product of operands that are in place or laid out
+hipError_t launch_wide_product(const Product& q, void* partial, hipStream_t s) {
+  const WidePlan w = wide_plan(q);
   const long long es = w.bf16 ? 2 : 4;
-  hipError_t e = hipSuccess;
-  if (w.copyA) e = lay_out_operand(q.A, w.bf16, q.I, q.Kc, base, w.ldA, s);
-  if (e == hipSuccess && w.copyB) e = lay_out_operand(q.B, w.bf16, q.J, q.Kc, base + w.offB, w.ldB, s);
-  if (e != hipSuccess) return e;
   WideArgs a = {};
-  a.A = w.copyA ? Plane{base, w.ldA * es, (q.A.kslow ? q.Kc : q.I) * w.ldA * es} : Plane{static_cast<const char*>(q.A.p), q.A.ld * es, q.A.part * es};
-  a.B = w.copyB ? Plane{base + w.offB, w.ldB * es, 0} : Plane{static_cast<const char*>(q.B.p), q.B.ld * es, 0};
+  a.A = Plane{static_cast<const char*>(q.A.p), q.A.ld * es, q.A.part * es};
+  a.B = Plane{static_cast<const char*>(q.B.p), q.B.ld * es, 0};
   a.e = q.e;
   a.I = q.I; a.J = q.J; a.Kc = q.Kc;
   a.slabs = w.slabs;
   a.passes = w.passes;
   a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;
-  const int parts = (w.slabs * w.passes + a.per - 1) / a.per;          // none of them empty
-  a.partial = parts > 1 ? reinterpret_cast<float*>(base + w.offP) : nullptr;
-  if (w.bf16) e = w.bt == 256 ? launch_wide_out<__bf16, 256>(a, q.A.kslow, q.B.kslow, parts, s) : launch_wide_out<__bf16, 128>(a, q.A.kslow, q.B.kslow, parts, s);
-  else e = w.bt == 256 ? launch_wide_out<float, 256>(a, q.A.kslow, q.B.kslow, parts, s) : launch_wide_out<float, 128>(a, q.A.kslow, q.B.kslow, parts, s);
-  if (e != hipSuccess || parts == 1) return e;
-  return join_parts(q, a.partial, parts, s);
+  a.partial = w.parts > 1 ? static_cast<float*>(partial) : nullptr;
+  hipError_t e;
+  const bool as = q.A.kslow, bs = q.B.kslow;
+  if (w.bf16) e = w.bt == 256 ? launch_wide_out<__bf16, 256>(a, as, bs, w.parts, s) : w.bt == 128 ? launch_wide_out<__bf16, 128>(a, as, bs, w.parts, s)
+                                                                                  : launch_wide_out<__bf16, 64>(a, as, bs, w.parts, s);
+  else e = w.bt == 256 ? launch_wide_out<float, 256>(a, as, bs, w.parts, s) : w.bt == 128 ? launch_wide_out<float, 128>(a, as, bs, w.parts, s)
+                                                                           : launch_wide_out<float, 64>(a, as, bs, w.parts, s);
+  return e != hipSuccess || w.parts == 1 ? e : join_parts(q, a.partial, w.parts, s);
 }
 
 // ---- the backward pass: G = dY * D is laid out once for both products where a large tile reads it and it is not there already
@@ -1181,42 +1238,48 @@ Product weight_product(const BackwardArgs& b) {
   q.I = b.F; q.J = b.K; q.Kc = b.M;
   return q;
 }
-// A gradient plane: rows along F, padded to whole slabs
-struct GradientPlane {
-  bool use[2];                        // [bf16]
-  long long ld[2];
-  size_t off[2], bytes;
+struct BackwardPlan {
+  Product x, w;                       // with their operands where the launches find them
+  Layout lay;
+  float* sums;                        // of chunks of rows, for db
+  int chunks;
+  char* partial;
+  size_t bytes;
 };
-bool reads_plane(const Product& q, bool bf16) {
-  const WidePlan w = wide_plan(q);
-  return w.wide && w.bf16 == bf16 && w.copyA;
-}
-GradientPlane gradient_plane(const BackwardArgs& b, const Product& x, const Product& w) {
-  GradientPlane g = {};
+// base: the workspace, or null for the size alone
+BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
+  BackwardPlan p = {};
+  p.lay.base = base;
+  p.x = input_product(b);
+  p.w = weight_product(b);
+  p.chunks = chunks_of(b.M);
+  p.sums = p.chunks > 1 ? reinterpret_cast<float*>(p.lay.take((size_t)p.chunks * b.F * sizeof(float))) : b.db;
+  const bool x = b.dX && wide_sizes(p.x), w = b.dW && wide_sizes(p.w);
+  bool summed = !b.db;
+  Operand G[2] = {};                  // [bf16]
   for (int bf16 = 0; bf16 < 2; ++bf16) {
-    g.use[bf16] = (b.dX && reads_plane(x, bf16)) || (b.dW && reads_plane(w, bf16));
-    if (!g.use[bf16]) continue;
+    const bool for_x = x && (p.x.A.type && p.x.B.type) == bf16 && !in_place(p.x.A, bf16, p.x.Kc);
+    const bool for_w = w && (p.w.A.type && p.w.B.type) == bf16 && !in_place(p.w.A, bf16, p.w.Kc);
+    if (!for_x && !for_w) continue;
+    Operand& g = G[bf16];
     const int m = slab_of(bf16);
-    g.ld[bf16] = (b.F + m - 1) / m * m;
-    g.off[bf16] = g.bytes;
-    g.bytes += up((size_t)b.M * g.ld[bf16] * (bf16 ? (b.D ? 4 : 2) : 4));
+    g.ld = (b.F + m - 1) / m * m;
+    g.type = bf16; g.padded = 1; g.parts = bf16 && b.D ? 2 : 1; g.part = b.M * g.ld;
+    g.p = p.lay.take((size_t)g.parts * g.part * (bf16 ? 2 : 4));
+    p.lay.add(b.dY, b.D, b.ytype, bf16, b.M, b.F, const_cast<void*>(g.p), g.ld, summed ? lay_span(b.M, (g.ld + 255) / 256) : sum_span(b.M), b.scale,
+              summed ? nullptr : p.sums);
+    summed = true;
+    if (for_x) p.x.A = g;
+    if (for_w) { p.w.A = g; p.w.A.kslow = 1; }
   }
-  return g;
-}
-// The product with its gradient operand from the plane
-Product from_plane(Product q, const BackwardArgs& b, const GradientPlane& g, char* ws) {
-  const WidePlan w = wide_plan(q);
-  if (!w.wide || !w.copyA) return q;
-  Operand o = {};
-  o.p = ws + g.off[w.bf16];
-  o.ld = g.ld[w.bf16];
-  o.type = w.bf16;
-  o.kslow = q.A.kslow;
-  o.padded = 1;
-  o.parts = w.bf16 && b.D ? 2 : 1;
-  o.part = b.M * g.ld[w.bf16];
-  q.A = o;
-  return q;
+  if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums);
+  if (x) p.x.B = p.lay.plane(p.x.B, p.x.A.type && p.x.B.type, p.x.J, p.x.Kc);
+  if (w) p.w.B = p.lay.plane(p.w.B, p.w.A.type && p.w.B.type, p.w.J, p.w.Kc);
+  p.partial = base + p.lay.bytes;
+  size_t n = b.dX ? parts_workspace(p.x) : 0;
+  if (b.dW) { const size_t k = parts_workspace(p.w); n = n > k ? n : k; }
+  p.bytes = p.lay.bytes + up(n);
+  return p;
 }
 
 // ---- thin gradients: at most 16 columns or rows of G
@@ -1281,7 +1344,7 @@ hipError_t launch_thin(const BackwardArgs& b, const ThinPlan& p, char* ws, hipSt
     e = join_parts(q, static_cast<const float*>(a.outT), p.chunks, s);
   }
   if (e == hipSuccess && b.db && c) {
-    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(256), 0, s, a.sum, p.chunks, b.F, b.db);
+    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(1024), 0, s, a.sum, p.chunks, b.F, b.db);
     e = hipGetLastError();
   }
   return e;
@@ -1292,10 +1355,13 @@ hipError_t launch_thin(const BackwardArgs& b, const ThinPlan& p, char* ws, hipSt
 size_t product_workspace(const Product& q) {
   const FewPlan f = few_plan(q);
   if (f.few) return f.parts > 1 ? (size_t)f.parts * (size_t)q.I * (size_t)q.J * sizeof(float) : 0;
-  const WidePlan w = wide_plan(q);
-  if (w.wide) return w.bytes;
-  const int parts = parts_of(q);
-  return parts > 1 ? (size_t)parts * (size_t)q.I * (size_t)q.J * sizeof(float) : 0;
+  if (!wide_sizes(q)) return parts_workspace(q);
+  Layout l = {};
+  Product p = q;
+  const bool bf16 = q.A.type && q.B.type;
+  p.A = l.plane(q.A, bf16, q.I, q.Kc);
+  p.B = l.plane(q.B, bf16, q.J, q.Kc);
+  return l.bytes + parts_workspace(p);
 }
 
 hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
@@ -1304,16 +1370,15 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
     const hipError_t e = launch_few(q, f, static_cast<float*>(ws), s);
     return e != hipSuccess || f.parts == 1 ? e : join_parts(q, static_cast<float*>(ws), f.parts, s);
   }
-  const WidePlan w = wide_plan(q);
-  if (w.wide) return launch_wide_product(q, w, ws, s);
-  const int parts = parts_of(q);
-  float* partial = static_cast<float*>(ws);
-  hipError_t e;
-  if (!q.A.kslow && !q.B.kslow) e = launch_types<false, false, false>(q, partial, parts, s);
-  else if (!q.A.kslow) e = q.A.f ? launch_types<true, false, true>(q, partial, parts, s) : launch_types<false, false, true>(q, partial, parts, s);
-  else e = q.A.f ? launch_types<true, true, true>(q, partial, parts, s) : launch_types<false, true, true>(q, partial, parts, s);
-  if (e != hipSuccess || parts == 1) return e;
-  return join_parts(q, partial, parts, s);
+  if (!wide_sizes(q)) return launch_any_product(q, ws, s);
+  Layout l = {};
+  l.base = static_cast<char*>(ws);
+  Product p = q;
+  const bool bf16 = q.A.type && q.B.type;
+  p.A = l.plane(q.A, bf16, q.I, q.Kc);
+  p.B = l.plane(q.B, bf16, q.J, q.Kc);
+  const hipError_t e = l.launch(s);
+  return e != hipSuccess ? e : launch_wide_product(p, l.base + l.bytes, s);
 }
 
 // What the calls with these sizes and types need, whichever outputs are wanted (the pointers say only whether one is there)
@@ -1321,44 +1386,28 @@ size_t backward_workspace(const BackwardArgs& b) {
   const ThinPlan t = thin_plan(b);
   if (t.thin) return t.bytes;
   size_t n = 0;
-  for (int wanted = 1; wanted < 4; ++wanted) {
+  for (int wanted = 0; wanted < 8; ++wanted) {
     BackwardArgs a = b;
     if (!(wanted & 1)) a.dX = nullptr;
     if (!(wanted & 2)) a.dW = nullptr;
-    const Product x = input_product(a), w = weight_product(a);
-    const GradientPlane g = gradient_plane(a, x, w);
-    size_t m = 0;
-    if (a.dX) m = product_workspace(from_plane(x, a, g, nullptr));
-    if (a.dW) { const size_t k = product_workspace(from_plane(w, a, g, nullptr)); m = m > k ? m : k; }
-    m += g.bytes;
+    if (!(wanted & 4)) a.db = nullptr;
+    const size_t m = backward_plan(a, nullptr).bytes;
     n = n > m ? n : m;
   }
-  return up(n) + up((size_t)chunks_of(b.M) * (size_t)b.F * sizeof(float));
+  return n;
 }
 
-hipError_t launch_backward(const BackwardArgs& b, void* ws, size_t bytes, hipStream_t s) {
-  char* base = static_cast<char*>(ws);
+hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s) {
   const ThinPlan t = thin_plan(b);
-  if (t.thin) return launch_thin(b, t, base, s);
-  const Product x = input_product(b), w = weight_product(b);
-  const GradientPlane g = gradient_plane(b, x, w);
-  const int chunks = chunks_of(b.M);
-  const size_t sums = up((size_t)chunks * (size_t)b.F * sizeof(float));
-  float* part = chunks > 1 ? reinterpret_cast<float*>(base + bytes / 256 * 256 - sums) : b.db;
-  bool summed = !b.db;
-  hipError_t e = hipSuccess;
-  for (int bf16 = 0; bf16 < 2 && e == hipSuccess; ++bf16)
-    if (g.use[bf16]) {
-      e = lay_out(b.dY, b.D, b.ytype, bf16, b.M, b.F, base + g.off[bf16], g.ld[bf16], b.scale, summed ? nullptr : part, s);
-      summed = true;
-    }
-  if (e == hipSuccess && !summed) e = lay_out(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, b.scale, part, s);
-  if (e == hipSuccess && b.db && chunks > 1) {
-    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(256), 0, s, part, chunks, b.F, b.db);
+  if (t.thin) return launch_thin(b, t, static_cast<char*>(ws), s);
+  const BackwardPlan p = backward_plan(b, static_cast<char*>(ws));
+  hipError_t e = p.lay.launch(s);
+  if (e == hipSuccess && b.db && p.chunks > 1) {
+    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(1024), 0, s, p.sums, p.chunks, b.F, b.db);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && b.dX) e = launch_product(from_plane(x, b, g, base), base + g.bytes, s);
-  if (e == hipSuccess && b.dW) e = launch_product(from_plane(w, b, g, base), base + g.bytes, s);
+  if (e == hipSuccess && b.dX) e = wide_sizes(p.x) ? launch_wide_product(p.x, p.partial, s) : launch_any_product(p.x, p.partial, s);
+  if (e == hipSuccess && b.dW) e = wide_sizes(p.w) ? launch_wide_product(p.w, p.partial, s) : launch_any_product(p.w, p.partial, s);
   return e;
 }
 

@@ -44,7 +44,7 @@ struct BackwardArgs {
   void* dX;  float* dW;  float* db;
 };
 size_t     backward_workspace(const BackwardArgs& b);
-hipError_t launch_backward(const BackwardArgs& b, void* ws, size_t bytes, hipStream_t s);   // bytes: backward_workspace or more
+hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s);
 hipError_t launch_zero(float* out, long long n, hipStream_t s);
 
 struct LossArgs {

@@ -125,7 +125,7 @@ int32_t mgrit_affine_backward(const mgrit_affine_t* p, const void* X, const void
   for (const void* q : {X, W, D, dY, static_cast<const void*>(dX), static_cast<const void*>(workspace)})
     if (!aligned_to(q, 16)) return MGRIT_ERR_POINTER;
   if (workspace_bytes < need) return MGRIT_ERR_WORKSPACE;
-  if (dX || dW || db) e = launch_backward(backward_args(p, X, W, D, dY, dX, dW, db), workspace, need, s);
+  if (dX || dW || db) e = launch_backward(backward_args(p, X, W, D, dY, dX, dW, db), workspace, s);
   return e == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
 }
 
