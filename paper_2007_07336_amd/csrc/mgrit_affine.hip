@@ -275,12 +275,32 @@ __global__ __launch_bounds__(256) void product_tile_kernel(Product q, long long 
   }
 }
 
-__global__ __launch_bounds__(256) void join_parts_kernel(Epilogue e, const float* partial, int parts, long long n, long long J) {
-  for (long long at = blockIdx.x * 256LL + threadIdx.x; at < n; at += gridDim.x * 256LL) {
-    float s = partial[at];
-    for (int k = 1; k < parts; ++k) s += partial[k * n + at];
-    if (e.otype) finish<__bf16>(e, at, at % J, s);
-    else finish<float>(e, at, at % J, s);
+// The sums of the parts, and the epilogue.  SETS = 16: 64 entries per workgroup and sixteen sets of parts, where there are many
+// (204 parts of 2176 entries: 82 us with one thread for an entry, which waits for one load after the other).
+template <int SETS>
+__global__ __launch_bounds__(SETS == 1 ? 256 : 64 * SETS) void join_parts_kernel(Epilogue e, const float* partial, int parts, long long n, long long J) {
+  __shared__ float sh[SETS][64];
+  constexpr int PER = SETS == 1 ? 256 : 64;
+  const int set = SETS == 1 ? 0 : threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (long long at0 = blockIdx.x * (long long)PER; at0 < n; at0 += gridDim.x * (long long)PER) {
+    const long long at = at0 + (SETS == 1 ? (int)threadIdx.x : lane);
+    float s = 0.0f;
+    if (at < n) {
+#pragma unroll 4
+      for (int k = set; k < parts; k += SETS) s += partial[k * n + at];
+    }
+    if (SETS > 1) {
+      sh[set][lane] = s;
+      __syncthreads();
+      if (set == 0)
+#pragma unroll
+        for (int i = 1; i < SETS; ++i) s += sh[i][lane];
+      __syncthreads();
+    }
+    if (set == 0 && at < n) {
+      if (e.otype) finish<__bf16>(e, at, at % J, s);
+      else finish<float>(e, at, at % J, s);
+    }
   }
 }
 
@@ -314,8 +334,10 @@ hipError_t launch_types(const Product& q, float* partial, int parts, hipStream_t
 }
 
 hipError_t join_parts(const Product& q, const float* partial, int parts, hipStream_t s) {
-  const long long n = q.I * q.J, blocks = (n + 255) / 256;
-  hipLaunchKernelGGL(join_parts_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, q.e, partial, parts, n, q.J);
+  const long long n = q.I * q.J, per = parts >= 16 ? 64 : 256, blocks = (n + per - 1) / per;
+  const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096));
+  if (parts >= 16) hipLaunchKernelGGL(join_parts_kernel<16>, grid, dim3(1024), 0, s, q.e, partial, parts, n, q.J);
+  else hipLaunchKernelGGL(join_parts_kernel<1>, grid, dim3(256), 0, s, q.e, partial, parts, n, q.J);
   return hipGetLastError();
 }
 // (for operands beyond the 32-bit offsets of the tiles below)
@@ -674,13 +696,14 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
     if (a.outS && e < a.nt) w[e] = load4(static_cast<const TT*>(a.T) + e * a.K + k, left);
   }
   __syncthreads();
+  // U rows are on their way while U others are multiplied
   constexpr int U = 4;
-  for (int r = wave; r < n; r += 4 * U) {
-    floatx4 x[U];
-    if (a.outT) {
+  floatx4 x[2][U];
+  auto load = [&](int set, int r) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = load4(static_cast<const TS*>(a.S) + (r0 + r + 4 * u) * a.K + k, r + 4 * u < n ? left : 0);
-    }
+    for (int u = 0; u < U; ++u) x[set][u] = load4(static_cast<const TS*>(a.S) + (r0 + r + 4 * u) * a.K + k, r + 4 * u < n ? left : 0);
+  };
+  auto multiply = [&](int set, int r) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool in = r + 4 * u < n;
@@ -695,9 +718,17 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
       }
       if (a.outT) {
 #pragma unroll
-        for (int e = 0; e < NT; ++e) s[e] += q[e] * x[u];
+        for (int e = 0; e < NT; ++e) s[e] += q[e] * x[set][u];
       }
     }
+  };
+  if (a.outT && wave < n) load(0, wave);
+  for (int r = wave; r < n; r += 8 * U) {
+    if (a.outT && r + 4 * U < n) load(1, r + 4 * U);
+    multiply(0, r);
+    if (r + 4 * U >= n) break;
+    if (a.outT && r + 8 * U < n) load(0, r + 8 * U);
+    multiply(1, r + 4 * U);
   }
   if (a.sum && L % blocks == 0) {
     if (a.by_column) {                 // sums of the chunk's columns
