@@ -62,26 +62,27 @@ __device__ __forceinline__ void finish(const Epilogue& e, long long at, long lon
   if (e.D) static_cast<OT*>(e.D)[at] = narrow<OT>(e.scale * o.d);
 }
 
-// Eight results of one row.  whole: all eight exist and lie on a multiple of eight
-template <typename T> struct Eight { T v[8]; };
+// Eight entries of a row, at whatever address: 16-byte accesses of global memory need no alignment.  whole: all eight exist.
+typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(p);
-  *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(p + 4);
+  *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4u*>(p);
+  *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4u*>(p + 4);
 }
 __device__ __forceinline__ void load8(const __bf16* p, float (&v)[8]) {
-  const bf16x8 b = *reinterpret_cast<const bf16x8*>(p);
+  const bf16x8 b = *reinterpret_cast<const bf16x8u*>(p);
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] = widen(b[k]);
 }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  *reinterpret_cast<floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
-  *reinterpret_cast<floatx4*>(p + 4) = floatx4{v[4], v[5], v[6], v[7]};
+  *reinterpret_cast<floatx4u*>(p) = floatx4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<floatx4u*>(p + 4) = floatx4{v[4], v[5], v[6], v[7]};
 }
 __device__ __forceinline__ void store8(__bf16* p, const float (&v)[8]) {
   bf16x8 b;
 #pragma unroll
   for (int k = 0; k < 8; ++k) b[k] = narrow<__bf16>(v[k]);
-  *reinterpret_cast<bf16x8*>(p) = b;
+  *reinterpret_cast<bf16x8u*>(p) = b;
 }
 template <typename OT>
 __device__ __forceinline__ void put8(OT* p, const float (&v)[8], bool whole, long long left) {
@@ -358,8 +359,6 @@ hipError_t launch_any_product(const Product& q, void* ws, hipStream_t s) {
 // before the sums.  Through LDS because the 16 x 16 matrix instructions want 16 rows in 16 consecutive lanes, and loads are only
 // fast if consecutive lanes read one row (64 rows x 4096 x 4096 bf16: 62 cache accesses a load straight into registers, 22 us).
 // Rows that are no multiples of 16 bytes, and what is left of the contraction, go straight into registers all the same.
-typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
-typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T, typename CT> struct Row8;                  // eight k of a row
 template <> struct Row8<__bf16, __bf16> {
   bf16x8 v;
@@ -800,7 +799,7 @@ struct WideArgs {
   long long I, J, Kc;
   int slabs;                   // of one pass over the contraction
   int passes;                  // A's parts, each of which is multiplied with B
-  int per;                     // slabs that one workgroup takes (blockIdx.y: which), all passes counted
+  int per;                     // slabs that one workgroup takes of its tile's, all passes counted
   float* partial;              // several workgroups: their sums
 };
 
@@ -896,18 +895,17 @@ struct Stream {
 // is multiplied in four steps, the next one is on its way.  Behind the last step's reads a barrier says that nobody needs the old slab
 // any more and that the next one has arrived; the loads of the one after go out at once and have a whole slab's time.
 template <typename CT, int BT, typename OT, bool AS, bool BS>
-__global__ __launch_bounds__(256, BT == 256 ? 1 : BT == 128 ? 2 : 4) void product_wide_kernel(WideArgs a) {
+__device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int share, unsigned char* lds) {
   typedef typename Mma<CT>::Frag Frag;
   constexpr int T = BT / 64, NL = BT / 32, SLAB = BT * 128;       // 32 x 32 tiles along a wavefront's side; loads per operand and slab
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave >> 1, wj = wave & 1;
   // tiles in groups of GM rows of tiles, so that the tiles that an XCD works on at a time share few panels of both operands
   constexpr int GM = 4;
   const long long ti = (a.I + BT - 1) / BT, tj = (a.J + BT - 1) / BT;
-  const long long L = logical_block(), group = L / (GM * tj), first = group * GM, size = ti - first < GM ? ti - first : GM, in = L - group * GM * tj;
+  const long long group = L / (GM * tj), first = group * GM, size = ti - first < GM ? ti - first : GM, in = L - group * GM * tj;
   const long long i0 = (first + in % size) * BT, j0 = in / size * BT;
 
-  const int total = a.slabs * a.passes, t0 = (int)blockIdx.y * a.per, t1 = t0 + a.per < total ? t0 + a.per : total;
+  const int total = a.slabs * a.passes, t0 = share * a.per, t1 = t0 + a.per < total ? t0 + a.per : total;
   Stream<CT, BT, AS> sa;
   Stream<CT, BT, BS> sb;
   sa.init(a.A, i0, a.I, a.Kc, t0 / a.slabs, t0 % a.slabs, wave, lane, wi);
@@ -991,7 +989,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : BT == 128 ? 2 : 4) void produc
   const int lc = lane % (W / 8) * 8, lr = lane / (W / 8);
   const long long col = j0 + wj * W + lc;
   const long long n = a.I * a.J;
-  const bool whole = a.J % 8 == 0 && col + 8 <= a.J;
+  const bool whole = col + 8 <= a.J;
   float bias[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) bias[k] = a.e.fwd && a.e.bias && !a.partial && col + k < a.J ? a.e.bias[col + k] : 0.0f;
@@ -1008,12 +1006,27 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : BT == 128 ? 2 : 4) void produc
       *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(strip + r * PITCH + lc);
       *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(strip + r * PITCH + lc + 4);
       if (row < a.I) {
-        if (a.partial) put8(a.partial + blockIdx.y * n + at, v, whole, a.J - col);
+        if (a.partial) put8(a.partial + share * n + at, v, whole, a.J - col);
         else finish8<OT>(a.e, at, v, bias, whole, a.J - col);
       }
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+constexpr int wide_waves(int bt) { return bt == 256 ? 1 : bt == 128 ? 2 : 4; }          // workgroups of a compute unit
+template <typename CT, int BT, typename OT, bool AS, bool BS>
+__global__ __launch_bounds__(256, wide_waves(BT)) void product_wide_kernel(WideArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  product_wide<CT, BT, OT, AS, BS>(a, logical_block(), blockIdx.y, lds);
+}
+// Both products of a backward pass, where one alone leaves compute units idle: dW (w, `first` workgroups) and dX.
+template <typename CT, int BT, typename OT>
+__global__ __launch_bounds__(256, wide_waves(BT)) void product_pair_kernel(WideArgs w, WideArgs x, unsigned first, unsigned tiles_w, unsigned tiles_x) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const unsigned b = blockIdx.x;
+  if (b < first) product_wide<CT, BT, float, true, true>(w, b % tiles_w, b / tiles_w, lds);
+  else product_wide<CT, BT, OT, false, true>(x, (b - first) % tiles_x, (b - first) / tiles_x, lds);
 }
 
 // Operand -> planes of CT: rows x (k padded to ldo with zeros), PARTS of them: 1 as it is (or widened); 2: the product of two bf16
@@ -1037,7 +1050,7 @@ __device__ __forceinline__ void lay_out(const LayJob& a, float (&sh)[8][256]) {
   const int t = threadIdx.x;
   const long long k = L % tiles * 256 + t % 32 * 8, r0 = chunk * a.span, r1 = r0 + a.span < a.rows ? r0 + a.span : a.rows;
   const long long left = K - k;
-  const bool whole = K % 8 == 0 && left >= 8;
+  const bool whole = left >= 8;
   float s[8] = {};
   if (k < (PARTS ? ldo : K)) {
     for (long long r = r0 + t / 32; r < r1; r += 8) {
@@ -1230,9 +1243,7 @@ hipError_t launch_wide_out(const WideArgs& a, bool as, bool bs, int parts, hipSt
   return a.e.otype ? launch_wide_tiles<CT, BT, __bf16, false, false>(a, parts, s) : launch_wide_tiles<CT, BT, float, false, false>(a, parts, s);
 }
 
-// The product of operands that are in place or laid out
-hipError_t launch_wide_product(const Product& q, void* partial, hipStream_t s) {
-  const WidePlan w = wide_plan(q);
+WideArgs wide_args(const Product& q, const WidePlan& w, void* partial) {
   const long long es = w.bf16 ? 2 : 4;
   WideArgs a = {};
   a.A = Plane{static_cast<const char*>(q.A.p), q.A.ld * es, q.A.part * es};
@@ -1243,6 +1254,12 @@ hipError_t launch_wide_product(const Product& q, void* partial, hipStream_t s) {
   a.passes = w.passes;
   a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;
   a.partial = w.parts > 1 ? static_cast<float*>(partial) : nullptr;
+  return a;
+}
+// The product of operands that are in place or laid out
+hipError_t launch_wide_product(const Product& q, void* partial, hipStream_t s) {
+  const WidePlan w = wide_plan(q);
+  const WideArgs a = wide_args(q, w, partial);
   hipError_t e;
   const bool as = q.A.kslow, bs = q.B.kslow;
   if (w.bf16) e = w.bt == 256 ? launch_wide_out<__bf16, 256>(a, as, bs, w.parts, s) : w.bt == 128 ? launch_wide_out<__bf16, 128>(a, as, bs, w.parts, s)
@@ -1250,6 +1267,31 @@ hipError_t launch_wide_product(const Product& q, void* partial, hipStream_t s) {
   else e = w.bt == 256 ? launch_wide_out<float, 256>(a, as, bs, w.parts, s) : w.bt == 128 ? launch_wide_out<float, 128>(a, as, bs, w.parts, s)
                                                                            : launch_wide_out<float, 64>(a, as, bs, w.parts, s);
   return e != hipSuccess || w.parts == 1 ? e : join_parts(q, a.partial, w.parts, s);
+}
+template <typename CT, int BT>
+hipError_t launch_pair_tiles(const WideArgs& w, const WideArgs& x, int parts_w, int parts_x, hipStream_t s) {
+  const size_t smem = 4 * BT * 128;                     // (at most 64 KB: no opt-in)
+  const unsigned tw = (unsigned)((w.I + BT - 1) / BT * ((w.J + BT - 1) / BT)), tx = (unsigned)((x.I + BT - 1) / BT * ((x.J + BT - 1) / BT));
+  const dim3 grid(tw * parts_w + tx * parts_x);
+  if (x.e.otype) hipLaunchKernelGGL((product_pair_kernel<CT, BT, __bf16>), grid, dim3(256), smem, s, w, x, tw * parts_w, tw, tx);
+  else hipLaunchKernelGGL((product_pair_kernel<CT, BT, float>), grid, dim3(256), smem, s, w, x, tw * parts_w, tw, tx);
+  return hipGetLastError();
+}
+// Whether both products of a backward pass go in one launch: same type, same small tiles, and fewer than four workgroups of one
+// of them for a compute unit.
+bool pairs(const Product& w, const Product& x) {
+  const WidePlan a = wide_plan(w), b = wide_plan(x);
+  const long long tw = (w.I + a.bt - 1) / a.bt * ((w.J + a.bt - 1) / a.bt) * a.parts, tx = (x.I + b.bt - 1) / b.bt * ((x.J + b.bt - 1) / b.bt) * b.parts;
+  return a.bf16 == b.bf16 && a.bt == b.bt && a.bt <= 128 && (tw < 1024 || tx < 1024) && tw + tx < (1LL << 30);
+}
+hipError_t launch_wide_pair(const Product& qw, const Product& qx, char* partial_w, char* partial_x, hipStream_t s) {
+  const WidePlan pw = wide_plan(qw), px = wide_plan(qx);
+  const WideArgs w = wide_args(qw, pw, partial_w), x = wide_args(qx, px, partial_x);
+  hipError_t e = pw.bf16 ? (pw.bt == 128 ? launch_pair_tiles<__bf16, 128>(w, x, pw.parts, px.parts, s) : launch_pair_tiles<__bf16, 64>(w, x, pw.parts, px.parts, s))
+                         : (pw.bt == 128 ? launch_pair_tiles<float, 128>(w, x, pw.parts, px.parts, s) : launch_pair_tiles<float, 64>(w, x, pw.parts, px.parts, s));
+  if (e == hipSuccess && pw.parts > 1) e = join_parts(qw, w.partial, pw.parts, s);
+  if (e == hipSuccess && px.parts > 1) e = join_parts(qx, x.partial, px.parts, s);
+  return e;
 }
 
 // ---- the backward pass: G = dY * D is laid out once for both products where a large tile reads it and it is not there already
@@ -1274,7 +1316,8 @@ struct BackwardPlan {
   Layout lay;
   float* sums;                        // of chunks of rows, for db
   int chunks;
-  char* partial;
+  bool pair;                          // dW and dX in one launch
+  char *partial_x, *partial_w;
   size_t bytes;
 };
 // base: the workspace, or null for the size alone
@@ -1306,10 +1349,11 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
   if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums);
   if (x) p.x.B = p.lay.plane(p.x.B, p.x.A.type && p.x.B.type, p.x.J, p.x.Kc);
   if (w) p.w.B = p.lay.plane(p.w.B, p.w.A.type && p.w.B.type, p.w.J, p.w.Kc);
-  p.partial = base + p.lay.bytes;
-  size_t n = b.dX ? parts_workspace(p.x) : 0;
-  if (b.dW) { const size_t k = parts_workspace(p.w); n = n > k ? n : k; }
-  p.bytes = p.lay.bytes + up(n);
+  p.pair = x && w && pairs(p.w, p.x);
+  const size_t nx = b.dX ? up(parts_workspace(p.x)) : 0, nw = b.dW ? up(parts_workspace(p.w)) : 0;
+  p.partial_x = base + p.lay.bytes;
+  p.partial_w = p.partial_x + (p.pair ? nx : 0);
+  p.bytes = p.lay.bytes + (p.pair ? nx + nw : nx > nw ? nx : nw);
   return p;
 }
 
@@ -1437,8 +1481,10 @@ hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s) {
     hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(1024), 0, s, p.sums, p.chunks, b.F, b.db);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && b.dX) e = wide_sizes(p.x) ? launch_wide_product(p.x, p.partial, s) : launch_any_product(p.x, p.partial, s);
-  if (e == hipSuccess && b.dW) e = wide_sizes(p.w) ? launch_wide_product(p.w, p.partial, s) : launch_any_product(p.w, p.partial, s);
+  if (e != hipSuccess) return e;
+  if (p.pair) return launch_wide_pair(p.w, p.x, p.partial_w, p.partial_x, s);
+  if (b.dX) e = wide_sizes(p.x) ? launch_wide_product(p.x, p.partial_x, s) : launch_any_product(p.x, p.partial_x, s);
+  if (e == hipSuccess && b.dW) e = wide_sizes(p.w) ? launch_wide_product(p.w, p.partial_w, s) : launch_any_product(p.w, p.partial_w, s);
   return e;
 }
 
