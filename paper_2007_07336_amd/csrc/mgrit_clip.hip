@@ -15,13 +15,27 @@ struct Entry {
   long long count, chunk0;                      // chunk0: chunks of the tensors before
   long long type;
 };
-constexpr int PER = 96;                         // entries that fit a kernel's arguments (4 KB)
-struct Entries { Entry e[PER]; };
+// The list of tensors goes to the workspace by kernel arguments, which a captured graph keeps, as many at a time as 4 KB of them
+// hold (600 tensors: 4 launches of 2 us).
+struct Given { const void* src; void* dst; long long count; };         // count: twice the entries, and 1 for bf16
+constexpr int PER = 168;
+struct Givens { Given e[PER]; };
+static_assert(sizeof(Givens) + 24 <= 4096, "kernel arguments");
 struct Space { double norm; double partial[GRID]; Entry table[1]; };
 
-// The list of tensors goes to the workspace by kernel arguments, which a captured graph keeps, in as many launches as it takes.
-__global__ __launch_bounds__(PER) void clip_table_kernel(Entries in, Entry* out, int n) {
-  if ((int)threadIdx.x < n) out[threadIdx.x] = in.e[threadIdx.x];
+__global__ __launch_bounds__(256) void clip_table_kernel(Givens in, Entry* out, int n, long long before) {
+  __shared__ long long sum[256];
+  const int t = threadIdx.x;
+  const long long count = t < n ? in.e[t].count >> 1 : 0, mine = (count + CHUNK - 1) / CHUNK;
+  sum[t] = mine;
+  __syncthreads();
+  for (int d = 1; d < 256; d *= 2) {            // running sums
+    const long long v = t >= d ? sum[t - d] : 0;
+    __syncthreads();
+    sum[t] += v;
+    __syncthreads();
+  }
+  if (t < n) out[t] = Entry{in.e[t].src, in.e[t].dst, count, before + sum[t] - mine, in.e[t].count & 1};
 }
 
 __device__ __forceinline__ float value(float v) { return v; }
@@ -128,14 +142,15 @@ hipError_t launch_clip(int n, const ClipTensor* t, float max_norm, float* norm, 
   long long chunks = 0;
   bool any = false;
   for (int i = 0; i < n; i += PER) {
-    Entries in = {};
+    Givens in = {};
     const int k = n - i < PER ? n - i : PER;
+    const long long before = chunks;
     for (int j = 0; j < k; ++j) {
-      in.e[j] = Entry{t[i + j].src, t[i + j].dst, t[i + j].count, chunks, t[i + j].type};
+      in.e[j] = Given{t[i + j].src, t[i + j].dst, 2 * t[i + j].count + (t[i + j].type ? 1 : 0)};
       chunks += (t[i + j].count + CHUNK - 1) / CHUNK;
       any = any || t[i + j].dst;
     }
-    hipLaunchKernelGGL(clip_table_kernel, dim3(1), dim3(PER), 0, s, in, sp->table + i, k);
+    hipLaunchKernelGGL(clip_table_kernel, dim3(1), dim3(256), 0, s, in, sp->table + i, k, before);
   }
   const int grid = chunks < GRID ? (int)chunks : GRID;
   if (grid > 0) hipLaunchKernelGGL(clip_norm_kernel, dim3((unsigned)grid), dim3(TH), 0, s, sp->table, n, chunks, sp->partial);

@@ -32,76 +32,170 @@ template <int N> __device__ __forceinline__ void take(Running& r, const float (&
   r.s = s;
 }
 
-// TH threads per row; a wavefront (TH = 64) needs no barrier, so four rows share a workgroup then.
 template <int TH> __device__ __forceinline__ Running join_threads(Running r, Running* sh) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) r = join(r, Running{__shfl_xor(r.m, d), __shfl_xor(r.s, d)});
-  if (TH > 64) {
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = r;
-    __syncthreads();
-    r = sh[0];
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = r;
+  __syncthreads();
+  r = sh[0];
 #pragma unroll
-    for (int w = 1; w < TH / 64; ++w) r = join(r, sh[w]);
-  }
+  for (int w = 1; w < TH / 64; ++w) r = join(r, sh[w]);
   return r;
 }
+// The vector as it was loaded: without this the compiler keeps its widened values, twice the registers, from one use to the next
+template <typename T> __device__ __forceinline__ void keep_packed(Vec<T>& a) {
+  typedef unsigned u4 __attribute__((ext_vector_type(4)));
+  u4 u = __builtin_bit_cast(u4, a);
+  asm volatile("" : "+v"(u));
+  a = __builtin_bit_cast(Vec<T>, u);
+}
+// What the row's results are made of: f times exp(x - m) is the gradient apart from the label's
+struct Row {
+  float m, s, w, f;
+  __device__ __forceinline__ float gradient(float x, bool label) const {
+    const float p = exp_below(x, m);
+    return label ? (p / s - 1.0f) * w : p * f;
+  }
+};
 
-// rows <- l_r, grad <- gradient.  weight: scale, divided by the number of counted rows if `counted` is given.
-template <typename T, int TH>
-__global__ __launch_bounds__(TH == 64 ? 256 : TH) void loss_rows_kernel(const T* logits, const int64_t* labels, float* rows, T* grad, int B, int V,
-                                                                      float scale, const int* counted) {
+// One row per workgroup of TH threads.  NV > 0: the row's whole 16-byte vectors fit NV registers of each thread, and the row is
+// read once.  NV = 0: it is read twice.  rows <- l_r, grad <- gradient; `counted`: the number of rows that scale is divided by.
+// Bound by memory: 4096 rows of 50021 bf16 (0.8 GB in and out), see the table of cases.
+template <typename T, int TH, int NV>
+__global__ __launch_bounds__(TH) void loss_rows_kernel(const T* logits, const int64_t* labels, float* rows, T* grad, int V, float scale, const int* counted) {
   constexpr int N = Vec<T>::N;
-  __shared__ Running sh[TH > 64 ? TH / 64 : 1];
-  const int t = threadIdx.x % TH;
-  const long long row = TH == 64 ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
-  if (row >= B) return;
+  __shared__ Running sh[TH / 64];
+  const int t = threadIdx.x;
+  const long long row = blockIdx.x;
   const int64_t label = labels[row];
   const T* x = logits + row * V;
   T* g = grad ? grad + row * V : nullptr;
-  // entries before the first whole vector, whole vectors, entries behind
-  const int off = (int)((row * V) % N), head = off ? (N - off < V ? N - off : V) : 0, nv = (V - head) / N, tail = head + nv * N;
   if (label < 0) {
     if (rows && t == 0) rows[row] = 0.0f;
     if (g)
       for (int v = t; v < V; v += TH) g[v] = T(0.0f);
     return;
   }
+  // entries before the first whole vector, whole vectors, entries behind
+  const int off = (int)((row * V) % N), head = off ? (N - off < V ? N - off : V) : 0, nv = (V - head) / N, tail = head + nv * N;
+  const bool good = label < V;
+  const float asked = good ? value(x[label]) : 0.0f;                     // (before the gradient may take the logits' place)
+  const float edge[2] = {t < head ? value(x[t]) : -INFINITY, t < V - tail ? value(x[tail + t]) : -INFINITY};
   Running r = {-INFINITY, 0.0f};
-  for (int v = t; v < nv; v += TH) {
-    const Vec<T> a = *reinterpret_cast<const Vec<T>*>(__builtin_assume_aligned(x + head + v * N, 16));
-    float f[N];
+  Vec<T> a[NV ? NV : 1];
+  if constexpr (NV > 0) {
+    // (loads are not predicated, or each would be waited for: threads behind the last vector read it once more)
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = value(a.v[i]);
-    take(r, f);
-  }
-  {
-    float f[2] = {t < head ? value(x[t]) : -INFINITY, t < V - tail ? value(x[tail + t]) : -INFINITY};
-    take(r, f);
+    for (int i = 0; i < NV; ++i) a[i] = *reinterpret_cast<const Vec<T>*>(__builtin_assume_aligned(x + head + (t + i * TH < nv ? t + i * TH : nv - 1) * N, 16));
+    float m = fmaxf(edge[0], edge[1]), s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) m = fmaxf(m, value(a[i].v[j]));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      keep_packed(a[i]);
+      float q = 0.0f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) { const float v = value(a[i].v[j]); q += v == -INFINITY ? 0.0f : exp_below(v, m); }
+      s += t + i * TH < nv ? q : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) s += edge[j] == -INFINITY ? 0.0f : exp_below(edge[j], m);
+    r = Running{m, s};
+  } else {
+    for (int v = t; v < nv; v += TH) {
+      const Vec<T> b = *reinterpret_cast<const Vec<T>*>(__builtin_assume_aligned(x + head + v * N, 16));
+      float f[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[j] = value(b.v[j]);
+      take(r, f);
+    }
+    take(r, edge);
   }
   r = join_threads<TH>(r, sh);
-  const bool good = label < V;
   if (r.s == 0.0f || !good) r.s = NAN;
-  // (before the gradient is written: it may lie where the logits are)
-  if (rows && t == 0) rows[row] = good ? r.m + __builtin_amdgcn_logf(r.s) * LN2 - value(x[label]) : NAN;
+  if (rows && t == 0) rows[row] = good ? r.m + __builtin_amdgcn_logf(r.s) * LN2 - asked : NAN;
   if (!g) return;
-  if (TH > 64) __syncthreads();
-  const float w = counted ? scale / (float)*counted : scale, f = w / r.s;
-  for (int v = t; v < nv; v += TH) {
-    Vec<T> a = *reinterpret_cast<const Vec<T>*>(__builtin_assume_aligned(x + head + v * N, 16));
+  const float w = counted ? scale / (float)*counted : scale;
+  const Row o = {r.m, r.s, w, w / r.s};
+  auto put = [&](Vec<T> b, int v) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float p = exp_below(value(a.v[i]), r.m);
-      a.v[i] = static_cast<T>(head + v * N + i == label ? (p / r.s - 1.0f) * w : p * f);
+    for (int j = 0; j < N; ++j) b.v[j] = static_cast<T>(o.gradient(value(b.v[j]), head + v * N + j == label));
+    *reinterpret_cast<Vec<T>*>(__builtin_assume_aligned(g + head + v * N, 16)) = b;
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      keep_packed(a[i]);
+      if (t + i * TH < nv) put(a[i], t + i * TH);
     }
-    *reinterpret_cast<Vec<T>*>(__builtin_assume_aligned(g + head + v * N, 16)) = a;
+  } else {
+    for (int v = t; v < nv; v += TH) put(*reinterpret_cast<const Vec<T>*>(__builtin_assume_aligned(x + head + v * N, 16)), v);
   }
-  for (int side = 0; side < 2; ++side) {
-    const int v = side ? tail + t : t;
-    if (side ? v < V : v < head) {
-      const float p = exp_below(value(x[v]), r.m);
-      g[v] = static_cast<T>(v == label ? (p / r.s - 1.0f) * w : p * f);
+  if (t < head) g[t] = static_cast<T>(o.gradient(edge[0], t == label));
+  if (t < V - tail) g[tail + t] = static_cast<T>(o.gradient(edge[1], tail + t == label));
+}
+
+// Short rows, V <= 16 L: L lanes of a wavefront per row, 16 entries each at most.  Alone (one workgroup of 1024 threads, few rows): it
+// counts the rows and adds up the losses as well, so that a small loss is a single launch.
+template <typename T, int L>
+__global__ __launch_bounds__(1024) void loss_short_kernel(const T* logits, const int64_t* labels, float* rows, T* grad, int B, int V, float scale, int mean,
+                                                         const int* counted, int alone, float* loss) {
+  __shared__ double part[16];
+  __shared__ int count[16];
+  const int t = threadIdx.x, l = t % L;
+  float w = scale;
+  if (mean && alone) {
+    int n = 0;
+    for (int r = t; r < B; r += blockDim.x) n += labels[r] >= 0;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
+    if ((t & 63) == 0) count[t >> 6] = n;
+    __syncthreads();
+    n = 0;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) n += count[i];
+    w = scale / (float)(n > 0 ? n : 1);
+  } else if (mean) {
+    w = scale / (float)*counted;
+  }
+  double total = 0.0;
+  for (long long row = blockIdx.x * (long long)(blockDim.x / L) + t / L; row < B; row += (long long)gridDim.x * (blockDim.x / L)) {
+    const int64_t label = labels[row];
+    const T* x = logits + row * V;
+    float v[16];
+    Running r = {-INFINITY, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      v[i] = l + i * L < V ? value(x[l + i * L]) : -INFINITY;
+      r.m = fmaxf(r.m, v[i]);
+    }
+    const bool good = label < V;
+    const float asked = label >= 0 && good ? value(x[label]) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r.s += v[i] == -INFINITY ? 0.0f : exp_below(v[i], r.m);
+#pragma unroll
+    for (int d = L / 2; d; d >>= 1) r = join(r, Running{__shfl_xor(r.m, d), __shfl_xor(r.s, d)});
+    if (r.s == 0.0f || !good) r.s = NAN;
+    const float lr = label < 0 ? 0.0f : good ? r.m + __builtin_amdgcn_logf(r.s) * LN2 - asked : NAN;
+    if (rows && l == 0) rows[row] = lr;
+    total += l == 0 ? (double)lr : 0.0;
+    if (grad) {
+      const Row o = {r.m, r.s, w, w / r.s};
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (l + i * L < V) grad[row * V + l + i * L] = static_cast<T>(label < 0 ? 0.0f : o.gradient(v[i], l + i * L == label));
     }
   }
+  if (!alone || !loss) return;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  if ((t & 63) == 0) part[t >> 6] = total;
+  __syncthreads();
+  if (t) return;
+  total = 0.0;
+  for (int i = 0; i < (int)blockDim.x / 64; ++i) total += part[i];
+  *loss = (float)(total * (double)w);
 }
 
 // Number of rows that count
@@ -135,16 +229,36 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* rows, int B
   }
 }
 
+// Short rows: V <= 1024 (longer ones are worth a workgroup)
+template <typename T>
+hipError_t launch_short(const LossArgs& a, float* rows, const int* counted, bool alone, hipStream_t s) {
+  const T* x = static_cast<const T*>(a.logits);
+  T* g = static_cast<T*>(a.grad);
+  const int lanes = a.V <= 16 ? 1 : a.V <= 64 ? 4 : a.V <= 256 ? 16 : 64, threads = alone ? 1024 : 256;
+  const long long blocks = (a.B + threads / lanes - 1LL) / (threads / lanes);
+  const dim3 grid((unsigned)(alone ? 1 : blocks < 65536 ? blocks : 65536));
+#define SHORT_ROWS(L) hipLaunchKernelGGL((loss_short_kernel<T, L>), grid, dim3(threads), 0, s, x, a.labels, rows, g, a.B, a.V, a.scale, a.mean, counted, alone, a.loss)
+  if (lanes == 1) SHORT_ROWS(1);
+  else if (lanes == 4) SHORT_ROWS(4);
+  else if (lanes == 16) SHORT_ROWS(16);
+  else SHORT_ROWS(64);
+#undef SHORT_ROWS
+  return hipGetLastError();
+}
 template <typename T>
 hipError_t launch_rows(const LossArgs& a, float* rows, const int* counted, hipStream_t s) {
   const T* x = static_cast<const T*>(a.logits);
   T* g = static_cast<T*>(a.grad);
-  if (a.V <= 1024)
-    hipLaunchKernelGGL((loss_rows_kernel<T, 64>), dim3((unsigned)((a.B + 3LL) / 4)), dim3(256), 0, s, x, a.labels, rows, g, a.B, a.V, a.scale, counted);
-  else if (a.V <= 16384)
-    hipLaunchKernelGGL((loss_rows_kernel<T, 256>), dim3((unsigned)a.B), dim3(256), 0, s, x, a.labels, rows, g, a.B, a.V, a.scale, counted);
-  else
-    hipLaunchKernelGGL((loss_rows_kernel<T, 1024>), dim3((unsigned)a.B), dim3(1024), 0, s, x, a.labels, rows, g, a.B, a.V, a.scale, counted);
+  const long long vectors = a.V / Vec<T>::N;
+#define LONG_ROWS(TH, NV) hipLaunchKernelGGL((loss_rows_kernel<T, TH, NV>), dim3((unsigned)a.B), dim3(TH), 0, s, x, a.labels, rows, g, a.V, a.scale, counted)
+  if (vectors <= 256) LONG_ROWS(256, 1);
+  else if (vectors <= 512) LONG_ROWS(256, 2);
+  else if (vectors <= 1024) LONG_ROWS(256, 4);
+  else if (vectors <= 2048) LONG_ROWS(512, 4);
+  else if (vectors <= 4096) LONG_ROWS(1024, 4);
+  else if (vectors <= 8192) LONG_ROWS(1024, 8);
+  else LONG_ROWS(1024, 0);
+#undef LONG_ROWS
   return hipGetLastError();
 }
 
@@ -153,15 +267,19 @@ hipError_t launch_rows(const LossArgs& a, float* rows, const int* counted, hipSt
 size_t loss_workspace(const LossArgs& a) { return 256 + (size_t)a.B * sizeof(float); }
 
 hipError_t launch_loss(const LossArgs& a, void* ws, hipStream_t s) {
+  // one launch for up to 32 entries of each of its threads
+  const bool alone = a.V <= 1024 && (long long)a.B * a.V <= 32768 && a.B <= 4096;
+  if (alone) return a.dtype ? launch_short<__bf16>(a, a.rows, nullptr, true, s) : launch_short<float>(a, a.rows, nullptr, true, s);
   int* counted = a.mean ? static_cast<int*>(ws) : nullptr;
   float* rows = a.rows ? a.rows : a.loss ? reinterpret_cast<float*>(static_cast<char*>(ws) + 256) : nullptr;
   if (counted && (a.loss || a.grad)) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, a.labels, a.B, counted);
-  if (a.B > 0) {
-    const hipError_t e = a.dtype ? launch_rows<__bf16>(a, rows, counted, s) : launch_rows<float>(a, rows, counted, s);
-    if (e != hipSuccess) return e;
+  hipError_t e = hipSuccess;
+  if (rows || a.grad) {
+    if (a.V <= 1024) e = a.dtype ? launch_short<__bf16>(a, rows, counted, false, s) : launch_short<float>(a, rows, counted, false, s);
+    else e = a.dtype ? launch_rows<__bf16>(a, rows, counted, s) : launch_rows<float>(a, rows, counted, s);
   }
-  if (a.loss) hipLaunchKernelGGL(sum_rows_kernel, dim3(1), dim3(1024), 0, s, rows, a.B, a.scale, counted, a.loss);
-  return hipGetLastError();
+  if (e == hipSuccess && a.loss) hipLaunchKernelGGL(sum_rows_kernel, dim3(1), dim3(1024), 0, s, rows, a.B, a.scale, counted, a.loss);
+  return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace mgrit
