@@ -84,6 +84,17 @@ __device__ __forceinline__ void store8(__bf16* p, const float (&v)[8]) {
   for (int k = 0; k < 8; ++k) b[k] = narrow<__bf16>(v[k]);
   *reinterpret_cast<bf16x8u*>(p) = b;
 }
+template <typename T> struct Raw8;                               // eight entries as they were loaded
+template <> struct Raw8<float> {
+  floatx4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const floatx4u*>(p); b = *reinterpret_cast<const floatx4u*>(p + 4); }
+  __device__ __forceinline__ float at(int k) const { return k < 4 ? a[k & 3] : b[k & 3]; }
+};
+template <> struct Raw8<__bf16> {
+  bf16x8 a;
+  __device__ __forceinline__ void load(const __bf16* p) { a = *reinterpret_cast<const bf16x8u*>(p); }
+  __device__ __forceinline__ float at(int k) const { return widen(a[k]); }
+};
 template <typename OT>
 __device__ __forceinline__ void put8(OT* p, const float (&v)[8], bool whole, long long left) {
   if (whole) {
@@ -94,8 +105,9 @@ __device__ __forceinline__ void put8(OT* p, const float (&v)[8], bool whole, lon
       if (k < left) p[k] = narrow<OT>(v[k]);
   }
 }
+// (r: the residual's eight where `whole`, loaded ahead)
 template <typename OT>
-__device__ __forceinline__ void finish8(const Epilogue& e, long long at, float (&v)[8], const float (&bias)[8], bool whole, long long left) {
+__device__ __forceinline__ void finish8(const Epilogue& e, long long at, float (&v)[8], const float (&bias)[8], const Raw8<OT>& r, bool whole, long long left) {
   OT* out = static_cast<OT*>(e.out) + at;
   if (!e.fwd) {
 #pragma unroll
@@ -103,21 +115,17 @@ __device__ __forceinline__ void finish8(const Epilogue& e, long long at, float (
     put8(out, v, whole, left);
     return;
   }
-  float d[8], r[8];
-  if (e.R) {
-    const OT* R = static_cast<const OT*>(e.R) + at;
-    if (whole) {
-      load8(R, r);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) r[k] = k < left ? widen(R[k]) : 0.0f;
-    }
-  }
+  float d[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const Out o = activate(v[k] + bias[k], e.act);
-    v[k] = e.R ? r[k] + e.scale * o.y : e.scale * o.y;
+    v[k] = e.scale * o.y;
     d[k] = e.scale * o.d;
+  }
+  if (e.R) {
+    const OT* R = static_cast<const OT*>(e.R) + at;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += whole ? r.at(k) : k < left ? widen(R[k]) : 0.0f;
   }
   put8(out, v, whole, left);
   if (e.D) put8(static_cast<OT*>(e.D) + at, d, whole, left);
@@ -891,8 +899,8 @@ struct Stream {
   }
 };
 
-// Tile of BT x BT outputs, four wavefronts with a quarter each.  Two slabs of both operands are in LDS: while one
-// is multiplied in four steps, the next one is on its way.  Behind the last step's reads a barrier says that nobody needs the old slab
+// Tile of BT x BT outputs, four wavefronts with a quarter each.  While one slab is multiplied in four steps, the next one and A's part of
+// the one after that are on their way into LDS.  Behind the last step's reads a barrier says that nobody needs the old slab
 // any more and that the next one has arrived; the loads of the one after go out at once and have a whole slab's time.
 template <typename CT, int BT, typename OT, bool AS, bool BS>
 __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int share, unsigned char* lds) {
@@ -910,24 +918,23 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   Stream<CT, BT, BS> sb;
   sa.init(a.A, i0, a.I, a.Kc, t0 / a.slabs, t0 % a.slabs, wave, lane, wi);
   sb.init(a.B, j0, a.J, a.Kc, 0, t0 % a.slabs, wave, lane, wj);
-  int left = a.slabs - t0 % a.slabs;                             // of this pass: A's parts one by one, each against the whole of B
+  // slabs left of this pass: A's parts one by one, each against the whole of B
+  int leftA = a.slabs - t0 % a.slabs, leftB = leftA;
   const unsigned lds_at = (unsigned)(unsigned long long)(LdsPtr*)lds;
-  auto load = [&](int buf, int i) {                              // load i of 2 NL
-    const unsigned slab = lds_at + buf * 2 * SLAB;
-    if (i < NL) sa.load(i, slab, wave);
-    else sb.load(i - NL, slab + SLAB, wave);
-  };
-  auto next = [&]() {
+  auto nextA = [&]() {
     sa.next(a.A);
+    if (--leftA == 0) { leftA = a.slabs; sa.again(a.A, a.slabs, true); }
+  };
+  auto nextB = [&]() {
     sb.next(a.B);
-    if (--left == 0) { left = a.slabs; sa.again(a.A, a.slabs, true); sb.again(a.B, a.slabs, false); }
+    if (--leftB == 0) { leftB = a.slabs; sb.again(a.B, a.slabs, false); }
   };
   const int c = lane & 31, g = lane >> 5;
   Frag fa[2][T], fb[2][T];
-  auto read = [&](int buf, int step, int n) {                    // fragment n of 2 T
-    const unsigned char* slab = lds + buf * 2 * SLAB;
-    if (n & 1) fb[step & 1][n / 2] = sb.read(slab + SLAB, step, n / 2);
-    else       fa[step & 1][n / 2] = sa.read(slab, step, n / 2);
+  // places in LDS: three of A's slabs, then two of B's
+  auto read = [&](int pa, int pb, int step, int i) {             // tile i's fragments
+    fa[step & 1][i] = sa.read(lds + pa, step, i);
+    fb[step & 1][i] = sb.read(lds + pb, step, i);
   };
   floatx16 acc[T][T];
 #pragma unroll
@@ -936,84 +943,109 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
     for (int j = 0; j < T; ++j) acc[i][j] = zero16();
 
   // One slab.  In every step the reads of the next one are spread over the first half of the multiplications; the order is fixed
-  // in NG groups of MG multiplications.  The loads of the slab after the next begin behind the barrier and are spread over SPREAD
-  // steps: the address unit takes 16 cycles for one, and a wavefront that waits for it multiplies nothing.
-  constexpr int NG = T == 1 ? 1 : 2 * T, MG = T * T / NG;
-  constexpr int SPREAD = 3, PER = (2 * NL + NG * SPREAD - 1) / (NG * SPREAD);             // loads in a group
-  auto multiply = [&](int buf, auto rest, auto more, auto last) {
+  // in NG groups of MG multiplications.  Loads are spread over all steps, a quarter of a slab's in each, because the address unit takes 16
+  // cycles for one of four wavefronts and a wavefront that waits for it multiplies nothing (all of them in two steps: 8192^3 bf16
+  // 828 us): B's of the slab after the next from step 3 on, behind the barrier that frees their place, and in the next slab's
+  // step 0, A's in steps 1 and 2.
+  constexpr int NG = T == 1 ? 1 : 2 * T, MG = T * T / NG, HALF = NL / 2;
+  int pa = 0, pb = 3 * SLAB;                                     // of the slab that is multiplied
+  auto multiply = [&](auto more, auto last) {
+    const int pa1 = pa == 2 * SLAB ? 0 : pa + SLAB, pa2 = pa1 == 2 * SLAB ? 0 : pa1 + SLAB, pb1 = 7 * SLAB - pb;
 #pragma unroll
     for (int step = 0; step < 4; ++step) {
-      if (step == 3) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      // what this slab's last reads asked for, and the next slab: all loads but those of steps 1 and 2
+      if (step == 3 && more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(NL) : "memory");
+      if (step == 3 && !more) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
-        if (n < T && !(step == 3 && last)) {
-          read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n);
-          read(step < 3 ? buf : buf ^ 1, (step + 1) & 3, 2 * n + 1);
-        }
-        const int group = (step + 1) % 4 * NG + n;
-#pragma unroll
-        for (int k = group * PER; k < (group + 1) * PER && k < 2 * NL; ++k) {
-          if (step == 3 && more) load(buf, k);
-          if (step < 3 && rest) load(buf ^ 1, k);
+        if (n < T && !(step == 3 && last)) read(step < 3 ? pa : pa1, step < 3 ? pb : pb1, (step + 1) & 3, n);
+        if (n * HALF % NG < HALF) {                               // every NG / HALF'th group: load k of the step's half
+          const int k = n * HALF / NG;
+          if (step == 0 && !last) sb.load(HALF + k, lds_at + pb1, wave);
+          if (step == 1 && more) sa.load(k, lds_at + pa2, wave);
+          if (step == 2 && more) sa.load(HALF + k, lds_at + pa2, wave);
+          if (step == 3 && more) sb.load(k, lds_at + pb, wave);
         }
 #pragma unroll
         for (int k = 0; k < MG; ++k) {
           const int m = n * MG + k;
-          Mma<CT>::go(fa[step & 1][m / T], fb[step & 1][m % T], acc[m / T][m % T]);
+          Mma<CT>::go(fb[step & 1][m % T], fa[step & 1][m / T], acc[m / T][m % T]);     // (B first: see the end)
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (step == SPREAD - 2 && rest) next();
+      if (step == 0 && !last) nextB();
+      if (step == 2 && more) nextA();
     }
+    pa = pa1;
+    pb = pb1;
   };
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
 #pragma unroll
-  for (int i = 0; i < 2 * NL; ++i) load(0, i);
-  next();
-  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  for (int i = 0; i < NL; ++i) { sa.load(i, lds_at, wave); sb.load(i, lds_at + 3 * SLAB, wave); }
+  nextA();
+  nextB();
   if (t0 + 1 < t1) {
 #pragma unroll
-    for (int i = 0; i < NG * PER && i < 2 * NL; ++i) load(1, i);
+    for (int i = 0; i < NL; ++i) sa.load(i, lds_at + SLAB, wave);
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) sb.load(i, lds_at + 4 * SLAB, wave);
+    nextA();
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(NL + HALF) : "memory");
+  } else {
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   }
 #pragma unroll
-  for (int n = 0; n < 2 * T; ++n) read(0, 0, n);
-  int buf = 0;
-  for (int t = t0; t < t1 - 2; ++t, buf ^= 1) multiply(buf, yes, yes, no);
-  if (t0 + 1 < t1) { multiply(buf, yes, no, no); buf ^= 1; }
-  multiply(buf, no, no, yes);
+  for (int i = 0; i < T; ++i) read(pa, pb, 0, i);
+  for (int t = t0; t < t1 - 2; ++t) multiply(yes, no);
+  if (t0 + 1 < t1) multiply(no, no);
+  multiply(no, yes);
 
-  // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands
-  constexpr int W = BT / 2, PITCH = W + 4;
-  float* strip = reinterpret_cast<float*>(lds) + wave * 32 * PITCH;
+  // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands.  With B as the
+  // instructions' first operand a lane has four consecutive columns of one row of every tile, which it writes at once.  (The rows
+  // are a loop that stays one: unrolled, the epilogue with its activations is 300 KB of instructions, and fetching them costs
+  // more than the residual's loads: 8192 x 1024 x 4096 bf16 109 us, 86 so.)
+  constexpr int W = BT / 2, PITCH = W + 4, STEP = 512 / W, IT = 32 / STEP;
   const int lc = lane % (W / 8) * 8, lr = lane / (W / 8);
-  const long long col = j0 + wj * W + lc;
-  const long long n = a.I * a.J;
-  const bool whole = col + 8 <= a.J;
-  float bias[8];
+  const long long col = j0 + wj * W + lc, n = a.I * a.J;
+  const bool whole = col + 8 <= a.J, residual = a.e.fwd && a.e.R && whole;
+  const long long row0 = i0 + wi * W + lr;
+  float bias[8] = {};
+  if (a.e.fwd && a.e.bias && !a.partial) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) bias[k] = a.e.fwd && a.e.bias && !a.partial && col + k < a.J ? a.e.bias[col + k] : 0.0f;
-#pragma unroll
+    for (int k = 0; k < 8; ++k) bias[k] = a.e.bias[col + k < a.J ? col + k : a.J - 1];
+  }
+#pragma unroll 1
   for (int i = 0; i < T; ++i) {
+    // (two strips in turn: what is read of one does not hold up the next one's writes)
+    float* strip = reinterpret_cast<float*>(lds) + (wave * 2 + (i & 1)) * 32 * PITCH;
 #pragma unroll
-    for (int j = 0; j < T; ++j)
+    for (int m = 0; m < T; ++m) {
+      if (m != i) continue;                                       // (registers have no index)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) strip[((r & 3) + 8 * (r >> 2) + 4 * g) * PITCH + j * 32 + c] = acc[i][j][r];
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<floatx4*>(strip + c * PITCH + j * 32 + 8 * q + 4 * g) = floatx4{acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
+    }
     __builtin_amdgcn_wave_barrier();
-    for (int r = lr; r < 32; r += 512 / W) {
-      const long long row = i0 + wi * W + i * 32 + r, at = row * a.J + col;
+    const float* from = strip + lr * PITCH + lc;
+    long long row = row0 + i * 32;
+#pragma unroll 2
+    for (int k = 0; k < IT; ++k, row += STEP, from += STEP * PITCH) {
+      const long long at = row * a.J + col;
+      if (row >= a.I) continue;
+      Raw8<OT> r = {};
+      if (residual && !a.partial) r.load(static_cast<const OT*>(a.e.R) + at);
       float v[8];
-      *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(strip + r * PITCH + lc);
-      *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(strip + r * PITCH + lc + 4);
-      if (row < a.I) {
-        if (a.partial) put8(a.partial + share * n + at, v, whole, a.J - col);
-        else finish8<OT>(a.e, at, v, bias, whole, a.J - col);
-      }
+      *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(from);
+      *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(from + 4);
+      if (a.partial) put8(a.partial + share * n + at, v, whole, a.J - col);
+      else finish8<OT>(a.e, at, v, bias, r, whole, a.J - col);
     }
     __builtin_amdgcn_wave_barrier();
   }
 }
-
 constexpr int wide_waves(int bt) { return bt == 256 ? 1 : bt == 128 ? 2 : 4; }          // workgroups of a compute unit
 template <typename CT, int BT, typename OT, bool AS, bool BS>
 __global__ __launch_bounds__(256, wide_waves(BT)) void product_wide_kernel(WideArgs a) {
@@ -1229,7 +1261,7 @@ size_t parts_workspace(const Product& q) {
 template <typename CT, int BT, typename OT, bool AS, bool BS>
 hipError_t launch_wide_tiles(const WideArgs& a, int parts, hipStream_t s) {
   static LdsOptIn opt;
-  const size_t smem = 4 * BT * 128;
+  const size_t smem = 5 * BT * 128;
   const hipError_t e = opt.raise(reinterpret_cast<const void*>(&product_wide_kernel<CT, BT, OT, AS, BS>), smem);
   if (e != hipSuccess) return e;
   const long long tiles = (a.I + BT - 1) / BT * ((a.J + BT - 1) / BT);
@@ -1270,7 +1302,11 @@ hipError_t launch_wide_product(const Product& q, void* partial, hipStream_t s) {
 }
 template <typename CT, int BT>
 hipError_t launch_pair_tiles(const WideArgs& w, const WideArgs& x, int parts_w, int parts_x, hipStream_t s) {
-  const size_t smem = 4 * BT * 128;                     // (at most 64 KB: no opt-in)
+  static LdsOptIn opt[2];
+  const size_t smem = 5 * BT * 128;
+  const hipError_t e = x.e.otype ? opt[1].raise(reinterpret_cast<const void*>(&product_pair_kernel<CT, BT, __bf16>), smem)
+                                 : opt[0].raise(reinterpret_cast<const void*>(&product_pair_kernel<CT, BT, float>), smem);
+  if (e != hipSuccess) return e;
   const unsigned tw = (unsigned)((w.I + BT - 1) / BT * ((w.J + BT - 1) / BT)), tx = (unsigned)((x.I + BT - 1) / BT * ((x.J + BT - 1) / BT));
   const dim3 grid(tw * parts_w + tx * parts_x);
   if (x.e.otype) hipLaunchKernelGGL((product_pair_kernel<CT, BT, __bf16>), grid, dim3(256), smem, s, w, x, tw * parts_w, tw, tx);
