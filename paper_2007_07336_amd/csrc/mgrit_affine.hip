@@ -1062,7 +1062,7 @@ __global__ __launch_bounds__(256, wide_waves(BT)) void product_pair_kernel(WideA
 }
 
 // Operand -> planes of CT: rows x (k padded to ldo with zeros), PARTS of them: 1 as it is (or widened); 2: the product of two bf16
-// values, which has 16 significant bits, as the sum of two.  A thread has eight columns of every eighth row of a workgroup's
+// values, which has 16 significant bits, as the sum of two; 3: a float as the sum of three.  A thread has eight columns of every eighth row of a workgroup's
 // span x 256 entries.  With `sums` the columns' sums over the span as well (of the gradient, for the bias), and PARTS = 0 is
 // those alone.  Bound by memory.  All that a call lays out goes in one launch, one job for each array.
 struct LayJob {
@@ -1105,11 +1105,15 @@ __device__ __forceinline__ void lay_out(const LayJob& a, float (&sh)[8][256]) {
       }
       if constexpr (PARTS > 0) {
         CT* o = out + r * ldo + k;
-        if constexpr (PARTS == 2) {
-          float lo[8];
+        if constexpr (PARTS >= 2) {
+          float lo[8], least[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) split2(v[j], &v[j], &lo[j]);
+          for (int j = 0; j < 8; ++j) {
+            split2(v[j], &v[j], &lo[j]);
+            if (PARTS == 3) split2(lo[j], &lo[j], &least[j]);
+          }
           store8(o + a.rows * ldo, lo);
+          if (PARTS == 3) store8(o + 2 * a.rows * ldo, least);
         }
         store8(o, v);
       }
@@ -1134,9 +1138,11 @@ __global__ __launch_bounds__(256) void lay_out_kernel(LayJobs jobs) {
   switch (a.kind) {
     case 0: lay_out<float, float, 1, false>(a, sh); break;
     case 1: lay_out<__bf16, float, 1, false>(a, sh); break;
+    case 2: lay_out<float, __bf16, 3, false>(a, sh); break;
     case 3: lay_out<__bf16, __bf16, 1, false>(a, sh); break;
     case 4: lay_out<float, float, 1, true>(a, sh); break;
     case 5: lay_out<__bf16, float, 1, true>(a, sh); break;
+    case 6: lay_out<float, __bf16, 3, true>(a, sh); break;
     case 7: lay_out<__bf16, __bf16, 2, true>(a, sh); break;
     case 8: lay_out<float, float, 0, false>(a, sh); break;
     case 9: lay_out<__bf16, float, 0, false>(a, sh); break;
@@ -1175,7 +1181,17 @@ int lay_span(long long rows, long long tiles) {
   return (int)(n < 8 ? 8 : n > 64 ? 64 : n);
 }
 
-// ---- which operands have to be laid out
+// ---- which matrix instructions, and which operands have to be laid out
+// Two bf16 operands go to the bf16 instructions, and a float A against a bf16 B does if the product is large: three parts hold
+// a float's 24 bits, and three passes of the bf16 instructions take less than one of the float ones, by more than the two planes' worth
+// of bytes that laying it out in parts costs over widening B.
+// us on the float / the bf16 instructions, float rows on bf16 weights: 256 x 1024 x 1024 18.1 / 18.0, 512 x 1024 x 1024 24.7 / 22.0, 1024^3
+// 28.6 / 25.1 (with its backward pass, whose two products then no longer share a launch, 75 / 76), 4096 x 1024 x 4096 263 / 114.
+constexpr double SPLIT = 1.0e9;
+inline bool on_bf16(const Product& q) {
+  return q.B.type && (q.A.type || (double)q.I * (double)q.J * (double)q.Kc >= SPLIT);
+}
+inline int bf16_parts(int type, const void* factors) { return type ? (factors ? 2 : 1) : 3; }
 inline int slab_of(bool bf16) { return bf16 ? 64 : 32; }
 inline bool in_place(const Operand& o, bool bf16, long long Kc) {
   if (o.f || (o.type != 0) != bf16) return false;
@@ -1201,7 +1217,7 @@ struct Layout {
     // (row length: whole slabs along k; with k slow whole 16-byte pieces, of which 8 entries are some)
     const long long m = o.kslow ? 8 : slab_of(bf16), r = o.kslow ? Kc : rows, k = o.kslow ? rows : Kc, ld = (k + m - 1) / m * m;
     Operand n = {};
-    n.parts = bf16 && o.f ? 2 : 1;
+    n.parts = bf16 ? bf16_parts(o.type, o.f) : 1;
     n.p = take((size_t)n.parts * r * ld * (bf16 ? 2 : 4));
     n.ld = ld; n.type = bf16; n.kslow = o.kslow; n.padded = 1; n.part = r * ld;
     add(o.p, o.f, o.type, bf16, r, k, const_cast<void*>(n.p), ld, lay_span(r, (ld + 255) / 256), 1.0f, nullptr);
@@ -1230,8 +1246,8 @@ struct WidePlan {
 // launch and the traffic that join the parts.
 WidePlan wide_plan(const Product& q) {
   WidePlan w = {};
-  w.bf16 = q.A.type && q.B.type;
-  w.passes = q.A.parts > 1 ? q.A.parts : w.bf16 && q.A.f ? 2 : 1;
+  w.bf16 = on_bf16(q);
+  w.passes = q.A.parts > 1 ? q.A.parts : 1;
   w.slabs = (int)((q.Kc + slab_of(w.bf16) - 1) / slab_of(w.bf16));
   const int total = w.slabs * w.passes;
   double best = 0.0;
@@ -1368,13 +1384,13 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
   bool summed = !b.db;
   Operand G[2] = {};                  // [bf16]
   for (int bf16 = 0; bf16 < 2; ++bf16) {
-    const bool for_x = x && (p.x.A.type && p.x.B.type) == bf16 && !in_place(p.x.A, bf16, p.x.Kc);
-    const bool for_w = w && (p.w.A.type && p.w.B.type) == bf16 && !in_place(p.w.A, bf16, p.w.Kc);
+    const bool for_x = x && on_bf16(p.x) == (bf16 != 0) && !in_place(p.x.A, bf16, p.x.Kc);
+    const bool for_w = w && on_bf16(p.w) == (bf16 != 0) && !in_place(p.w.A, bf16, p.w.Kc);
     if (!for_x && !for_w) continue;
     Operand& g = G[bf16];
     const int m = slab_of(bf16);
     g.ld = (b.F + m - 1) / m * m;
-    g.type = bf16; g.padded = 1; g.parts = bf16 && b.D ? 2 : 1; g.part = b.M * g.ld;
+    g.type = bf16; g.padded = 1; g.parts = bf16 ? bf16_parts(b.ytype, b.D) : 1; g.part = b.M * g.ld;
     g.p = p.lay.take((size_t)g.parts * g.part * (bf16 ? 2 : 4));
     p.lay.add(b.dY, b.D, b.ytype, bf16, b.M, b.F, const_cast<void*>(g.p), g.ld, summed ? lay_span(b.M, (g.ld + 255) / 256) : sum_span(b.M), b.scale,
               summed ? nullptr : p.sums);
@@ -1383,8 +1399,8 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
     if (for_w) { p.w.A = g; p.w.A.kslow = 1; }
   }
   if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums);
-  if (x) p.x.B = p.lay.plane(p.x.B, p.x.A.type && p.x.B.type, p.x.J, p.x.Kc);
-  if (w) p.w.B = p.lay.plane(p.w.B, p.w.A.type && p.w.B.type, p.w.J, p.w.Kc);
+  if (x) p.x.B = p.lay.plane(p.x.B, on_bf16(p.x), p.x.J, p.x.Kc);
+  if (w) p.w.B = p.lay.plane(p.w.B, on_bf16(p.w), p.w.J, p.w.Kc);
   p.pair = x && w && pairs(p.w, p.x);
   const size_t nx = b.dX ? up(parts_workspace(p.x)) : 0, nw = b.dW ? up(parts_workspace(p.w)) : 0;
   p.partial_x = base + p.lay.bytes;
@@ -1469,7 +1485,7 @@ size_t product_workspace(const Product& q) {
   if (!wide_sizes(q)) return parts_workspace(q);
   Layout l = {};
   Product p = q;
-  const bool bf16 = q.A.type && q.B.type;
+  const bool bf16 = on_bf16(q);
   p.A = l.plane(q.A, bf16, q.I, q.Kc);
   p.B = l.plane(q.B, bf16, q.J, q.Kc);
   return l.bytes + parts_workspace(p);
@@ -1485,7 +1501,7 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
   Layout l = {};
   l.base = static_cast<char*>(ws);
   Product p = q;
-  const bool bf16 = q.A.type && q.B.type;
+  const bool bf16 = on_bf16(q);
   p.A = l.plane(q.A, bf16, q.I, q.Kc);
   p.B = l.plane(q.B, bf16, q.J, q.Kc);
   const hipError_t e = l.launch(s);

@@ -198,3 +198,49 @@ def test_the_same_call_gives_the_same_bits():
         first = a.backward(D)
         for _ in range(3):
             assert all(torch.equal(x, y) for x, y in zip(first, a.backward(D)))
+
+
+# float rows against bf16 weights, large enough for products in parts: forward, both gradients, with factors and without
+@pytest.mark.parametrize("types", ["fbf", "bbf"])
+@pytest.mark.parametrize("rows,K,F", [(1100, 1024, 1000), (300, 1999, 2111), (4096, 520, 600)])
+def test_products_in_parts(rows, K, F, types):
+    a = Affine(rows, K, F, types, "tanh", 0.5, residual=True)
+    _, D = a.check_forward(factor=True)
+    a.check_backward(D)
+    Affine(rows, K, F, types, "identity", -0.7, seed=3).check_backward(None)
+
+
+@pytest.mark.parametrize("types,rows,K,F", [("fbf", 1100, 1024, 1000), ("bbb", 600, 512, 520)])
+def test_infinities_in_products_in_parts(types, rows, K, F):
+    """Not finite where the formula is not, and nowhere else."""
+    a = Affine(rows, K, F, types, "tanh")
+    D = torch.rand((rows, F), generator=torch.Generator().manual_seed(1)).to(a.dY.dtype).cuda() + 0.1
+    a.X[1, 3], a.X[2, 0], a.W[5, 7], a.dY[4, 2], D[9, 9] = (float(v) for v in ("inf", "nan", "-inf", "inf", "nan"))
+    big = torch.finfo(torch.float32).max if types[0] == "f" else 3e38
+    a.X[7, 7], a.W[5, 8] = big, 0.5                             # next to what bf16 rounds to infinity
+    Y = a.new((rows, F), types[2])
+    p = M.make_affine(M=rows, K=K, F=F, xtype=a.p.xtype, wtype=a.p.wtype, ytype=a.p.ytype)
+    M.mgrit_affine_forward(p, a.X, a.W, None, None, Y, None, a.ws)
+    z = a.X.double() @ a.W.double().T
+    over = z.abs() > 3.3e38                                      # sums that leave float may do so at any point
+    assert torch.equal(torch.isfinite(Y)[~over], torch.isfinite(z)[~over])
+    dX, dW, db = a.backward(D)
+    G = a.dY.double() * D.double()
+    for got, want in ((dX, G @ a.W.double()), (dW, G.T @ a.X.double()), (db, G.sum(0))):
+        over = want.abs() > 3.3e38
+        assert torch.equal(torch.isfinite(got)[~over], torch.isfinite(want)[~over])
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Contractions and rows whose offsets within a tile pass 2^31 bytes: the plain tile takes them."""
+    a = Affine(70, 1100001, 66, "bbb", "tanh", residual=True)
+    _, D = a.check_forward(factor=True)
+    a = Affine(17, 4300003, 18, "bbb", bias=False)
+    a.check_backward(None)
+
+
+@pytest.mark.parametrize("rows,K,F", [(1, 300000, 1), (70000, 5, 2), (2, 3, 200000), (1, 2, 3), (100000, 20, 20), (19, 1, 70), (70, 70, 1)])
+def test_long_and_thin(rows, K, F):
+    a = Affine(rows, K, F, "fff", "tanh", 0.5)
+    _, D = a.check_forward(factor=True)
+    a.check_backward(D)
