@@ -402,6 +402,26 @@ def mgrit_cross_entropy(p: mgrit_loss_t, logits, labels, loss, row_loss, grad, w
         p, _ptr(logits), _ptr(labels), _ptr(loss), _ptr(row_loss), _ptr(grad), _ptr(workspace), _size(workspace), s))
 
 
+def _refuse_overlap(where, spans):
+    """Refuses results that overlap a tensor other than the one they replace, or another result: a tensor that is listed twice would
+    be scaled twice.  spans: (address, bytes, index, 1 for a result)."""
+    furthest = [[(0, -1), (0, -1)], [(0, -1), (0, -1)]]       # of all spans and of results: the two furthest ends of different indices
+    place = {}
+    for at, size, i, k in sorted(spans):
+        others = furthest[0 if k else 1]
+        end = others[0][0] if others[0][1] != i else others[1][0]
+        mine = place.setdefault(i, (at, size))
+        if at < end or (mine != (at, size) and at < mine[0] + mine[1]):
+            raise ValueError(f"{where}: {'result' if k else 'tensor'} {i} overlaps another one")
+        for f in furthest[:2 if k else 1]:
+            if i == f[0][1]:
+                f[0] = (max(f[0][0], at + size), i)
+            elif at + size > f[0][0]:
+                f[0], f[1] = (at + size, i), f[0]
+            elif i == f[1][1] or at + size > f[1][0]:
+                f[1] = (max(at + size, f[1][0] if i == f[1][1] else 0), i)
+
+
 class TensorList:
     """Tensors to clip: the descriptors handed to the library, and the tensors, which are kept alive."""
 
@@ -411,7 +431,7 @@ class TensorList:
         if len(self.src) != len(self.dst):
             raise ValueError(f"{where}: {len(self.src)} tensors, {len(self.dst)} results")
         self.array = (mgrit_tensor_t * max(1, len(self.src)))()
-        self.device = None
+        self.device, spans = None, []
         for i, (a, b) in enumerate(zip(self.src, self.dst)):
             if a.dtype not in T[:2]:
                 raise ValueError(f"{where}: tensor {i} has type {a.dtype}")
@@ -419,7 +439,10 @@ class TensorList:
             if self.device is not None and device != self.device:
                 raise ValueError(f"{where}: tensor {i} is on GPU {device}, others on GPU {self.device}")
             self.device = device
+            spans += [(t.data_ptr(), t.numel() * t.element_size(), i, k) for k, t in enumerate((a, b)) if t is not None and t.numel()]
             self.array[i] = mgrit_tensor_t(src=_ptr(a), dst=_ptr(b), count=a.numel(), dtype=T.index(a.dtype))
+
+        _refuse_overlap(where, spans)
 
     def __len__(self):
         return len(self.src)

@@ -465,8 +465,8 @@ __global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_fe
     const unsigned mine = (unsigned)(unsigned long long)(LdsPtr*)lds + wave * Sh::D * Sh::SLAB;
     const unsigned char* my = lds + wave * Sh::D * Sh::SLAB;
     constexpr int LOADS = 2 * (SB * Sh::PS + FB * Sh::PF);
-    auto issue = [&](int t) {                       // slab t to its place; behind the last one the last again, so that the count of loads is the same
-      const long long at = k + (long long)(t < n ? t : n - 1) * Sh::K;
+    auto issue = [&](int t) {                       // slab t to its place
+      const long long at = k + (long long)t * Sh::K;
       const unsigned to = mine + t % Sh::D * Sh::SLAB;
 #pragma unroll
       for (int i = 0; i < SB; ++i)
@@ -484,12 +484,17 @@ __global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_fe
     };
     if (n > 0) {
 #pragma unroll
-      for (int t = 0; t < Sh::D - 1; ++t) issue(t);
+      for (int t = 0; t < Sh::D - 1; ++t)
+        if (t < n) issue(t);
       for (int t = 0; t < n; ++t) {
-        // what was read from the place that is filled next has arrived; then all but the last D - 1 slabs' loads
+        // what was read from the place that is filled next has arrived; then all but the last D - 1 slabs' loads (near the end: all)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        issue(t + Sh::D - 1);
-        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS * (Sh::D - 1)) : "memory");
+        if (t + Sh::D - 1 < n) {
+          issue(t + Sh::D - 1);
+          asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS * (Sh::D - 1)) : "memory");
+        } else {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
         const unsigned char* slab = my + t % Sh::D * Sh::SLAB;
 #pragma unroll
         for (int st = 0; st < Sh::K / 32; ++st) {
@@ -505,7 +510,6 @@ __global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_fe
             for (int j = 0; j < FB; ++j) multiply16(a[i], b[j], acc[i][j]);
         }
       }
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       k += (long long)n * Sh::K;
     }
   }

@@ -2,7 +2,6 @@
 // the order of the launches.  The arithmetic is in mgrit_affine.hip, mgrit_loss.hip and mgrit_clip.hip.
 #include <math.h>
 
-#include <new>
 #include <vector>
 
 #include "../../include/mgrit.h"
@@ -59,7 +58,7 @@ int collect(const mgrit_tensor_t* t, int32_t n, std::vector<ClipTensor>& out) {
   if (n > 0 && !t) return MGRIT_ERR_POINTER;
   try {
     out.reserve((size_t)n);
-  } catch (const std::bad_alloc&) {
+  } catch (...) {
     return MGRIT_ERR_WORKSPACE;
   }
   long long total = 0;

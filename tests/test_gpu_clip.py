@@ -139,3 +139,15 @@ def test_captured_calls_replay():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, w) for x, w in zip(dst + [n], want)), replay
+
+
+def test_tensors_that_overlap_results_are_refused():
+    a, b = normal((100,)), torch.empty((100,), device="cuda")
+    for src, dst in (([a, a], None), ([a, a[50:]], None), ([a, a[10:20]], [None, a[10:20]]), ([a[:50], a[40:]], [b[:50], b[40:]]),
+                     ([a[10:60]], [a[20:70]]), ([a, normal((40,))], [b, a[:40]])):
+        with pytest.raises(ValueError, match="overlaps"):
+            M.make_tensor_list(src, dst)
+    M.make_tensor_list([a], [b])
+    M.make_tensor_list([a, a, a[5:]], [None, None, b[5:]])     # tensors that are only read may overlap
+    M.make_tensor_list([a[:50], a[50:]], [a[:50], a[50:]])
+    M.make_tensor_list([a[:50], a[50:]], [b[:50], b[50:]])

@@ -142,3 +142,30 @@ def test_binding_refuses_tensors_that_do_not_fit():
         M.make_tensor_list([X], [X, X])
     with pytest.raises(ValueError, match="no tensor given"):
         M.mgrit_clip_gradients(M.make_tensor_list([]), 1.0, None, None)
+
+
+def test_overlap_rule_against_every_pair():
+    """Results may lie on the tensor they replace and on nothing else; tensors that are only read may overlap."""
+    import random
+    r, refused = random.Random(1), 0
+
+    def bad_pair(x, y):
+        meet = x[0] < y[0] + y[1] and y[0] < x[0] + x[1]
+        return meet and (x[3] or y[3]) and not (x[:3] == y[:3] and x[3] != y[3])
+
+    for _ in range(20000):
+        spans = []
+        for i in range(r.randint(1, 5)):
+            n, at, kind = r.randint(1, 4), r.randint(1, 30), r.random()
+            spans.append((at, n, i, 0))
+            if kind < 0.8:
+                spans.append((at if kind < 0.4 else r.randint(1, 30), n, i, 1))
+        want = any(bad_pair(x, y) for k, x in enumerate(spans) for y in spans[:k])
+        try:
+            Bd._refuse_overlap("x", spans)
+            got = False
+        except ValueError:
+            got = True
+        assert got == want, spans
+        refused += want
+    assert 2000 < refused < 18000
