@@ -810,7 +810,8 @@ struct WideArgs {
   Epilogue e;
   long long I, J, Kc;
   int slabs;                   // of one pass over the contraction
-  int passes;                  // A's parts, each of which is multiplied with B
+  int passes;                  // pairs of parts that are multiplied
+  unsigned partA, partB;       // of pass s: bits 4 s .. 4 s + 3
   int per;                     // slabs that one workgroup takes of its tile's, all passes counted
   float* partial;              // several workgroups: their sums
 };
@@ -876,11 +877,11 @@ struct Stream {
     if (KS) { base += KSLAB * p.ld; room -= KSLAB * p.ld; }
     else along += 128;
   }
-  // from behind the last slab to the first one, of the next part (A) or the same (B)
-  __device__ __forceinline__ void again(const Plane& p, int slabs, bool next_part) {
+  // from behind the last slab to the first one, `parts` parts further
+  __device__ __forceinline__ void again(const Plane& p, int slabs, int parts) {
     if (KS) { base -= (long long)slabs * KSLAB * p.ld; room += (long long)slabs * KSLAB * p.ld; }
     else along = 0;
-    if (next_part) base += p.part;
+    base += parts * p.part;
   }
   // fragment of tile i in step `step`
   __device__ __forceinline__ Frag read(const unsigned char* slab, int step, int i) const {
@@ -920,18 +921,20 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   const int total = a.slabs * a.passes, t0 = share * a.per, t1 = t0 + a.per < total ? t0 + a.per : total;
   Stream<CT, BT, AS> sa;
   Stream<CT, BT, BS> sb;
-  sa.init(a.A, i0, a.I, a.Kc, t0 / a.slabs, t0 % a.slabs, wave, lane, wi);
-  sb.init(a.B, j0, a.J, a.Kc, 0, t0 % a.slabs, wave, lane, wj);
-  // slabs left of this pass: A's parts one by one, each against the whole of B
+  // the pass of either operand's next slab, and its slabs that are left; parts by pass
+  int passA = t0 / a.slabs, passB = passA;
+  auto part = [](unsigned parts, int pass) { return (int)(parts >> (4 * pass) & 15u); };
+  sa.init(a.A, i0, a.I, a.Kc, part(a.partA, passA), t0 % a.slabs, wave, lane, wi);
+  sb.init(a.B, j0, a.J, a.Kc, part(a.partB, passB), t0 % a.slabs, wave, lane, wj);
   int leftA = a.slabs - t0 % a.slabs, leftB = leftA;
   const unsigned lds_at = (unsigned)(unsigned long long)(LdsPtr*)lds;
   auto nextA = [&]() {
     sa.next(a.A);
-    if (--leftA == 0) { leftA = a.slabs; sa.again(a.A, a.slabs, true); }
+    if (--leftA == 0) { leftA = a.slabs; sa.again(a.A, a.slabs, part(a.partA, passA + 1) - part(a.partA, passA)); ++passA; }
   };
   auto nextB = [&]() {
     sb.next(a.B);
-    if (--leftB == 0) { leftB = a.slabs; sb.again(a.B, a.slabs, false); }
+    if (--leftB == 0) { leftB = a.slabs; sb.again(a.B, a.slabs, part(a.partB, passB + 1) - part(a.partB, passB)); ++passB; }
   };
   const int c = lane & 31, g = lane >> 5;
   Frag fa[2][T], fb[2][T];
@@ -1192,8 +1195,12 @@ int lay_span(long long rows, long long tiles) {
 // us on the float / the bf16 instructions, float rows on bf16 weights: 256 x 1024 x 1024 18.1 / 18.0, 512 x 1024 x 1024 24.7 / 22.0, 1024^3
 // 28.6 / 25.1 (with its backward pass, whose two products then no longer share a launch, 75 / 76), 4096 x 1024 x 4096 263 / 114.
 constexpr double SPLIT = 1.0e9;
-inline bool on_bf16(const Product& q) {
-  return q.B.type && (q.A.type || (double)q.I * (double)q.J * (double)q.Kc >= SPLIT);
+// Two float operands, six passes, on the float / the bf16 instructions: 2048 x 1024 x 2048 70 / 70, 2048^3 129 / 123 and its backward pass
+// 258 / 228, 4096 x 1024 x 4096 273 / 195, 4096^3 936 / 656; backward of 2048 x 1000 x 1000 82 / 131.
+constexpr double SPLIT2 = 6.0e9;
+inline bool on_bf16(const Product& q) {                         // of a product whose operands are not laid out yet, or both
+  const double size = (double)q.I * (double)q.J * (double)q.Kc;
+  return q.A.type ? q.B.type : size >= (q.B.type ? SPLIT : SPLIT2);
 }
 inline int bf16_parts(int type, const void* factors) { return type ? (factors ? 2 : 1) : 3; }
 inline int slab_of(bool bf16) { return bf16 ? 64 : 32; }
@@ -1250,8 +1257,8 @@ struct WidePlan {
 // launch and the traffic that join the parts.
 WidePlan wide_plan(const Product& q) {
   WidePlan w = {};
-  w.bf16 = on_bf16(q);
-  w.passes = q.A.parts > 1 ? q.A.parts : 1;
+  w.bf16 = q.A.type != 0;                                       // (they are planes of one type)
+  w.passes = q.B.parts > 1 ? 6 : q.A.parts > 1 ? q.A.parts : 1;
   w.slabs = (int)((q.Kc + slab_of(w.bf16) - 1) / slab_of(w.bf16));
   const int total = w.slabs * w.passes;
   double best = 0.0;
@@ -1295,21 +1302,32 @@ hipError_t launch_wide_out(const WideArgs& a, bool as, bool bs, int parts, hipSt
   return a.e.otype ? launch_wide_tiles<CT, BT, __bf16, false, false>(a, parts, s) : launch_wide_tiles<CT, BT, float, false, false>(a, parts, s);
 }
 
+// Both operands are planes of the same type
+bool ready(const Product& q) {
+  const bool bf16 = q.A.type != 0;
+  return q.B.type == q.A.type && in_place(q.A, bf16, q.Kc) && in_place(q.B, bf16, q.Kc);
+}
 WideArgs wide_args(const Product& q, const WidePlan& w, void* partial) {
   const long long es = w.bf16 ? 2 : 4;
   WideArgs a = {};
   a.A = Plane{static_cast<const char*>(q.A.p), q.A.ld * es, q.A.part * es};
-  a.B = Plane{static_cast<const char*>(q.B.p), q.B.ld * es, 0};
+  a.B = Plane{static_cast<const char*>(q.B.p), q.B.ld * es, q.B.part * es};
   a.e = q.e;
   a.I = q.I; a.J = q.J; a.Kc = q.Kc;
   a.slabs = w.slabs;
   a.passes = w.passes;
+  // A's parts each against B; of three parts each, the six pairs that make up a float product: the three that are left out are
+  // at most 2^-23 of it together.  The smallest first: added to the sum of the large ones, each of them would round that once
+  // more (1024^3 float: 6.7e-7 off with the largest first, 1.8e-7 so, the float instructions 5.7e-7).
+  a.partA = w.passes == 6 ? 0x001120u : w.passes == 3 ? 0x012u : w.passes == 2 ? 0x01u : 0u;
+  a.partB = w.passes == 6 ? 0x010102u : 0u;
   a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;
   a.partial = w.parts > 1 ? static_cast<float*>(partial) : nullptr;
   return a;
 }
 // The product of operands that are in place or laid out
 hipError_t launch_wide_product(const Product& q, void* partial, hipStream_t s) {
+  if (!ready(q)) return hipErrorInvalidValue;
   const WidePlan w = wide_plan(q);
   const WideArgs a = wide_args(q, w, partial);
   hipError_t e;
@@ -1341,6 +1359,7 @@ bool pairs(const Product& w, const Product& x) {
   return a.bf16 == b.bf16 && a.bt == b.bt && a.bt <= 128 && (tw < 1024 || tx < 1024) && tw + tx < (1LL << 30);
 }
 hipError_t launch_wide_pair(const Product& qw, const Product& qx, char* partial_w, char* partial_x, hipStream_t s) {
+  if (!ready(qw) || !ready(qx)) return hipErrorInvalidValue;
   const WidePlan pw = wide_plan(qw), px = wide_plan(qx);
   const WideArgs w = wide_args(qw, pw, partial_w), x = wide_args(qx, px, partial_x);
   hipError_t e = pw.bf16 ? (pw.bt == 128 ? launch_pair_tiles<__bf16, 128>(w, x, pw.parts, px.parts, s) : launch_pair_tiles<__bf16, 64>(w, x, pw.parts, px.parts, s))
@@ -1385,11 +1404,12 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
   p.chunks = chunks_of(b.M);
   p.sums = p.chunks > 1 ? reinterpret_cast<float*>(p.lay.take((size_t)p.chunks * b.F * sizeof(float))) : b.db;
   const bool x = b.dX && wide_sizes(p.x), w = b.dW && wide_sizes(p.w);
+  const bool x_bf16 = on_bf16(p.x), w_bf16 = on_bf16(p.w);      // (before the planes' types take the operands' place)
   bool summed = !b.db;
   Operand G[2] = {};                  // [bf16]
   for (int bf16 = 0; bf16 < 2; ++bf16) {
-    const bool for_x = x && on_bf16(p.x) == (bf16 != 0) && !in_place(p.x.A, bf16, p.x.Kc);
-    const bool for_w = w && on_bf16(p.w) == (bf16 != 0) && !in_place(p.w.A, bf16, p.w.Kc);
+    const bool for_x = x && x_bf16 == (bf16 != 0) && !in_place(p.x.A, bf16, p.x.Kc);
+    const bool for_w = w && w_bf16 == (bf16 != 0) && !in_place(p.w.A, bf16, p.w.Kc);
     if (!for_x && !for_w) continue;
     Operand& g = G[bf16];
     const int m = slab_of(bf16);
@@ -1403,8 +1423,8 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
     if (for_w) { p.w.A = g; p.w.A.kslow = 1; }
   }
   if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums);
-  if (x) p.x.B = p.lay.plane(p.x.B, on_bf16(p.x), p.x.J, p.x.Kc);
-  if (w) p.w.B = p.lay.plane(p.w.B, on_bf16(p.w), p.w.J, p.w.Kc);
+  if (x) p.x.B = p.lay.plane(p.x.B, x_bf16, p.x.J, p.x.Kc);
+  if (w) p.w.B = p.lay.plane(p.w.B, w_bf16, p.w.J, p.w.Kc);
   p.pair = x && w && pairs(p.w, p.x);
   const size_t nx = b.dX ? up(parts_workspace(p.x)) : 0, nw = b.dW ? up(parts_workspace(p.w)) : 0;
   p.partial_x = base + p.lay.bytes;

@@ -24,18 +24,19 @@ static_assert(sizeof(Givens) + 24 <= 4096, "kernel arguments");
 struct Space { double norm; double partial[GRID]; Entry table[1]; };
 
 __global__ __launch_bounds__(256) void clip_table_kernel(Givens in, Entry* out, int n, long long before) {
-  __shared__ long long sum[256];
+  __shared__ long long of_wave[4];
   const int t = threadIdx.x;
   const long long count = t < n ? in.e[t].count >> 1 : 0, mine = (count + CHUNK - 1) / CHUNK;
-  sum[t] = mine;
-  __syncthreads();
-  for (int d = 1; d < 256; d *= 2) {            // running sums
-    const long long v = t >= d ? sum[t - d] : 0;
-    __syncthreads();
-    sum[t] += v;
-    __syncthreads();
+  long long sum = mine;                         // running sums
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const long long v = __shfl_up(sum, d);
+    if ((t & 63) >= d) sum += v;
   }
-  if (t < n) out[t] = Entry{in.e[t].src, in.e[t].dst, count, before + sum[t] - mine, in.e[t].count & 1};
+  if ((t & 63) == 63) of_wave[t >> 6] = sum;
+  __syncthreads();
+  for (int w = 0; w < t >> 6; ++w) sum += of_wave[w];
+  if (t < n) out[t] = Entry{in.e[t].src, in.e[t].dst, count, before + sum - mine, in.e[t].count & 1};
 }
 
 __device__ __forceinline__ float value(float v) { return v; }

@@ -244,3 +244,12 @@ def test_long_and_thin(rows, K, F):
     a = Affine(rows, K, F, "fff", "tanh", 0.5)
     _, D = a.check_forward(factor=True)
     a.check_backward(D)
+
+
+# two float operands, large enough for products in parts of both; and with a float weight the other types
+@pytest.mark.parametrize("types", ["fff", "ffb", "bff"])
+@pytest.mark.parametrize("rows,K,F", [(2200, 2100, 2301), (4096, 1024, 2560)])
+def test_float_products_in_parts(rows, K, F, types):
+    a = Affine(rows, K, F, types, "tanh", 0.5)
+    _, D = a.check_forward(factor=True)
+    a.check_backward(D)
