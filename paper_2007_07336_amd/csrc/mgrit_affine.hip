@@ -416,7 +416,7 @@ template <typename TS, typename TF, int SB, int FB> struct FewShape {
   static constexpr int K = sizeof(TS) == 2 || sizeof(TF) == 2 ? 64 : 32;       // of a slab
   static constexpr int PS = K * (int)sizeof(TS) / 128, PF = K * (int)sizeof(TF) / 128, SLAB = (SB * PS + FB * PF) * 2048;   // panels; bytes
   // two blocks of stream rows are taken where there are many workgroups: two of them share a compute unit then, if they fit
-  static constexpr int ROOM = (SB == 2 && 4 * 2 * SLAB <= 76 * 1024 ? 76 : 152) * 1024, W = 8 * 2 * SLAB <= ROOM ? 8 : 4 * 2 * SLAB <= ROOM ? 4 : 2;     // wavefronts
+  static constexpr int ROOM = (SB == 2 && 4 * 2 * SLAB <= 76 * 1024 ? 76 : 160) * 1024, W = 8 * 2 * SLAB <= ROOM ? 8 : 4 * 2 * SLAB <= ROOM ? 4 : 2;     // wavefronts
   static constexpr int FIT = ROOM / (W * SLAB), D = FIT > 4 ? 4 : FIT;         // slabs
   static_assert(D >= 2, "two slabs in turn");
 };
@@ -691,6 +691,14 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const long long k = L % blocks * 256 + lane * 4, left = a.K - k;
   const TY *g = static_cast<const TY*>(a.g), *f = static_cast<const TY*>(a.f);
+  // U rows are on their way while U others are multiplied
+  constexpr int U = 4;
+  floatx4 x[2][U];
+  auto load = [&](int set, int r) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[set][u] = load4(static_cast<const TS*>(a.S) + (r0 + r + 4 * u) * a.K + k, r + 4 * u < n ? left : 0);
+  };
+  if (a.outT && wave < n) load(0, wave);         // (before anything is waited for)
   for (int i = t; i < n * NT; i += 256) {
     const int r = a.by_column ? i / NT : i % n, e = a.by_column ? i % NT : i / n;
     float v = 0.0f;
@@ -707,13 +715,6 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
     if (a.outS && e < a.nt) w[e] = load4(static_cast<const TT*>(a.T) + e * a.K + k, left);
   }
   __syncthreads();
-  // U rows are on their way while U others are multiplied
-  constexpr int U = 4;
-  floatx4 x[2][U];
-  auto load = [&](int set, int r) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) x[set][u] = load4(static_cast<const TS*>(a.S) + (r0 + r + 4 * u) * a.K + k, r + 4 * u < n ? left : 0);
-  };
   auto multiply = [&](int set, int r) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -733,7 +734,6 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
       }
     }
   };
-  if (a.outT && wave < n) load(0, wave);
   for (int r = wave; r < n; r += 8 * U) {
     if (a.outT && r + 4 * U < n) load(1, r + 4 * U);
     multiply(0, r);
