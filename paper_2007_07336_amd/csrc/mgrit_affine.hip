@@ -131,6 +131,29 @@ __device__ __forceinline__ void finish8(const Epilogue& e, long long at, float (
   if (e.D) put8(static_cast<OT*>(e.D) + at, d, whole, left);
 }
 
+// The same of eight that all exist, with the kind of epilogue fixed: an activation of the forward pass, or PLAIN
+enum { PLAIN = 3 };
+template <typename OT, int KIND>
+__device__ __forceinline__ void finish8_whole(const Epilogue& e, long long at, float (&v)[8], const float (&bias)[8], const Raw8<OT>& r) {
+  float d[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if constexpr (KIND == PLAIN) {
+      v[k] *= e.scale;
+    } else {
+      const Out o = activate(v[k] + bias[k], KIND);
+      v[k] = e.scale * o.y;
+      d[k] = e.scale * o.d;
+    }
+  }
+  if (KIND != PLAIN && e.R) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += r.at(k);
+  }
+  store8(static_cast<OT*>(e.out) + at, v);
+  if (KIND != PLAIN && e.D) store8(static_cast<OT*>(e.D) + at, d);
+}
+
 // ------------------------------------------------------------------------------------------ from memory to LDS
 typedef __attribute__((address_space(3))) void LdsPtr;
 // 16 bytes per lane from base + each lane's offset + along to LDS address `to` and the 1008 bytes behind it, in lane order; zeros from
@@ -1013,13 +1036,16 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   multiply(no, yes);
 
   // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands.  With B as the
-  // instructions' first operand a lane has four consecutive columns of one row of every tile, which it writes at once.  (The rows
-  // are a loop that stays one: unrolled, the epilogue with its activations is 300 KB of instructions, and fetching them costs
-  // more than the residual's loads: 8192 x 1024 x 4096 bf16 109 us, 86 so.)
+  // instructions' first operand a lane has four consecutive columns of one row of every tile, which it writes at once.  Strips are
+  // a loop, and the unrolled code of a strip's rows is one for each kind of epilogue, of which a call runs one: with everything unrolled the
+  // epilogue is 300 KB of instructions, and fetching those costs more than what they do (8192 x 1024 x 4096 bf16: 109 us, a loop
+  // over rows 89).  The residual of a strip's rows is asked for at once (8192 x 4096 x 4096 bf16 with tanh, residual and factors: 294 us
+  // with two rows' at a time, 250 so).
   constexpr int W = BT / 2, PITCH = W + 4, STEP = 512 / W, IT = 32 / STEP;
   const int lc = lane % (W / 8) * 8, lr = lane / (W / 8);
   const long long col = j0 + wj * W + lc, n = a.I * a.J;
   const bool whole = col + 8 <= a.J, residual = a.e.fwd && a.e.R && whole;
+  const bool inside = i0 + BT <= a.I && j0 + BT <= a.J && !a.partial;
   const long long row0 = i0 + wi * W + lr;
   float bias[8] = {};
   if (a.e.fwd && a.e.bias && !a.partial) {
@@ -1028,6 +1054,11 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   }
 #pragma unroll 1
   for (int i = 0; i < T; ++i) {
+    Raw8<OT> ahead[IT];
+    if (inside && residual) {
+#pragma unroll
+      for (int k = 0; k < IT; ++k) ahead[k].load(static_cast<const OT*>(a.e.R) + (row0 + i * 32 + k * STEP) * a.J + col);
+    }
     // (two strips in turn: what is read of one does not hold up the next one's writes)
     float* strip = reinterpret_cast<float*>(lds) + (wave * 2 + (i & 1)) * 32 * PITCH;
 #pragma unroll
@@ -1042,17 +1073,35 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
     __builtin_amdgcn_wave_barrier();
     const float* from = strip + lr * PITCH + lc;
     long long row = row0 + i * 32;
-#pragma unroll 2
-    for (int k = 0; k < IT; ++k, row += STEP, from += STEP * PITCH) {
-      const long long at = row * a.J + col;
-      if (row >= a.I) continue;
-      Raw8<OT> r = {};
-      if (residual && !a.partial) r.load(static_cast<const OT*>(a.e.R) + at);
-      float v[8];
-      *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(from);
-      *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(from + 4);
-      if (a.partial) put8(a.partial + share * n + at, v, whole, a.J - col);
-      else finish8<OT>(a.e, at, v, bias, r, whole, a.J - col);
+    if (inside) {
+      // all rows and columns exist: the strip's rows one behind the other, the residual of all of them loaded before
+      auto rows = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+#pragma unroll
+        for (int k = 0; k < IT; ++k) {
+          float v[8];
+          *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(from + k * STEP * PITCH);
+          *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(from + k * STEP * PITCH + 4);
+          finish8_whole<OT, KIND>(a.e, (row + k * STEP) * a.J + col, v, bias, ahead[k]);
+        }
+      };
+      if (!a.e.fwd) rows(std::integral_constant<int, PLAIN>{});
+      else if (a.e.act == ACT_TANH) rows(std::integral_constant<int, ACT_TANH>{});
+      else if (a.e.act == ACT_RELU) rows(std::integral_constant<int, ACT_RELU>{});
+      else rows(std::integral_constant<int, ACT_IDENT>{});
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < IT; ++k, row += STEP, from += STEP * PITCH) {
+        const long long at = row * a.J + col;
+        if (row >= a.I) continue;
+        Raw8<OT> r = {};
+        if (residual && !a.partial) r.load(static_cast<const OT*>(a.e.R) + at);
+        float v[8];
+        *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(from);
+        *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(from + 4);
+        if (a.partial) put8(a.partial + share * n + at, v, whole, a.J - col);
+        else finish8<OT>(a.e, at, v, bias, r, whole, a.J - col);
+      }
     }
     __builtin_amdgcn_wave_barrier();
   }
