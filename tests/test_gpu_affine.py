@@ -253,3 +253,25 @@ def test_float_products_in_parts(rows, K, F, types):
     a = Affine(rows, K, F, types, "tanh", 0.5)
     _, D = a.check_forward(factor=True)
     a.check_backward(D)
+
+
+# few rows on one side against so many on the other that a workgroup takes two blocks of them; aligned rows and odd ones; either side
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("few", [3, 16, 17, 32, 33, 50, 64, 65])
+def test_few_rows_against_many(few, types):
+    for K in (200, 515):
+        Affine(few, K, 8203, types, "tanh", 0.5, residual=True).check_forward(factor=True)
+        Affine(8203, K, few, types, "relu", 2.0, bias=False, seed=7).check_forward()
+    a = Affine(few, 72, 8203, types, "identity", 0.3, seed=11)
+    a.check_backward(None)
+
+
+@pytest.mark.parametrize("types", ["fff", "bbb", "fbf"])
+def test_sizes_around_the_tiles(types):
+    """One more and one less than whole tiles and slabs, in every place, so that edges of all three kinds meet."""
+    for n in (63, 65, 127, 129, 255, 257):
+        for rows, K, F in ((n, 96, 160), (160, n, 130), (130, 160, n), (n, n, n)):
+            a = Affine(rows, K, F, types, "tanh", 0.5, seed=n)
+            _, D = a.check_forward(factor=True)
+            a.check_backward(D)
+    Affine(16 * 256 + 1, 64, 16 * 256 - 1, types, "relu", residual=True).check_forward()
