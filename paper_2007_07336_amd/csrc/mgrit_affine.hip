@@ -809,8 +809,8 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------ large products
-// Operands as planes of CT in memory, 16-byte pieces: rows along k, padded with zeros to whole slabs (64 bf16 or 32 float), or
-// with k slow, as the backward pass meets its operands, rows of any multiple of 16 bytes.  What the caller has in this form is read
+// Operands as planes of CT in memory, with rows of any multiple of 16 bytes, along k or with k slow, as the backward pass meets its
+// operands.  What the caller has in this form is read
 // in place; anything else -- ragged, with a factor, of another type -- is laid out in the workspace first, which costs a pass
 // over the operand and keeps the multiplying loop free of everything but multiplications.
 template <typename CT> struct Mma;
@@ -830,6 +830,7 @@ struct Plane {
   const char* p;
   long long ld;                // bytes from row to row (k slow: from k to k)
   long long part;              // bytes from part to part
+  int row;                     // bytes of a row that count: zeros from there on (not with k slow)
 };
 struct WideArgs {
   Plane A, B;
@@ -854,7 +855,7 @@ struct Stream {
   static constexpr int SLAB = BT * 128;
   const char* base;            // of the next slab to load
   long long room;              // bytes from there to the end (k slow)
-  int along, offset[NL];
+  int along, offset[NL], piece[2], row;          // piece: byte of the row's slab that this lane asks for in even and odd loads
   int at[KS ? T : 4];          // where this lane reads: per tile (k slow) or per step
 
   // which pieces of row k change places (k slow)
@@ -886,18 +887,23 @@ struct Stream {
     } else {
       base = p.p + part * p.part + r0 * p.ld;
       along = skip * 128;
+      row = p.row;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
-        const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
-        offset[i] = (int)((r0 + r < rows ? r : rows - 1 - r0) * p.ld) + piece * 16;
+        const int r = wave * (BT / 4) + i * 8 + (lane >> 3);
+        piece[i & 1] = ((lane & 7) ^ ((r >> 1) & 7)) * 16;       // (the same for every second load)
+        offset[i] = (int)((r0 + r < rows ? r : rows - 1 - r0) * p.ld) + piece[i & 1];
       }
 #pragma unroll
       for (int step = 0; step < 4; ++step) at[step] = (side * (BT / 2) + c) * 128 + (((2 * step + g) ^ ((c >> 1) & 7)) << 4);
     }
   }
   __device__ __forceinline__ void load(int i, unsigned slab, int wave) const {
-    const unsigned most = 0xffffffffu;
-    to_lds(base, offset[i], along, KS && room < (long long)most ? (unsigned)room : most, slab + (wave * NL + i) * 1024);
+    // (rows along k: offsets stay below 2^31 - 2^16, see wide_sizes; a piece behind the row's end is asked for from further on.  Tiles of
+    // 256 have whole slabs only: these two instructions for a load cost them 2 %)
+    const unsigned most = KS ? 0xffffffffu : 0x7fff0000u;
+    const int from = KS || BT == 256 || along + piece[i & 1] < row ? offset[i] : 0x7ffffff0;
+    to_lds(base, from, along, KS && room < (long long)most ? (unsigned)room : most, slab + (wave * NL + i) * 1024);
   }
   __device__ __forceinline__ void next(const Plane& p) {
     if (KS) { base += KSLAB * p.ld; room -= KSLAB * p.ld; }
@@ -1257,10 +1263,13 @@ inline bool on_bf16(const Product& q) {                         // of a product 
 }
 inline int bf16_parts(int type, const void* factors) { return type ? (factors ? 2 : 1) : 3; }
 inline int slab_of(bool bf16) { return bf16 ? 64 : 32; }
-inline bool in_place(const Operand& o, bool bf16, long long Kc) {
+// Rows along k need whole 16-byte pieces, and whole slabs where 256 x 256 tiles read them: a product with few of those takes smaller ones
+// and its operands as they are (us with a copy / so: 181 x 1100 x 6311 float 52 / 41, 2000 x 1000 x 1000 bf16 18.6 / 12.6).
+inline bool few_tiles(const Product& q) { return (q.I + 255) / 256 * ((q.J + 255) / 256) < 128; }
+inline bool whole_slabs(const Operand& o, bool bf16) { return o.kslow || o.ld % slab_of(bf16) == 0; }
+inline bool in_place(const Operand& o, bool bf16, long long Kc, bool any_pieces) {
   if (o.f || (o.type != 0) != bf16) return false;
-  if (o.kslow) return o.ld % (bf16 ? 8 : 4) == 0;
-  return o.ld % slab_of(bf16) == 0 && (o.ld == Kc || o.padded);
+  return o.ld % (bf16 ? 8 : 4) == 0 && (o.kslow || ((any_pieces || whole_slabs(o, bf16)) && (o.ld == Kc || o.padded)));
 }
 // The launch that lays out, as it comes together, and what it takes of the workspace
 struct Layout {
@@ -1276,8 +1285,8 @@ struct Layout {
     blocks += ((out ? ldo : K) + 255) / 256 * ((rows + span - 1) / span);
   }
   // the operand itself, or its plane in the workspace
-  Operand plane(const Operand& o, bool bf16, long long rows, long long Kc) {
-    if (in_place(o, bf16, Kc)) return o;
+  Operand plane(const Operand& o, bool bf16, long long rows, long long Kc, bool any_pieces) {
+    if (in_place(o, bf16, Kc, any_pieces)) return o;
     // (row length: whole slabs along k; with k slow whole 16-byte pieces, of which 8 entries are some)
     const long long m = o.kslow ? 8 : slab_of(bf16), r = o.kslow ? Kc : rows, k = o.kslow ? rows : Kc, ld = (k + m - 1) / m * m;
     Operand n = {};
@@ -1315,7 +1324,7 @@ WidePlan wide_plan(const Product& q) {
   w.slabs = (int)((q.Kc + slab_of(w.bf16) - 1) / slab_of(w.bf16));
   const int total = w.slabs * w.passes;
   double best = 0.0;
-  for (int bt = 256; bt >= 64; bt /= 2) {
+  for (int bt = whole_slabs(q.A, w.bf16) && whole_slabs(q.B, w.bf16) ? 256 : 128; bt >= 64; bt /= 2) {
     const long long tiles = (q.I + bt - 1) / bt * ((q.J + bt - 1) / bt);
     const double slab = w.bf16 ? (bt == 256 ? 1.6 : bt == 128 ? 0.55 : 0.2) : (bt == 256 ? 7.2 : bt == 128 ? 1.9 : 0.55), ends = bt == 256 ? 6.0 : bt == 128 ? 3.0 : 2.0;
     for (int parts = 1; parts <= 32 && (parts == 1 || (2 * parts <= total && tiles * parts <= 2048)); ++parts) {
@@ -1358,13 +1367,14 @@ hipError_t launch_wide_out(const WideArgs& a, bool as, bool bs, int parts, hipSt
 // Both operands are planes of the same type
 bool ready(const Product& q) {
   const bool bf16 = q.A.type != 0;
-  return q.B.type == q.A.type && in_place(q.A, bf16, q.Kc) && in_place(q.B, bf16, q.Kc);
+  return q.B.type == q.A.type && in_place(q.A, bf16, q.Kc, true) && in_place(q.B, bf16, q.Kc, true);
 }
 WideArgs wide_args(const Product& q, const WidePlan& w, void* partial) {
   const long long es = w.bf16 ? 2 : 4;
   WideArgs a = {};
-  a.A = Plane{static_cast<const char*>(q.A.p), q.A.ld * es, q.A.part * es};
-  a.B = Plane{static_cast<const char*>(q.B.p), q.B.ld * es, q.B.part * es};
+  auto plane = [&](const Operand& o) { return Plane{static_cast<const char*>(o.p), o.ld * es, o.part * es, o.kslow ? 0 : (int)(o.ld * es)}; };
+  a.A = plane(q.A);
+  a.B = plane(q.B);
   a.e = q.e;
   a.I = q.I; a.J = q.J; a.Kc = q.Kc;
   a.slabs = w.slabs;
@@ -1461,8 +1471,8 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
   bool summed = !b.db;
   Operand G[2] = {};                  // [bf16]
   for (int bf16 = 0; bf16 < 2; ++bf16) {
-    const bool for_x = x && x_bf16 == (bf16 != 0) && !in_place(p.x.A, bf16, p.x.Kc);
-    const bool for_w = w && w_bf16 == (bf16 != 0) && !in_place(p.w.A, bf16, p.w.Kc);
+    const bool for_x = x && x_bf16 == (bf16 != 0) && !in_place(p.x.A, bf16, p.x.Kc, few_tiles(p.x));
+    const bool for_w = w && w_bf16 == (bf16 != 0) && !in_place(p.w.A, bf16, p.w.Kc, few_tiles(p.w));
     if (!for_x && !for_w) continue;
     Operand& g = G[bf16];
     const int m = slab_of(bf16);
@@ -1476,8 +1486,8 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
     if (for_w) { p.w.A = g; p.w.A.kslow = 1; }
   }
   if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums);
-  if (x) p.x.B = p.lay.plane(p.x.B, x_bf16, p.x.J, p.x.Kc);
-  if (w) p.w.B = p.lay.plane(p.w.B, w_bf16, p.w.J, p.w.Kc);
+  if (x) p.x.B = p.lay.plane(p.x.B, x_bf16, p.x.J, p.x.Kc, few_tiles(p.x));
+  if (w) p.w.B = p.lay.plane(p.w.B, w_bf16, p.w.J, p.w.Kc, few_tiles(p.w));
   p.pair = x && w && pairs(p.w, p.x);
   const size_t nx = b.dX ? up(parts_workspace(p.x)) : 0, nw = b.dW ? up(parts_workspace(p.w)) : 0;
   p.partial_x = base + p.lay.bytes;
@@ -1563,8 +1573,8 @@ size_t product_workspace(const Product& q) {
   Layout l = {};
   Product p = q;
   const bool bf16 = on_bf16(q);
-  p.A = l.plane(q.A, bf16, q.I, q.Kc);
-  p.B = l.plane(q.B, bf16, q.J, q.Kc);
+  p.A = l.plane(q.A, bf16, q.I, q.Kc, few_tiles(q));
+  p.B = l.plane(q.B, bf16, q.J, q.Kc, few_tiles(q));
   return l.bytes + parts_workspace(p);
 }
 
@@ -1579,8 +1589,8 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
   l.base = static_cast<char*>(ws);
   Product p = q;
   const bool bf16 = on_bf16(q);
-  p.A = l.plane(q.A, bf16, q.I, q.Kc);
-  p.B = l.plane(q.B, bf16, q.J, q.Kc);
+  p.A = l.plane(q.A, bf16, q.I, q.Kc, few_tiles(q));
+  p.B = l.plane(q.B, bf16, q.J, q.Kc, few_tiles(q));
   const hipError_t e = l.launch(s);
   return e != hipSuccess ? e : launch_wide_product(p, l.base + l.bytes, s);
 }
