@@ -74,7 +74,7 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const T* logits, const in
   if (label < 0) {
     if (rows && t == 0) rows[row] = 0.0f;
     if (g)
-      for (int v = t; v < V; v += TH) g[v] = T(0.0f);
+      for (long long v = t; v < V; v += TH) g[v] = T(0.0f);             // (V + TH may pass 31 bits)
     return;
   }
   // entries before the first whole vector, whole vectors, entries behind

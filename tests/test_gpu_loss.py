@@ -1,4 +1,6 @@
 """Cross-entropy with its gradient (mgrit_cross_entropy) against 64-bit formulas."""
+import math
+
 import pytest
 import torch
 
@@ -192,3 +194,24 @@ def test_nothing_is_written_past_the_outputs():
         rows = torch.full((B + 64,), 7.0, device="cuda")
         M.mgrit_cross_entropy(a.p, a.x, a.labels, None, rows[:B], whole[4096:4096 + B * V].view(B, V), a.ws)
         assert bool((whole[:4096] == 7.0).all()) and bool((whole[4096 + B * V:] == 7.0).all()) and bool((rows[B:] == 7.0).all())
+
+
+def test_the_largest_number_of_classes():
+    """2^31 - 1 classes: a row that does not count is zeroed to its end and no further, the row behind it is right."""
+    V = 2 ** 31 - 1
+    p = M.make_loss(B=2, V=V, dtype=M.MGRIT_BF16, reduction=M.MGRIT_LOSS_SUM)
+    ws = torch.empty(M.mgrit_cross_entropy_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    whole = torch.zeros(2 * V + 4096, dtype=torch.bfloat16, device="cuda")
+    whole[:V] = 3.0
+    whole[2 * V:] = 7.0
+    x, labels, rows = whole[:2 * V].view(2, V), torch.tensor([-1, V - 1], device="cuda"), torch.full((2,), float("nan"), device="cuda")
+    M.mgrit_cross_entropy(p, x, labels, None, rows, x, ws)
+    assert bool((whole[2 * V:] == 7.0).all()) and float(rows[0]) == 0.0
+    # the row behind: log V (2 steps for the logarithm and its product with log 2), 1 / V, and 1 / V - 1 at the label
+    assert abs(float(rows[1]) - math.log(V)) <= 2.0 ** -22 * math.log(V)
+    third = 1 << 30
+    for a in range(0, V, third):
+        assert not x[0, a:a + third].any()
+        part = x[1, a:min(a + third, V - 1)]
+        assert abs(float(part.min()) * V - 1.0) <= 2.0 ** -8 * 1.001 and abs(float(part.max()) * V - 1.0) <= 2.0 ** -8 * 1.001
+    assert float(x[1, V - 1]) == -1.0
