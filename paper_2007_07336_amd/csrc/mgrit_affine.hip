@@ -709,7 +709,7 @@ constexpr int THIN_ROWS = 256;
 
 template <typename TS, typename TT, typename TY, int NT>
 __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
-  __shared__ float G[THIN_ROWS][NT];
+  __shared__ float G[THIN_ROWS + 1][NT];         // the last row: zeros for rows behind the chunk's (x is zero there, another row's G may be infinite)
   __shared__ floatx4 half[2][NT][64];
   const long long blocks = (a.K + 255) / 256;
   const long long L = logical_block(), c = L / blocks, r0 = c * a.chunk;
@@ -734,6 +734,7 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
     }
     G[r][e] = v;
   }
+  if (t < NT) G[THIN_ROWS][t] = 0.0f;
   floatx4 w[NT], s[NT];
 #pragma unroll
   for (int e = 0; e < NT; ++e) {
@@ -745,7 +746,7 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool in = r + 4 * u < n;
-      const float* q = G[in ? r + 4 * u : 0];          // (x is zero behind the last row)
+      const float* q = G[in ? r + 4 * u : THIN_ROWS];
       if (a.outS && in) {
         floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll

@@ -275,3 +275,17 @@ def test_sizes_around_the_tiles(types):
             _, D = a.check_forward(factor=True)
             a.check_backward(D)
     Affine(16 * 256 + 1, 64, 16 * 256 - 1, types, "relu", residual=True).check_forward()
+
+
+@pytest.mark.parametrize("types", ["fff", "bbb", "fbf"])
+@pytest.mark.parametrize("M_,K,F,at", [(20, 40, 10, (0, 3)), (70, 300, 10, (64, 9)), (1000, 33, 3, (0, 0)), (5, 40, 50, (2, 0)), (3, 700, 333, (0, 32)),
+                                       (1, 9, 17, (0, 0)), (300, 20, 16, (288, 15))])
+def test_an_infinite_gradient_in_the_first_row_of_a_chunk(M_, K, F, at, types):
+    """Thin gradients: rows behind a chunk's last one take no part, so an infinity stays one where the formula has it."""
+    a = Affine(M_, K, F, types)
+    a.dY[at] = float("inf")
+    dX, dW, db = a.backward(None)
+    for got, want in ((dX, a.dY.double() @ a.W.double()), (dW, a.dY.double().T @ a.X.double()), (db, a.dY.double().sum(0))):
+        assert torch.isinf(want).any()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+        assert torch.equal(got[torch.isinf(want)].double(), want[torch.isinf(want)])
