@@ -49,6 +49,9 @@ template <typename T> __device__ __forceinline__ void keep_packed(Vec<T>& a) {
   asm volatile("" : "+v"(u));
   a = __builtin_bit_cast(Vec<T>, u);
 }
+// A row's loss.  The maximum less the label's logit first: the sum's logarithm, at most log V, added to the maximum alone would be rounded to
+// that one's size (logits near 1000: 6e-5).
+__device__ __forceinline__ float loss_of(Running r, float asked) { return (r.m - asked) + __builtin_amdgcn_logf(r.s) * LN2; }
 // What the row's results are made of: f times exp(x - m) is the gradient apart from the label's
 struct Row {
   float m, s, w, f;
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const T* logits, const in
   }
   r = join_threads<TH>(r, sh);
   if (r.s == 0.0f || !good) r.s = NAN;
-  if (rows && t == 0) rows[row] = good ? r.m + __builtin_amdgcn_logf(r.s) * LN2 - asked : NAN;
+  if (rows && t == 0) rows[row] = good ? loss_of(r, asked) : NAN;
   if (!g) return;
   const float w = counted ? scale / (float)*counted : scale;
   const Row o = {r.m, r.s, w, w / r.s};
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(1024) void loss_short_kernel(const T* logits, const
 #pragma unroll
     for (int d = L / 2; d; d >>= 1) r = join(r, Running{__shfl_xor(r.m, d), __shfl_xor(r.s, d)});
     if (r.s == 0.0f || !good) r.s = NAN;
-    const float lr = label < 0 ? 0.0f : good ? r.m + __builtin_amdgcn_logf(r.s) * LN2 - asked : NAN;
+    const float lr = label < 0 ? 0.0f : good ? loss_of(r, asked) : NAN;
     if (rows && l == 0) rows[row] = lr;
     total += l == 0 ? (double)lr : 0.0;
     if (grad) {

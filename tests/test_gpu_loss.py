@@ -215,3 +215,31 @@ def test_the_largest_number_of_classes():
         part = x[1, a:min(a + third, V - 1)]
         assert abs(float(part.min()) * V - 1.0) <= 2.0 ** -8 * 1.001 and abs(float(part.max()) * V - 1.0) <= 2.0 ** -8 * 1.001
     assert float(x[1, V - 1]) == -1.0
+
+
+@pytest.mark.parametrize("t", ["f", "b"])
+@pytest.mark.parametrize("V", [1, 10, 300, 3001, 20000, 70001])
+@pytest.mark.parametrize("offset", [1e3, -1e4, 2.0 ** 25, 3e38, "lowest"])
+def test_losses_do_not_depend_on_a_common_offset(offset, V, t):
+    """Logits far from zero: the loss is as exact as that of the differences to the row's maximum, which are exact here or nearly so.
+    A row of equal classes has log V, whatever they are."""
+    a = Loss(6, V, t, mean=False, scale=0.5)
+    c = float(torch.finfo(TYPES[t]).min) if offset == "lowest" else offset
+    a.x.copy_(a.x.double() + c if offset != "lowest" else torch.full_like(a.x, c))
+    a.x[1] = c
+    a.x[2, V // 2:] = -INF
+    a.x[2, 0] = c
+    a.labels[2] = 0
+    x, at = a.x.double(), a.labels[:, None]
+    m = x.max(1, keepdim=True).values
+    d = m - x
+    e = torch.exp(-d)
+    s = e.sum(1)
+    below = (m - x.gather(1, at))[:, 0]
+    want = torch.log(s) + below
+    # terms of the sum as in Loss.exact, the logarithm and its product with log 2, the difference to the label and the last addition
+    bound = (e * (d.nan_to_num(0.0, 0.0, 0.0) + 2.0)).sum(1) / s * 2.0 ** -23 + V * 2.0 ** -24 + 2.0 ** -22 * (torch.log(s) + below)
+    loss, rows, _ = a.call()
+    near(rows, want, bound + TINY, "rows")
+    near(loss, 0.5 * want.sum().reshape(1), 0.5 * bound.sum() + 2.0 ** -23 * want.sum() + TINY, "loss")
+    assert abs(float(rows[1]) - math.log(V)) <= (V * 2.0 ** -24 + 2.0 ** -22 * math.log(V)) + TINY
