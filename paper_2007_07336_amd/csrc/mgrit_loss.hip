@@ -288,7 +288,7 @@ hipError_t launch_loss(const LossArgs& a, void* ws, hipStream_t s) {
   float* rows = a.rows ? a.rows : a.loss ? reinterpret_cast<float*>(static_cast<char*>(ws) + 256) : nullptr;
   if (counted && (a.loss || a.grad)) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, a.labels, a.B, counted);
   hipError_t e = hipSuccess;
-  if (rows || a.grad) {
+  if (a.B > 0 && (rows || a.grad)) {            // (no launch of no workgroups: that is an error)
     if (a.V <= 1024) e = a.dtype ? launch_short<__bf16>(a, rows, counted, false, s) : launch_short<float>(a, rows, counted, false, s);
     else e = a.dtype ? launch_rows<__bf16>(a, rows, counted, s) : launch_rows<float>(a, rows, counted, s);
   }

@@ -243,3 +243,14 @@ def test_losses_do_not_depend_on_a_common_offset(offset, V, t):
     near(rows, want, bound + TINY, "rows")
     near(loss, 0.5 * want.sum().reshape(1), 0.5 * bound.sum() + 2.0 ** -23 * want.sum() + TINY, "loss")
     assert abs(float(rows[1]) - math.log(V)) <= (V * 2.0 ** -24 + 2.0 ** -22 * math.log(V)) + TINY
+
+
+@pytest.mark.parametrize("t", ["f", "b"])
+@pytest.mark.parametrize("V", [1, 1024, 1025, 5000, 70000])
+@pytest.mark.parametrize("mean", [True, False])
+def test_no_rows_of_many_classes(mean, V, t):
+    a = Loss(0, V, t, mean=mean)
+    loss = torch.full((1,), 5.0, device="cuda")
+    M.mgrit_cross_entropy(a.p, a.x, a.labels, loss, torch.empty((0,), device="cuda"), torch.empty_like(a.x), a.ws)
+    assert float(loss) == 0.0
+    M.mgrit_cross_entropy(a.p, a.x, a.labels, None, None, torch.empty_like(a.x), a.ws)
