@@ -264,15 +264,22 @@ hipError_t launch_rows(const LossArgs& a, float* rows, const int* counted, hipSt
   const T* x = static_cast<const T*>(a.logits);
   T* g = static_cast<T*>(a.grad);
   const long long vectors = a.V / Vec<T>::N;
-#define LONG_ROWS(TH, NV) hipLaunchKernelGGL((loss_rows_kernel<T, TH, NV>), dim3((unsigned)a.B), dim3(TH), 0, s, x, a.labels, rows, g, a.V, a.scale, counted)
-  if (vectors <= 256) LONG_ROWS(256, 1);
-  else if (vectors <= 512) LONG_ROWS(256, 2);
-  else if (vectors <= 1024) LONG_ROWS(256, 4);
-  else if (vectors <= 2048) LONG_ROWS(512, 4);
-  else if (vectors <= 4096) LONG_ROWS(1024, 4);
-  else if (vectors <= 8192) LONG_ROWS(1024, 8);
-  else LONG_ROWS(1024, 0);
+  // a launch has fewer than 2^32 threads; 2^21 rows begin a multiple of 16 bytes further, as the kernel expects of its arrays
+  for (long long r0 = 0; r0 < a.B; r0 += 1LL << 21) {
+    const unsigned n = (unsigned)(a.B - r0 < 1LL << 21 ? a.B - r0 : 1LL << 21);
+    const T* xr = x + r0 * a.V;
+    T* gr = g ? g + r0 * a.V : nullptr;
+    float* rr = rows ? rows + r0 : nullptr;
+#define LONG_ROWS(TH, NV) hipLaunchKernelGGL((loss_rows_kernel<T, TH, NV>), dim3(n), dim3(TH), 0, s, xr, a.labels + r0, rr, gr, a.V, a.scale, counted)
+    if (vectors <= 256) LONG_ROWS(256, 1);
+    else if (vectors <= 512) LONG_ROWS(256, 2);
+    else if (vectors <= 1024) LONG_ROWS(256, 4);
+    else if (vectors <= 2048) LONG_ROWS(512, 4);
+    else if (vectors <= 4096) LONG_ROWS(1024, 4);
+    else if (vectors <= 8192) LONG_ROWS(1024, 8);
+    else LONG_ROWS(1024, 0);
 #undef LONG_ROWS
+  }
   return hipGetLastError();
 }
 
@@ -288,7 +295,7 @@ hipError_t launch_loss(const LossArgs& a, void* ws, hipStream_t s) {
   float* rows = a.rows ? a.rows : a.loss ? reinterpret_cast<float*>(static_cast<char*>(ws) + 256) : nullptr;
   if (counted && (a.loss || a.grad)) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, a.labels, a.B, counted);
   hipError_t e = hipSuccess;
-  if (a.B > 0 && (rows || a.grad)) {            // (no launch of no workgroups: that is an error)
+  if (a.B > 0 && (rows || a.grad)) {            // (a launch of no workgroups is an error)
     if (a.V <= 1024) e = a.dtype ? launch_short<__bf16>(a, rows, counted, false, s) : launch_short<float>(a, rows, counted, false, s);
     else e = a.dtype ? launch_rows<__bf16>(a, rows, counted, s) : launch_rows<float>(a, rows, counted, s);
   }

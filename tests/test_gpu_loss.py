@@ -254,3 +254,29 @@ def test_no_rows_of_many_classes(mean, V, t):
     M.mgrit_cross_entropy(a.p, a.x, a.labels, loss, torch.empty((0,), device="cuda"), torch.empty_like(a.x), a.ws)
     assert float(loss) == 0.0
     M.mgrit_cross_entropy(a.p, a.x, a.labels, None, None, torch.empty_like(a.x), a.ws)
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    """2^24 + 5 rows of 1025 classes are more than 2^32 threads; the rows repeat, so that a small call has all results."""
+    B, V, n = (1 << 24) + 5, 1025, 1 << 14
+    few = Loss(n, V, "b", mean=False, scale=0.25)
+    few.labels[::7] = -1
+    _, want_rows, want = few.call()
+    p = M.make_loss(B=B, V=V, dtype=M.MGRIT_BF16, reduction=M.MGRIT_LOSS_SUM, scale=0.25)
+    x, labels = torch.empty((B, V), dtype=torch.bfloat16, device="cuda"), torch.empty((B,), dtype=torch.int64, device="cuda")
+    for a in range(0, B, n):
+        k = min(n, B - a)
+        x[a:a + k], labels[a:a + k] = few.x[:k], few.labels[:k]
+    loss, rows = torch.full((1,), float("nan"), device="cuda"), torch.full((B,), float("nan"), device="cuda")
+    ws = torch.empty(M.mgrit_cross_entropy_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    M.mgrit_cross_entropy(p, x, labels, loss, rows, x, ws)
+    total, same = 0.0, torch.ones((), dtype=torch.bool, device="cuda")
+    for a in range(0, B, n):
+        k = min(n, B - a)
+        same &= (x[a:a + k] == want[:k]).all() & (rows[a:a + k] == want_rows[:k]).all()
+        total += 1 if k == n else 0
+    assert bool(same)
+    total = 0.25 * (total * float(want_rows.double().sum()) + float(want_rows[:5].double().sum()))
+    assert abs(float(loss) - total) <= 2.0 ** -23 * abs(total)
+    del x, labels, rows, ws
+    torch.cuda.empty_cache()
