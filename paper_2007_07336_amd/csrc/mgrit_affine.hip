@@ -446,9 +446,9 @@ template <typename TS, typename TF, int SB, int FB> struct FewShape {
   static_assert(D >= 2, "two slabs in turn");
 };
 
-// SWAP: the stream is A (out's rows), the few are B (out's columns); otherwise the other way round.
+// first: workgroups of the launches before.  SWAP: the stream is A (out's rows), the few are B (out's columns); otherwise the other way round.
 template <typename TS, typename TF, typename CT, int SB, int FB, bool SWAP>
-__global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_few_kernel(Product q, long long kpart, float* partial, int slabs_in_lds) {
+__global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_few_kernel(Product q, long long kpart, float* partial, int slabs_in_lds, int first) {
   typedef FewShape<TS, TF, SB, FB> Sh;
   constexpr int NS = SB * 16, NF = FB * 16, PITCH = SWAP ? NF + 1 : NS + 4, U = FB >= 4 ? 1 : 2, FEW_WAVES = Sh::W;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -456,7 +456,7 @@ __global__ __launch_bounds__((64 * FewShape<TS, TF, SB, FB>::W)) void product_fe
   constexpr int SUMS = (SWAP ? NS : NF) * PITCH;                               // of one wavefront
   static_assert(FEW_WAVES * SUMS * 4 <= Sh::W * Sh::SLAB * Sh::D, "the sums take the slabs' place");
   const Operand &so = SWAP ? q.A : q.B, &fo = SWAP ? q.B : q.A;
-  const long long ns = SWAP ? q.I : q.J, nf = SWAP ? q.J : q.I, s0 = (long long)logical_block() * NS;
+  const long long ns = SWAP ? q.I : q.J, nf = SWAP ? q.J : q.I, s0 = ((long long)first + logical_block()) * NS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, k8 = (lane >> 4) * 8;
   const long long p0 = blockIdx.y * kpart, p1 = p0 + kpart < q.Kc ? p0 + kpart : q.Kc;
   const long long kw = ((p1 - p0 + FEW_WAVES - 1) / FEW_WAVES + 31) / 32 * 32;
@@ -638,8 +638,11 @@ hipError_t launch_few_kernel(const Product& q, const FewPlan& p, float* partial,
   // (16-byte pieces of rows; offsets within the few's 64 rows and along a row are 31 bits)
   const Operand &so = SWAP ? q.A : q.B, &fo = SWAP ? q.B : q.A;
   const int in_lds = so.ld * sizeof(TS) % 16 == 0 && fo.ld * sizeof(TF) % 16 == 0 && q.Kc <= (1LL << 22);
-  hipLaunchKernelGGL((product_few_kernel<TS, TF, CT, SB, FB, SWAP>), dim3((unsigned)((many + 16 * SB - 1) / (16 * SB)), (unsigned)p.parts), dim3(64 * Sh::W),
-                     smem, s, q, p.kpart, p.parts > 1 ? partial : nullptr, in_lds);
+  // (a launch has fewer than 2^32 threads)
+  const long long blocks = (many + 16 * SB - 1) / (16 * SB), most = 1LL << 22;
+  for (long long b = 0; b < blocks; b += most)
+    hipLaunchKernelGGL((product_few_kernel<TS, TF, CT, SB, FB, SWAP>), dim3((unsigned)(blocks - b < most ? blocks - b : most), (unsigned)p.parts), dim3(64 * Sh::W),
+                       smem, s, q, p.kpart, p.parts > 1 ? partial : nullptr, in_lds, (int)b);
   return hipGetLastError();
 }
 template <typename TS, typename TF, typename CT, int SB, int FB>

@@ -289,3 +289,22 @@ def test_an_infinite_gradient_in_the_first_row_of_a_chunk(M_, K, F, at, types):
         assert torch.isinf(want).any()
         assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
         assert torch.equal(got[torch.isinf(want)].double(), want[torch.isinf(want)])
+
+
+@pytest.mark.parametrize("many_rows", [True, False])
+def test_more_few_rows_workgroups_than_a_launch_has_threads_for(many_rows):
+    """2^29 + 5 rows, or columns, of one term each: a product of two bf16 values is exact in float, with the bias it is rounded once."""
+    n = (1 << 29) + 5
+    v = normal((1 << 14,), 1.0, "b", 1)
+    long = torch.empty((n, 1), dtype=torch.bfloat16, device="cuda")
+    whole = n // (1 << 14) * (1 << 14)
+    long[:whole].view(-1, 1 << 14).copy_(v.expand(whole >> 14, 1 << 14))
+    long[whole:, 0] = v[:n - whole]
+    one = torch.full((1, 1), 1.625, dtype=torch.bfloat16, device="cuda")
+    Y = torch.full((n, 1) if many_rows else (1, n), float("nan"), device="cuda")
+    p = M.make_affine(M=n if many_rows else 1, K=1, F=1 if many_rows else n, xtype=1, wtype=1)
+    assert M.mgrit_affine_workspace_bytes(p) == 0
+    M.mgrit_affine_forward(p, *((long, one) if many_rows else (one, long)), None, None, Y, None, None)
+    want = v.float() * 1.625
+    flat = Y.view(-1)
+    assert bool((flat[:whole].view(-1, 1 << 14) == want).all()) and torch.equal(flat[whole:], want[:n - whole])
