@@ -7,6 +7,10 @@ namespace mgrit {
 
 namespace {
 
+// Workgroups of one launch along x where there may be more than any launch takes: it has fewer than 2^32 threads, and what is beyond
+// is dropped without an error
+constexpr long long MOST_BLOCKS = 1LL << 22;
+
 // ------------------------------------------------------------------------------------------ values
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(__bf16 v) { return static_cast<float>(v); }
@@ -267,14 +271,13 @@ __device__ __forceinline__ void multiply_slab(const __bf16* As, const __bf16* Bs
   }
 }
 
-// blockIdx.x: tile; blockIdx.y: part of the contraction (kpart long).  One part: the epilogue here; more: sums to
+// blockIdx.x: tile, behind `first` of the launches before; blockIdx.y: part of the contraction (kpart long).  One part: the epilogue here; more: sums to
 // partial[part][i][j].
 template <typename TA, typename TB, typename CT, bool HF, bool AS, bool BS>
-__global__ __launch_bounds__(256) void product_tile_kernel(Product q, long long kpart, float* partial) {
+__global__ __launch_bounds__(256) void product_tile_kernel(Product q, long long kpart, float* partial, int first) {
   __shared__ __attribute__((aligned(16))) CT As[GT * Slab<CT>::ST], Bs[GT * Slab<CT>::ST];
   const long long tj = (q.J + GT - 1) / GT;
-  const int L = logical_block();
-  const long long i0 = L / tj * GT, j0 = L % tj * GT;
+  const long long L = (long long)first + logical_block(), i0 = L / tj * GT, j0 = L % tj * GT;
   const long long k0 = blockIdx.y * kpart, kend = k0 + kpart < q.Kc ? k0 + kpart : q.Kc;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave >> 1, wj = wave & 1;
   Loader<TA, CT, HF, AS> la;
@@ -351,8 +354,10 @@ template <typename TA, typename TB, typename CT, bool HF, bool AS, bool BS>
 hipError_t launch_tiles(const Product& q, float* partial, int parts, hipStream_t s) {
   constexpr int BK = Slab<CT>::BK;
   const long long kpart = ((q.Kc + parts - 1) / parts + BK - 1) / BK * BK;
-  hipLaunchKernelGGL((product_tile_kernel<TA, TB, CT, HF, AS, BS>), dim3((unsigned)tiles_of(q), (unsigned)parts), dim3(256), 0, s, q,
-                     kpart, parts > 1 ? partial : nullptr);
+  const long long tiles = tiles_of(q);
+  for (long long b = 0; b < tiles; b += MOST_BLOCKS)
+    hipLaunchKernelGGL((product_tile_kernel<TA, TB, CT, HF, AS, BS>), dim3((unsigned)(tiles - b < MOST_BLOCKS ? tiles - b : MOST_BLOCKS), (unsigned)parts), dim3(256),
+                       0, s, q, kpart, parts > 1 ? partial : nullptr, (int)b);
   return hipGetLastError();
 }
 template <bool HF, bool AS, bool BS>
@@ -638,11 +643,10 @@ hipError_t launch_few_kernel(const Product& q, const FewPlan& p, float* partial,
   // (16-byte pieces of rows; offsets within the few's 64 rows and along a row are 31 bits)
   const Operand &so = SWAP ? q.A : q.B, &fo = SWAP ? q.B : q.A;
   const int in_lds = so.ld * sizeof(TS) % 16 == 0 && fo.ld * sizeof(TF) % 16 == 0 && q.Kc <= (1LL << 22);
-  // (a launch has fewer than 2^32 threads)
-  const long long blocks = (many + 16 * SB - 1) / (16 * SB), most = 1LL << 22;
-  for (long long b = 0; b < blocks; b += most)
-    hipLaunchKernelGGL((product_few_kernel<TS, TF, CT, SB, FB, SWAP>), dim3((unsigned)(blocks - b < most ? blocks - b : most), (unsigned)p.parts), dim3(64 * Sh::W),
-                       smem, s, q, p.kpart, p.parts > 1 ? partial : nullptr, in_lds, (int)b);
+  const long long blocks = (many + 16 * SB - 1) / (16 * SB);
+  for (long long b = 0; b < blocks; b += MOST_BLOCKS)
+    hipLaunchKernelGGL((product_few_kernel<TS, TF, CT, SB, FB, SWAP>), dim3((unsigned)(blocks - b < MOST_BLOCKS ? blocks - b : MOST_BLOCKS), (unsigned)p.parts),
+                       dim3(64 * Sh::W), smem, s, q, p.kpart, p.parts > 1 ? partial : nullptr, in_lds, (int)b);
   return hipGetLastError();
 }
 template <typename TS, typename TF, typename CT, int SB, int FB>
@@ -1145,10 +1149,10 @@ struct LayJob {
 };
 struct LayJobs { LayJob j[4]; int n; };
 template <typename T, typename CT, int PARTS, bool HF>
-__device__ __forceinline__ void lay_out(const LayJob& a, float (&sh)[8][256]) {
+__device__ __forceinline__ void lay_out(const LayJob& a, unsigned block, float (&sh)[8][256]) {
   const T *p = static_cast<const T*>(a.p), *f = static_cast<const T*>(a.f);
   CT* out = static_cast<CT*>(a.out);
-  const long long K = a.K, ldo = a.ldo, tiles = ((PARTS ? ldo : K) + 255) / 256, L = blockIdx.x - a.first, chunk = L / tiles;
+  const long long K = a.K, ldo = a.ldo, tiles = ((PARTS ? ldo : K) + 255) / 256, L = block - a.first, chunk = L / tiles;
   const int t = threadIdx.x;
   const long long k = L % tiles * 256 + t % 32 * 8, r0 = chunk * a.span, r1 = r0 + a.span < a.rows ? r0 + a.span : a.rows;
   const long long left = K - k;
@@ -1200,40 +1204,50 @@ __device__ __forceinline__ void lay_out(const LayJob& a, float (&sh)[8][256]) {
   for (int i = 1; i < 8; ++i) x += sh[i][t];
   a.sums[chunk * K + col] = a.scale * x;
 }
-__global__ __launch_bounds__(256) void lay_out_kernel(LayJobs jobs) {
+__global__ __launch_bounds__(256) void lay_out_kernel(LayJobs jobs, unsigned before) {
   __shared__ float sh[8][256];
+  const unsigned block = before + blockIdx.x;    // of all launches
   int i = 0;
-  while (i + 1 < jobs.n && blockIdx.x >= jobs.j[i + 1].first) ++i;
+  while (i + 1 < jobs.n && block >= jobs.j[i + 1].first) ++i;
   const LayJob a = jobs.j[i];
   switch (a.kind) {
-    case 0: lay_out<float, float, 1, false>(a, sh); break;
-    case 1: lay_out<__bf16, float, 1, false>(a, sh); break;
-    case 2: lay_out<float, __bf16, 3, false>(a, sh); break;
-    case 3: lay_out<__bf16, __bf16, 1, false>(a, sh); break;
-    case 4: lay_out<float, float, 1, true>(a, sh); break;
-    case 5: lay_out<__bf16, float, 1, true>(a, sh); break;
-    case 6: lay_out<float, __bf16, 3, true>(a, sh); break;
-    case 7: lay_out<__bf16, __bf16, 2, true>(a, sh); break;
-    case 8: lay_out<float, float, 0, false>(a, sh); break;
-    case 9: lay_out<__bf16, float, 0, false>(a, sh); break;
-    case 12: lay_out<float, float, 0, true>(a, sh); break;
-    case 13: lay_out<__bf16, float, 0, true>(a, sh); break;
+    case 0: lay_out<float, float, 1, false>(a, block, sh); break;
+    case 1: lay_out<__bf16, float, 1, false>(a, block, sh); break;
+    case 2: lay_out<float, __bf16, 3, false>(a, block, sh); break;
+    case 3: lay_out<__bf16, __bf16, 1, false>(a, block, sh); break;
+    case 4: lay_out<float, float, 1, true>(a, block, sh); break;
+    case 5: lay_out<__bf16, float, 1, true>(a, block, sh); break;
+    case 6: lay_out<float, __bf16, 3, true>(a, block, sh); break;
+    case 7: lay_out<__bf16, __bf16, 2, true>(a, block, sh); break;
+    case 8: lay_out<float, float, 0, false>(a, block, sh); break;
+    case 9: lay_out<__bf16, float, 0, false>(a, block, sh); break;
+    case 12: lay_out<float, float, 0, true>(a, block, sh); break;
+    case 13: lay_out<__bf16, float, 0, true>(a, block, sh); break;
   }
 }
 // out[col] = sum over the chunks; 64 columns and sixteen sets of chunks per workgroup
 __global__ __launch_bounds__(1024) void add_chunks_kernel(const float* part, int chunks, long long F, float* out) {
   __shared__ float sh[16][64];
   const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
-  const long long col = blockIdx.x * 64LL + lane;
-  float s = 0.0f;
-  if (col < F)
-    for (int c = set; c < chunks; c += 16) s += part[c * F + col];
-  sh[set][lane] = s;
-  __syncthreads();
-  if (set || col >= F) return;
+  for (long long col0 = blockIdx.x * 64LL; col0 < F; col0 += gridDim.x * 64LL) {
+    const long long col = col0 + lane;
+    float s = 0.0f;
+    if (col < F)
+      for (int c = set; c < chunks; c += 16) s += part[c * F + col];
+    sh[set][lane] = s;
+    __syncthreads();
+    if (set == 0 && col < F) {
 #pragma unroll
-  for (int i = 1; i < 16; ++i) s += sh[i][lane];
-  out[col] = s;
+      for (int i = 1; i < 16; ++i) s += sh[i][lane];
+      out[col] = s;
+    }
+    __syncthreads();
+  }
+}
+hipError_t add_chunks(const float* part, int chunks, long long F, float* out, hipStream_t s) {
+  const long long blocks = (F + 63) / 64;
+  hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(1024), 0, s, part, chunks, F, out);
+  return hipGetLastError();
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(float* out, long long n) {
@@ -1301,17 +1315,19 @@ struct Layout {
     return n;
   }
   hipError_t launch(hipStream_t s) const {
-    if (jobs.n) hipLaunchKernelGGL(lay_out_kernel, dim3((unsigned)blocks), dim3(256), 0, s, jobs);
+    for (long long b = 0; b < blocks; b += MOST_BLOCKS)
+      hipLaunchKernelGGL(lay_out_kernel, dim3((unsigned)(blocks - b < MOST_BLOCKS ? blocks - b : MOST_BLOCKS)), dim3(256), 0, s, jobs, (unsigned)b);
     return hipGetLastError();
   }
 };
 
 // ---- which tiles
-// (32-bit offsets within a tile's rows, or within a slab's where k is slow)
+// (32-bit offsets within a tile's rows, or within a slab's where k is slow; tiles of 128 and their 256 threads in one launch)
+constexpr long long MOST_TILES = (1LL << 24) - 1;
 inline bool wide_sizes(const Product& q) {
   const long long most = 1LL << 20;
   return (q.A.kslow ? q.I <= 4 * most : q.Kc <= most) && (q.B.kslow ? q.J <= 4 * most : q.Kc <= most) && q.Kc <= (1LL << 30) &&
-         (q.I + 63) / 64 * ((q.J + 63) / 64) < (1LL << 30);
+         (q.I + 127) / 128 * ((q.J + 127) / 128) <= MOST_TILES;
 }
 struct WidePlan {
   bool bf16;
@@ -1330,6 +1346,7 @@ WidePlan wide_plan(const Product& q) {
   double best = 0.0;
   for (int bt = whole_slabs(q.A, w.bf16) && whole_slabs(q.B, w.bf16) ? 256 : 128; bt >= 64; bt /= 2) {
     const long long tiles = (q.I + bt - 1) / bt * ((q.J + bt - 1) / bt);
+    if (tiles > MOST_TILES) continue;
     const double slab = w.bf16 ? (bt == 256 ? 1.6 : bt == 128 ? 0.55 : 0.2) : (bt == 256 ? 7.2 : bt == 128 ? 1.9 : 0.55), ends = bt == 256 ? 6.0 : bt == 128 ? 3.0 : 2.0;
     for (int parts = 1; parts <= 32 && (parts == 1 || (2 * parts <= total && tiles * parts <= 2048)); ++parts) {
       const int per = (total + parts - 1) / parts;
@@ -1423,7 +1440,7 @@ hipError_t launch_pair_tiles(const WideArgs& w, const WideArgs& x, int parts_w, 
 bool pairs(const Product& w, const Product& x) {
   const WidePlan a = wide_plan(w), b = wide_plan(x);
   const long long tw = (w.I + a.bt - 1) / a.bt * ((w.J + a.bt - 1) / a.bt) * a.parts, tx = (x.I + b.bt - 1) / b.bt * ((x.J + b.bt - 1) / b.bt) * b.parts;
-  return a.bf16 == b.bf16 && a.bt == b.bt && a.bt <= 128 && (tw < 1024 || tx < 1024) && tw + tx < (1LL << 30);
+  return a.bf16 == b.bf16 && a.bt == b.bt && a.bt <= 128 && (tw < 1024 || tx < 1024) && tw + tx <= MOST_TILES;
 }
 hipError_t launch_wide_pair(const Product& qw, const Product& qx, char* partial_w, char* partial_x, hipStream_t s) {
   if (!ready(qw) || !ready(qx)) return hipErrorInvalidValue;
@@ -1561,10 +1578,7 @@ hipError_t launch_thin(const BackwardArgs& b, const ThinPlan& p, char* ws, hipSt
     q.I = a.nt; q.J = b.K;
     e = join_parts(q, static_cast<const float*>(a.outT), p.chunks, s);
   }
-  if (e == hipSuccess && b.db && c) {
-    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(1024), 0, s, a.sum, p.chunks, b.F, b.db);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && b.db && c) e = add_chunks(a.sum, p.chunks, b.F, b.db, s);
   return e;
 }
 
@@ -1620,10 +1634,7 @@ hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s) {
   if (t.thin) return launch_thin(b, t, static_cast<char*>(ws), s);
   const BackwardPlan p = backward_plan(b, static_cast<char*>(ws));
   hipError_t e = p.lay.launch(s);
-  if (e == hipSuccess && b.db && p.chunks > 1) {
-    hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)((b.F + 63) / 64)), dim3(1024), 0, s, p.sums, p.chunks, b.F, b.db);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && b.db && p.chunks > 1) e = add_chunks(p.sums, p.chunks, b.F, b.db, s);
   if (e != hipSuccess) return e;
   if (p.pair) return launch_wide_pair(p.w, p.x, p.partial_w, p.partial_x, s);
   if (b.dX) e = wide_sizes(p.x) ? launch_wide_product(p.x, p.partial_x, s) : launch_any_product(p.x, p.partial_x, s);

@@ -308,3 +308,25 @@ def test_more_few_rows_workgroups_than_a_launch_has_threads_for(many_rows):
     want = v.float() * 1.625
     flat = Y.view(-1)
     assert bool((flat[:whole].view(-1, 1 << 14) == want).all()) and torch.equal(flat[whole:], want[:n - whole])
+
+
+def test_more_columns_than_a_launch_has_threads_for():
+    """1.5e9 columns of G: its sums over chunks of rows, the chunks' sums and the tiles of dW are each more than 2^32 threads.  Small whole
+    numbers, so that every sum is exact; the columns repeat."""
+    rows, F, n = 17, 1_500_000_001, 1 << 14
+    g = torch.Generator().manual_seed(1)
+    v = torch.randint(-8, 9, (rows, n), generator=g).to(torch.bfloat16).cuda()
+    X = torch.randint(-8, 9, (rows, 1), generator=g).to(torch.bfloat16).cuda()
+    dY = torch.empty((rows, F), dtype=torch.bfloat16, device="cuda")
+    whole = F // n * n
+    for r in range(rows):
+        dY[r, :whole].view(-1, n).copy_(v[r].expand(whole // n, n))
+        dY[r, whole:] = v[r, :F - whole]
+    p = M.make_affine(M=rows, K=1, F=F, xtype=1, wtype=1, ytype=1)
+    ws = torch.empty(M.mgrit_affine_backward_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    dW, db = torch.full((F, 1), float("nan"), device="cuda"), torch.full((F,), float("nan"), device="cuda")
+    M.mgrit_affine_backward(p, X, None, None, dY, None, dW, db, ws)
+    for got, want in ((db, v.float().sum(0)), (dW[:, 0], (v.float() * X.float()).sum(0))):
+        assert bool((got[:whole].view(-1, n) == want).all()) and torch.equal(got[whole:], want[:F - whole])
+    del dY, ws, dW, db, got
+    torch.cuda.empty_cache()
