@@ -28,13 +28,14 @@ __device__ __forceinline__ float tanh_with_slope(float z, float* slope) {
   return a < 0.35f ? series : copysignf((1.0f - e) * r, z);
 }
 
-// v = hi + lo, both representable in bf16 if v has 16 significant bits.  What overflows by rounding is cut instead; an infinity or
-// a NaN stays in hi.
+// v = hi + lo / 256, both representable in bf16 if v has 16 significant bits.  lo is 256 times what hi leaves so that it is about as large
+// as v: what is left of small values would be below bf16's range otherwise (floats below 2^-110 lost bits).  What overflows by
+// rounding is cut instead; an infinity or a NaN stays in hi.
 __device__ __forceinline__ void split2(float v, float* hi, float* lo) {
   float h = widen(narrow<__bf16>(v));
   if (fabsf(h) == INFINITY && fabsf(v) < INFINITY) h = copysignf(0x1.fep127f, v);
   *hi = h;
-  *lo = fabsf(h) < INFINITY ? v - h : 0.0f;
+  *lo = fabsf(h) < INFINITY ? (v - h) * 256.0f : 0.0f;
 }
 
 struct Out { float y, d; };
@@ -1045,9 +1046,55 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   }
 #pragma unroll
   for (int i = 0; i < T; ++i) read(pa, pb, 0, i);
-  for (int t = t0; t < t1 - 2; ++t) multiply(yes, no);
-  if (t0 + 1 < t1) multiply(no, no);
+  // Part i of an operand is kept 256^i times as large.  Passes come in the order of their scale, the largest first, and the sums are
+  // brought to that of the next pass where it is another, at last to 1: exact, and every bit of a float arrives (4096 x 1024 x 4096 float rows
+  // on bf16 weights 107 us without, 110 so; two float operands 186 and 190).
+  int pass = t0 / a.slabs, left = a.slabs - t0 % a.slabs;         // of the slab that is multiplied, and how many of it are left
+  auto scale_of = [&](int p) { return part(a.partA, p) + part(a.partB, p); };
+  auto shrink = [&]() {
+    const float f = 0x1p-8f;
+    // Where all accumulation registers are taken the compiler moves them to vector registers at once, and that through memory; so in
+    // assembly, four at a time.  It does not see to the waits there: they stand before the first and behind the last.
+    if constexpr (T == 4) asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int k = 0; k < 16; k += 4) {
+          if constexpr (T == 4) {
+            float x0 = acc[i][j][k], x1 = acc[i][j][k + 1], x2 = acc[i][j][k + 2], x3 = acc[i][j][k + 3], y0, y1, y2, y3;
+            asm volatile("v_accvgpr_read_b32 %4, %0\n\tv_accvgpr_read_b32 %5, %1\n\tv_accvgpr_read_b32 %6, %2\n\tv_accvgpr_read_b32 %7, %3\n\t"
+                         "v_mul_f32 %4, %8, %4\n\tv_mul_f32 %5, %8, %5\n\tv_mul_f32 %6, %8, %6\n\tv_mul_f32 %7, %8, %7\n\t"
+                         "v_accvgpr_write_b32 %0, %4\n\tv_accvgpr_write_b32 %1, %5\n\tv_accvgpr_write_b32 %2, %6\n\tv_accvgpr_write_b32 %3, %7"
+                         : "+a"(x0), "+a"(x1), "+a"(x2), "+a"(x3), "=&v"(y0), "=&v"(y1), "=&v"(y2), "=&v"(y3) : "v"(f));
+            acc[i][j][k] = x0; acc[i][j][k + 1] = x1; acc[i][j][k + 2] = x2; acc[i][j][k + 3] = x3;
+          } else {
+#pragma unroll
+            for (int l = 0; l < 4; ++l) acc[i][j][k + l] *= f;
+          }
+        }
+    if constexpr (T == 4) asm volatile("s_nop 7" ::: "memory");
+  };
+  auto done = [&]() {
+    if (--left) return;
+    left = a.slabs;
+    if constexpr (sizeof(CT) == 2) {                              // (float operands have one part)
+      if (scale_of(pass + 1) < scale_of(pass)) shrink();          // (by one step: see wide_args)
+    }
+    ++pass;
+  };
+  for (int t = t0; t < t1 - 2; ++t) {
+    multiply(yes, no);
+    done();
+  }
+  if (t0 + 1 < t1) {
+    multiply(no, no);
+    done();
+  }
   multiply(no, yes);
+  const int last_scale = sizeof(CT) == 2 ? scale_of(pass) : 0;
+  const float unscale = last_scale == 0 ? 1.0f : last_scale == 1 ? 0x1p-8f : 0x1p-16f;
 
   // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands.  With B as the
   // instructions' first operand a lane has four consecutive columns of one row of every tile, which it writes at once.  Strips are
@@ -1082,7 +1129,8 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
       for (int j = 0; j < T; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<floatx4*>(strip + c * PITCH + j * 32 + 8 * q + 4 * g) = floatx4{acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
+          *reinterpret_cast<floatx4*>(strip + c * PITCH + j * 32 + 8 * q + 4 * g) =
+              floatx4{acc[m][j][4 * q] * unscale, acc[m][j][4 * q + 1] * unscale, acc[m][j][4 * q + 2] * unscale, acc[m][j][4 * q + 3] * unscale};
     }
     __builtin_amdgcn_wave_barrier();
     const float* from = strip + lr * PITCH + lc;
@@ -1136,7 +1184,8 @@ __global__ __launch_bounds__(256, wide_waves(BT)) void product_pair_kernel(WideA
 }
 
 // Operand -> planes of CT: rows x (k padded to ldo with zeros), PARTS of them: 1 as it is (or widened); 2: the product of two bf16
-// values, which has 16 significant bits, as the sum of two; 3: a float as the sum of three.  A thread has eight columns of every eighth row of a workgroup's
+// values, which has 16 significant bits, as the sum of two; 3: a float as the sum of three; part i is kept 256^i times as
+// large (the bf16 instructions take subnormal values as they are).  A thread has eight columns of every eighth row of a workgroup's
 // span x 256 entries.  With `sums` the columns' sums over the span as well (of the gradient, for the bias), and PARTS = 0 is
 // those alone.  Bound by memory: 8192 x 4096 bf16 with factors into two parts, with sums, 268 MB in 45 us.  All that a call lays out goes in one launch, one job for each array.
 struct LayJob {
@@ -1402,7 +1451,8 @@ WideArgs wide_args(const Product& q, const WidePlan& w, void* partial) {
   a.passes = w.passes;
   // A's parts each against B; of three parts each, the six pairs that make up a float product: the three that are left out are
   // at most 2^-23 of it together.  The smallest first: added to the sum of the large ones, each of them would round that once
-  // more (1024^3 float: 6.7e-7 off with the largest first, 1.8e-7 so, the float instructions 5.7e-7).
+  // more (1024^3 float: 6.7e-7 off with the largest first, 1.8e-7 so, the float instructions 5.7e-7).  The numbers of a pass's parts add
+  // up to its scale, which falls by one at a time.
   a.partA = w.passes == 6 ? 0x001120u : w.passes == 3 ? 0x012u : w.passes == 2 ? 0x01u : 0u;
   a.partB = w.passes == 6 ? 0x010102u : 0u;
   a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;

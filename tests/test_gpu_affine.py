@@ -330,3 +330,77 @@ def test_more_columns_than_a_launch_has_threads_for():
         assert bool((got[:whole].view(-1, n) == want).all()) and torch.equal(got[whole:], want[:F - whole])
     del dY, ws, dW, db, got
     torch.cuda.empty_cache()
+
+
+def _whole(shape, bits, seed):
+    """Odd whole numbers of `bits` bits, either sign, as doubles."""
+    g = torch.Generator().manual_seed(seed)
+    v = torch.randint(1 << (bits - 1), 1 << bits, shape, generator=g, dtype=torch.int64) | 1
+    return (v * (2 * torch.randint(0, 2, shape, generator=g) - 1)).double().cuda()
+
+
+def _picks(rows, cols, value, t, seed):
+    """[rows][cols] with one entry of +-value in every row, and the column it is in."""
+    g = torch.Generator().manual_seed(seed)
+    at = torch.randint(0, cols, (rows,), generator=g).cuda()
+    m = torch.zeros((rows, cols), dtype=torch.float64, device="cuda")
+    m[torch.arange(rows, device="cuda"), at] = ((2 * torch.randint(0, 2, (rows,), generator=g) - 1).double() * value).cuda()
+    return m.to(t)
+
+
+# Products in parts: every row of one operand picks a single entry of the other, whose 24 bits all have to arrive.  (float rows and bf16
+# weights are taken in parts from 1e9 multiplications on, two float operands from 6e9; tiles of 256 and 128, whole and ragged)
+PARTED = [("fbf", 1100, 1024, 1000), ("fbf", 4096, 1024, 4096), ("fff", 2200, 2100, 2301), ("fff", 4096, 1024, 2560), ("fbf", 4096, 64, 4096), ("fff", 8200, 96, 8200)]
+
+
+@pytest.mark.parametrize("exponent,lift", [(0, 0), (-126, 100), (-131, 60), (-149, 80), (-140, 127), (90, -80), (104, 0)])
+@pytest.mark.parametrize("types,rows,K,F", PARTED)
+def test_every_bit_of_a_float_operand_arrives(types, rows, K, F, exponent, lift):
+    """Entries v 2^exponent with v of 24 bits, down to the smallest normal float and up to the largest, times 2^lift."""
+    a = Affine(rows, K, F, types, bias=False)
+    v = _whole((rows, K), 24, 1) * 2.0 ** exponent
+    assert bool((v.float().double() == v).all())
+    a.X.copy_(v)
+    a.W.copy_(_picks(F, K, 2.0 ** lift, a.W.dtype, 2))
+    Y, _ = a.forward()
+    assert torch.equal(Y.double(), v @ a.W.double().T)
+    if types == "fff":                                             # the other operand, and both gradients
+        w = _whole((F, K), 24, 3) * 2.0 ** exponent
+        a.W.copy_(w)
+        a.X.copy_(_picks(rows, K, 2.0 ** lift, torch.float32, 4))
+        assert torch.equal(a.forward()[0].double(), a.X.double() @ w.T)
+        g = _whole((rows, F), 24, 5) * 2.0 ** exponent
+        a.dY.copy_(g)
+        a.W.copy_(_picks(K, F, 2.0 ** lift, torch.float32, 6).T)
+        a.X.copy_(_picks(K, rows, 2.0 ** lift, torch.float32, 7).T)
+        dX, dW, _ = a.backward(None)
+        assert torch.equal(dX.double(), g @ a.W.double()) and torch.equal(dW.double(), g.T @ a.X.double())
+
+
+@pytest.mark.parametrize("exponent,lift", [(0, 0), (-126, 100), (-140, 100), (100, -60), (111, 0)])
+@pytest.mark.parametrize("rows,K,F", [(600, 512, 520), (2048, 1024, 1024)])
+def test_every_bit_of_a_product_of_two_bf16_values_arrives(rows, K, F, exponent, lift):
+    """G = dY * D has 16 bits and goes into the products as it is."""
+    a = Affine(rows, K, F, "bbb", "tanh")
+    d = _whole((rows, F), 8, 1) * 2.0 ** -7
+    y = _whole((rows, F), 8, 2) * 2.0 ** (exponent + 7)
+    a.dY.copy_(y)
+    g = y * d
+    D = d.bfloat16()
+    assert bool((a.dY.double() * D.double() == g).all()) and bool((g.float().double() == g).all())
+    a.X.copy_(_picks(K, rows, 2.0 ** lift, torch.bfloat16, 7).T)
+    a.W.copy_(_picks(K, F, 2.0 ** lift, torch.bfloat16, 6).T)
+    dX, dW, _ = a.backward(D)
+    assert torch.equal(dW.double(), g.T @ a.X.double())
+    assert torch.equal(dX, (g @ a.W.double()).bfloat16())
+
+
+@pytest.mark.parametrize("rows,K,F", [(2200, 2100, 2301), (4096, 1024, 2560)])
+def test_the_middle_parts_of_both_operands_meet(rows, K, F):
+    """12 bits times 12 bits: the parts behind the first of either operand are multiplied with each other, too."""
+    a = Affine(rows, K, F, "fff", bias=False)
+    v = _whole((rows, K), 12, 1)
+    a.X.copy_(v)
+    w = _picks(F, K, 1.0, torch.float64, 2) * _whole((F, 1), 12, 3)
+    a.W.copy_(w)
+    assert torch.equal(a.forward()[0].double(), v @ w.T)
