@@ -169,3 +169,16 @@ def test_overlap_rule_against_every_pair():
         assert got == want, spans
         refused += want
     assert 2000 < refused < 18000
+
+
+def test_assembly_that_writes_m0_says_so():
+    """The compiler takes m0 as its own between statements unless one of them names it as overwritten."""
+    csrc, found = os.path.join(ROOT, "paper_2007_07336_amd", "csrc"), 0
+    for name in sorted(os.listdir(csrc)):
+        if name.endswith((".hip", ".h")):
+            text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, name)).read())
+            for statement in re.findall(r"\basm\s+volatile\s*\((.*?)\)\s*;", text, flags=re.S):
+                if re.search(r"s_\w+\s+m0\b", statement):
+                    found += 1
+                    assert re.search(r':\s*(?:"\w+",\s*)*"m0"', statement), (name, statement)
+    assert found
