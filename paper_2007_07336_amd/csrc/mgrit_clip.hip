@@ -138,26 +138,29 @@ __global__ __launch_bounds__(TH) void clip_scale_kernel(const Entry* table, int 
 
 }  // namespace
 
-size_t clip_workspace(int n, const ClipTensor*) { return sizeof(Space) + (size_t)n * sizeof(Entry); }
+size_t clip_workspace(int filled) { return sizeof(Space) + (size_t)filled * sizeof(Entry); }
 
-hipError_t launch_clip(int n, const ClipTensor* t, float max_norm, float* norm, void* ws, const double** norm_dev, hipStream_t s) {
+hipError_t launch_clip(int n, const mgrit_tensor_t* t, float max_norm, float* norm, void* ws, const double** norm_dev, hipStream_t s) {
   Space* sp = static_cast<Space*>(ws);
   long long chunks = 0;
   bool any = false;
-  for (int i = 0; i < n; i += PER) {
+  int filled = 0;                               // entries of the table
+  for (int i = 0; i < n;) {
     Givens in = {};
-    const int k = n - i < PER ? n - i : PER;
+    int k = 0;
     const long long before = chunks;
-    for (int j = 0; j < k; ++j) {
-      in.e[j] = Given{t[i + j].src, t[i + j].dst, 2 * t[i + j].count + (t[i + j].type ? 1 : 0)};
-      chunks += (t[i + j].count + CHUNK - 1) / CHUNK;
-      any = any || t[i + j].dst;
+    for (; i < n && k < PER; ++i) {
+      if (t[i].count == 0) continue;
+      in.e[k++] = Given{t[i].src, t[i].dst, 2 * t[i].count + (t[i].dtype == MGRIT_BF16 ? 1 : 0)};
+      chunks += (t[i].count + CHUNK - 1) / CHUNK;
+      any = any || t[i].dst;
     }
-    hipLaunchKernelGGL(clip_table_kernel, dim3(1), dim3(256), 0, s, in, sp->table + i, k, before);
+    if (k > 0) hipLaunchKernelGGL(clip_table_kernel, dim3(1), dim3(256), 0, s, in, sp->table + filled, k, before);
+    filled += k;
   }
   const int grid = chunks < GRID ? (int)chunks : GRID;
-  if (grid > 0) hipLaunchKernelGGL(clip_norm_kernel, dim3((unsigned)grid), dim3(TH), 0, s, sp->table, n, chunks, sp->partial);
-  hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)(any ? grid : 1)), dim3(TH), 0, s, sp->table, any ? n : 0, any ? chunks : 0, sp->partial, grid, &sp->norm,
+  if (grid > 0) hipLaunchKernelGGL(clip_norm_kernel, dim3((unsigned)grid), dim3(TH), 0, s, sp->table, filled, chunks, sp->partial);
+  hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)(any ? grid : 1)), dim3(TH), 0, s, sp->table, any ? filled : 0, any ? chunks : 0, sp->partial, grid, &sp->norm,
                      norm, max_norm);
   *norm_dev = &sp->norm;
   return hipGetLastError();

@@ -1,5 +1,6 @@
 // Launch descriptors of the operators around the solver: end layers, loss, clipping.  Internal, as mgrit_internal.h.
 #pragma once
+#include "../../include/mgrit.h"
 #include "mgrit_internal.h"
 
 namespace mgrit {
@@ -57,9 +58,8 @@ struct LossArgs {
 size_t     loss_workspace(const LossArgs& a);
 hipError_t launch_loss(const LossArgs& a, void* ws, hipStream_t s);
 
-struct ClipTensor { const void* src; void* dst; long long count; int type; };
-size_t     clip_workspace(int n, const ClipTensor* t);
+size_t     clip_workspace(int filled);                 // tensors that have entries; the others are passed over
 // norm_dev <- where the norm lies in the workspace as a double
-hipError_t launch_clip(int n, const ClipTensor* t, float max_norm, float* norm, void* ws, const double** norm_dev, hipStream_t s);
+hipError_t launch_clip(int n, const mgrit_tensor_t* t, float max_norm, float* norm, void* ws, const double** norm_dev, hipStream_t s);
 
 }  // namespace mgrit

@@ -2,8 +2,6 @@
 // the order of the launches.  The arithmetic is in mgrit_affine.hip, mgrit_loss.hip and mgrit_clip.hip.
 #include <math.h>
 
-#include <vector>
-
 #include "../../include/mgrit.h"
 #include "mgrit_ops.h"
 
@@ -52,15 +50,11 @@ LossArgs loss_args(const mgrit_loss_t* p) {
   return a;
 }
 
-// The tensors that have entries; false: no room for the list.
-int collect(const mgrit_tensor_t* t, int32_t n, std::vector<ClipTensor>& out) {
+// filled: how many of the tensors have entries
+int check_tensors(const mgrit_tensor_t* t, int32_t n, int* filled) {
+  *filled = 0;
   if (n < 0) return MGRIT_ERR_PROBLEM;
   if (n > 0 && !t) return MGRIT_ERR_POINTER;
-  try {
-    out.reserve((size_t)n);
-  } catch (...) {
-    return MGRIT_ERR_WORKSPACE;
-  }
   long long total = 0;
   for (int i = 0; i < n; ++i) {
     if (t[i].count < 0 || !good_type(t[i].dtype)) return MGRIT_ERR_PROBLEM;
@@ -68,7 +62,7 @@ int collect(const mgrit_tensor_t* t, int32_t n, std::vector<ClipTensor>& out) {
     if (t[i].count == 0) continue;
     const size_t e = t[i].dtype == MGRIT_FP32 ? 4 : 2;
     if (!t[i].src || !aligned_to(t[i].src, e) || !aligned_to(t[i].dst, e)) return MGRIT_ERR_POINTER;
-    out.push_back(ClipTensor{t[i].src, t[i].dst, (long long)t[i].count, t[i].dtype});
+    ++*filled;
   }
   return MGRIT_OK;
 }
@@ -149,22 +143,21 @@ int32_t mgrit_cross_entropy(const mgrit_loss_t* p, const void* logits, const int
 }
 
 size_t mgrit_clip_workspace_bytes(const mgrit_tensor_t* tensors, int32_t n) {
-  std::vector<ClipTensor> t;
-  if (collect(tensors, n, t) != MGRIT_OK) return 0;
-  return clip_workspace((int)t.size(), t.data());
+  int filled = 0;
+  return check_tensors(tensors, n, &filled) == MGRIT_OK ? clip_workspace(filled) : 0;
 }
 
 int32_t mgrit_clip_gradients(const mgrit_tensor_t* tensors, int32_t n, float max_norm, float* norm, double* norm_host,
                              void* workspace, size_t workspace_bytes, void* hip_stream) {
-  std::vector<ClipTensor> t;
-  const int rc = collect(tensors, n, t);
+  int filled = 0;
+  const int rc = check_tensors(tensors, n, &filled);
   if (rc != MGRIT_OK) return rc;
   if (!(max_norm >= 0.0f)) return MGRIT_ERR_PROBLEM;
   if (!workspace || !aligned_to(workspace, 16) || !aligned_to(norm, 4)) return MGRIT_ERR_POINTER;
-  if (workspace_bytes < clip_workspace((int)t.size(), t.data())) return MGRIT_ERR_WORKSPACE;
+  if (workspace_bytes < clip_workspace(filled)) return MGRIT_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const double* at = nullptr;
-  if (launch_clip((int)t.size(), t.data(), max_norm, norm, workspace, &at, s) != hipSuccess) return MGRIT_ERR_HIP;
+  if (launch_clip(n, tensors, max_norm, norm, workspace, &at, s) != hipSuccess) return MGRIT_ERR_HIP;
   if (norm_host) {
     if (hipMemcpyAsync(norm_host, at, sizeof(double), hipMemcpyDeviceToHost, s) != hipSuccess) return MGRIT_ERR_HIP;
     if (hipStreamSynchronize(s) != hipSuccess) return MGRIT_ERR_HIP;

@@ -151,3 +151,19 @@ def test_tensors_that_overlap_results_are_refused():
     M.make_tensor_list([a, a, a[5:]], [None, None, b[5:]])     # tensors that are only read may overlap
     M.make_tensor_list([a[:50], a[50:]], [a[:50], a[50:]])
     M.make_tensor_list([a[:50], a[50:]], [b[:50], b[50:]])
+
+
+def test_empty_tensors_between_hundreds_of_others():
+    """Empty tensors anywhere in a list of several launches' length, at its ends and in whole launches' worth of them."""
+    g = torch.Generator().manual_seed(5)
+    sizes = (torch.rand(700, generator=g) * 7).exp().int().tolist()
+    for i in list(range(0, 3)) + list(range(160, 340)) + list(range(500, 700, 2)) + [698, 699]:
+        sizes[i] = 0
+    full = [normal((n,), 1e-2, "b" if i % 3 == 0 else "f", i) for i, n in enumerate(sizes)]
+    some = [t for t in full if t.numel()]
+    dst, alone = [torch.full_like(t, 7.0) for t in full], [torch.full_like(t, 7.0) for t in some]
+    n, _, host = _clip(full, dst, 0.5, want_norm=True)
+    n2, _, host2 = _clip(some, alone, 0.5, want_norm=True)
+    assert host == host2 and torch.equal(n, n2)
+    for a, b in zip([t for t in dst if t.numel()], alone):
+        assert torch.equal(a, b)

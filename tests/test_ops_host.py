@@ -182,3 +182,11 @@ def test_assembly_that_writes_m0_says_so():
                     found += 1
                     assert re.search(r':\s*(?:"\w+",\s*)*"m0"', statement), (name, statement)
     assert found
+
+
+def test_the_operators_take_no_memory_on_the_host():
+    """The header promises that nothing is allocated, of host memory either."""
+    csrc = os.path.join(ROOT, "paper_2007_07336_amd", "csrc")
+    for name in ("mgrit_ops_api.hip", "mgrit_affine.hip", "mgrit_loss.hip", "mgrit_clip.hip", "mgrit_ops.h"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, name)).read())
+        assert not re.search(r"\b(new|malloc|calloc|hipMalloc\w*|hipHostMalloc|std::(vector|string|map|unique_ptr|function|make_\w+))\b", text), name
