@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2007_07336_amd as M
-from tests.ops_util import Affine, normal, near, sum_bound
+from tests.ops_util import TINY, Affine, normal, near, sum_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -404,3 +404,32 @@ def test_the_middle_parts_of_both_operands_meet(rows, K, F):
     w = _picks(F, K, 1.0, torch.float64, 2) * _whole((F, 1), 12, 3)
     a.W.copy_(w)
     assert torch.equal(a.forward()[0].double(), v @ w.T)
+
+
+@pytest.mark.parametrize("rows", [1 << 16, 200])
+def test_tanh_and_its_slope_near_saturation(rows):
+    """Relative errors in steps of 2^-23: the exponential and its correction 1.5, the reciprocal of a rounded sum 1.5, and half a step for
+    each product, so 5.5 for 4 e r^2 and at most 4 for (1 - e) r; the result is scaled by 1."""
+    z = torch.cat([torch.linspace(-43, 43, rows - 100), torch.linspace(-0.4, 0.4, 90), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 0.35, -0.35, 1e30, -1e30, 88.0, 3e38])])
+    X = z[:, None].cuda()
+    W, Y, D = torch.ones((1, 1), device="cuda"), torch.empty_like(X), torch.empty_like(X)
+    if rows == 200:                                              # columns, with the large tiles' code
+        X, W = torch.ones((300, 8), device="cuda"), torch.zeros((rows, 8))
+        W[:, 3] = z
+        W, Y, D = W.cuda(), torch.empty((300, rows), device="cuda"), torch.empty((300, rows), device="cuda")
+    p = M.make_affine(M=X.shape[0], K=X.shape[1], F=W.shape[0], act=M.MGRIT_ACT_TANH)
+    ws = torch.empty(M.mgrit_affine_workspace_bytes(p) + 16, dtype=torch.uint8, device="cuda")
+    M.mgrit_affine_forward(p, X, W, None, None, Y, D, ws)
+    v = (X.double() @ W.double().T)
+    e = torch.exp(-2.0 * v.abs())
+    near(Y, torch.tanh(v), 4 * 2.0 ** -23 * torch.tanh(v).abs() + TINY, "tanh")
+    slope = 4.0 * e / (1.0 + e) ** 2
+    near(D, slope, 6 * 2.0 ** -23 * slope + 8 * TINY, "slope")
+
+
+def test_tanh_of_what_is_not_finite():
+    X = torch.tensor([[float("inf")], [float("-inf")], [float("nan")]], device="cuda")
+    Y, D = torch.empty_like(X), torch.empty_like(X)
+    p = M.make_affine(M=3, K=1, F=1, act=M.MGRIT_ACT_TANH)
+    M.mgrit_affine_forward(p, X, torch.ones((1, 1), device="cuda"), None, None, Y, D, None)
+    assert Y[:2, 0].tolist() == [1.0, -1.0] and D[:2, 0].tolist() == [0.0, 0.0] and bool(torch.isnan(Y[2]) & torch.isnan(D[2]))
