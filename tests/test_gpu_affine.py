@@ -433,3 +433,13 @@ def test_tanh_of_what_is_not_finite():
     p = M.make_affine(M=3, K=1, F=1, act=M.MGRIT_ACT_TANH)
     M.mgrit_affine_forward(p, X, torch.ones((1, 1), device="cuda"), None, None, Y, D, None)
     assert Y[:2, 0].tolist() == [1.0, -1.0] and D[:2, 0].tolist() == [0.0, 0.0] and bool(torch.isnan(Y[2]) & torch.isnan(D[2]))
+
+
+# few rows against many with so long a contraction that every wavefront goes through several slabs: places in LDS are filled again while
+# others are read.  Whole 16-byte rows in all types, with whole slabs and without; a contraction shared by workgroups
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("few,many,K", [(3, 8203, 2048), (16, 8203, 2056), (17, 8203, 4096), (32, 8203, 2048), (64, 8203, 2056), (64, 8203, 4104), (16, 500, 9000),
+                                        (33, 129, 16384)])
+def test_few_rows_with_a_long_contraction(few, many, K, types):
+    Affine(few, K, many, types, "tanh", 0.5, residual=True).check_forward(factor=True)
+    Affine(many, K, few, types, "relu", 2.0, bias=False, seed=7).check_forward()
