@@ -247,7 +247,7 @@ enum { MGRIT_ACT_IDENTITY = 2 };                           /* with MGRIT_ACT_TAN
  * (ReLU'(0) = 0; a NaN stays a NaN in every activation).  Types: X (and dX) xtype, W wtype, and R, Y, D, dY ytype, each MGRIT_FP32 or
  * MGRIT_BF16; b, dW and db are float.  Operands enter the products as they are stored, sums are float: bf16 operands are
  * not rounded again and float ones not rounded at all (unlike the solver's, whose MGRIT_BF16 rounds the state).  Some products
- * take an operand in several parts whose sum it is; where operands hold infinities, an entry that the formula makes infinite
+ * take an operand in several parts whose sum it is, every bit of it down to the smallest normal float; where operands hold infinities, an entry that the formula makes infinite
  * may come out as NaN then.  Entries that no infinity or NaN takes part in are not touched by it. */
 typedef struct mgrit_affine {
   int32_t M;           /* rows (samples), >= 0; with 0 rows only dW and db are written, as zero                  */

@@ -623,8 +623,10 @@ struct FewPlan {
   int sb, fb, parts;
   long long kpart;
 };
-// Where one side has at most 64 rows.  Workgroups: one for 16 stream rows, for 32 from 16384 on against at most 16; the contraction is shared between
-// workgroups where there are fewer than two for each of the 256 compute units, down to 1024 a part (128 for each wavefront).
+// Where one side has at most 64 rows.  Workgroups: one for 16 stream rows, from FEW_MANY of them on one for 32 (us with 16 / 32, contraction of
+// 4096: 64 rows on 4096 bf16 11.4 / 16.3, on 8192 20 / 16, on 32768 76 / 58; one row on 4096 8.7 / 11.6, on 8192 13.7 / 12.4, on 32768 45 / 39).
+// The contraction is shared between workgroups where there are fewer than one for each of the 256 compute units, to about two for each, down
+// to 1024 a part (128 for each wavefront where there are eight).
 FewPlan few_plan(const Product& q) {
   FewPlan p = {};
   const long long few = q.I < q.J ? q.I : q.J, many = q.I < q.J ? q.J : q.I;
@@ -680,9 +682,10 @@ hipError_t launch_few(const Product& q, const FewPlan& p, float* partial, hipStr
 // The backward pass where G has at most 16 columns (a head's classes) or rows (samples): both of its products in one pass over
 // the large operand S, whose rows go with G's long side:
 //   outS[r][k] = sum_t G(r, t) T[t][k],   outT[t][k] = sum_r G(r, t) S[r][k]
-// (few classes: S = X, T = W, outS = dX, outT = dW; few samples: S = W, T = X, outS = dW, outT = dX).  Bound by reading S and writing
-// outS: 2 NT multiplications for two values that pass are within what the vector unit does at that rate (2 samples on 39889 x 1088
-// float: 348 MB in 84 us; 8192 samples x 4096, 16 classes, float: 268 MB in 97; 32 x 65536, 10 classes: latency, 12).  Workgroup: 256 k by a chunk of
+// (few classes: S = X, T = W, outS = dX, outT = dW; few samples: S = W, T = X, outS = dW, outT = dX).  With few of them bound by reading S and
+// writing outS (2 samples on 39889 x 1088 float: 348 MB in 82 us, 4.2 TB/s).  With many by the wavefronts' own work and waits, 2 NT
+// multiplications for each entry of S: 8192 samples x 4096, 16 classes, float is 268 MB in 94 us, 2.9 TB/s, the vector units busy 40 % of the time and
+// the wavefronts waiting half of theirs, with 1024 workgroups where 768 fit at once.  32 x 65536, 10 classes: latency, 13.  Workgroup: 256 k by a chunk of
 // rows, a wavefront every fourth row; a lane has four k of all of T and of outT in registers, G lies in LDS.
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Any4 { T v[4]; };
 template <typename T> __device__ __forceinline__ floatx4 load4(const T* p, long long n) {       // n of them exist

@@ -63,8 +63,8 @@ struct Row {
 
 // One row per workgroup of TH threads.  NV > 0: the row's whole 16-byte vectors fit NV registers of each thread, and the row is
 // read once.  NV = 0: it is read twice.  rows <- l_r, grad <- gradient; `counted`: the number of rows that scale is divided by.
-// Bound by memory: 4096 rows of 50021 bf16, 0.8 GB in and out, 172 to 190 us, 4.3 to 4.8 TB/s where a large copy reaches 5.0 (read
-// twice: 197).
+// Bound by memory: 4096 rows of 50021 bf16, 0.8 GB in and out, 164 us, 5.0 TB/s as a large copy (183 where the same tensors are taken again
+// at once, and 197 there with rows that are read twice).
 template <typename T, int TH, int NV>
 __global__ __launch_bounds__(TH) void loss_rows_kernel(const T* logits, const int64_t* labels, float* rows, T* grad, int V, float scale, const int* counted) {
   constexpr int N = Vec<T>::N;
