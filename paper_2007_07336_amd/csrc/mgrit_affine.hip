@@ -855,10 +855,10 @@ struct WideArgs {
   Plane A, B;
   Epilogue e;
   long long I, J, Kc;
-  int slabs;                   // of one pass over the contraction
+  int slabs;                   // of the contraction
   int passes;                  // pairs of parts that are multiplied
   unsigned partA, partB;       // of pass s: bits 4 s .. 4 s + 3
-  int per;                     // slabs that one workgroup takes of its tile's, all passes counted
+  int per;                     // slabs that one workgroup takes, in all passes
   float* partial;              // several workgroups: their sums
 };
 
@@ -928,10 +928,10 @@ struct Stream {
     if (KS) { base += KSLAB * p.ld; room -= KSLAB * p.ld; }
     else along += 128;
   }
-  // from behind the last slab to the first one, `parts` parts further
+  // back by `slabs`, and `parts` parts further
   __device__ __forceinline__ void again(const Plane& p, int slabs, int parts) {
     if (KS) { base -= (long long)slabs * KSLAB * p.ld; room += (long long)slabs * KSLAB * p.ld; }
-    else along = 0;
+    else along -= slabs * 128;
     base += parts * p.part;
   }
   // fragment of tile i in step `step`
@@ -970,23 +970,25 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   const long long group = L / (GM * tj), first = group * GM, size = ti - first < GM ? ti - first : GM, in = L - group * GM * tj;
   const long long i0 = (first + in % size) * BT, j0 = in / size * BT;
 
-  const int total = a.slabs * a.passes, t0 = share * a.per, t1 = t0 + a.per < total ? t0 + a.per : total;
+  // Where workgroups share a tile each takes a piece of the contraction, through all passes: with a product's passes in different
+  // sums, one part too many rounded up could overflow before the others come in.
+  const int s0 = share * a.per, slabs = s0 + a.per < a.slabs ? a.per : a.slabs - s0, total = slabs * a.passes;
   Stream<CT, BT, AS> sa;
   Stream<CT, BT, BS> sb;
   // the pass of either operand's next slab, and its slabs that are left; parts by pass
-  int passA = t0 / a.slabs, passB = passA;
+  int passA = 0, passB = 0;
   auto part = [](unsigned parts, int pass) { return (int)(parts >> (4 * pass) & 15u); };
-  sa.init(a.A, i0, a.I, a.Kc, part(a.partA, passA), t0 % a.slabs, wave, lane, wi);
-  sb.init(a.B, j0, a.J, a.Kc, part(a.partB, passB), t0 % a.slabs, wave, lane, wj);
-  int leftA = a.slabs - t0 % a.slabs, leftB = leftA;
+  sa.init(a.A, i0, a.I, a.Kc, part(a.partA, 0), s0, wave, lane, wi);
+  sb.init(a.B, j0, a.J, a.Kc, part(a.partB, 0), s0, wave, lane, wj);
+  int leftA = slabs, leftB = slabs;
   const unsigned lds_at = (unsigned)(unsigned long long)(LdsPtr*)lds;
   auto nextA = [&]() {
     sa.next(a.A);
-    if (--leftA == 0) { leftA = a.slabs; sa.again(a.A, a.slabs, part(a.partA, passA + 1) - part(a.partA, passA)); ++passA; }
+    if (--leftA == 0) { leftA = slabs; sa.again(a.A, slabs, part(a.partA, passA + 1) - part(a.partA, passA)); ++passA; }
   };
   auto nextB = [&]() {
     sb.next(a.B);
-    if (--leftB == 0) { leftB = a.slabs; sb.again(a.B, a.slabs, part(a.partB, passB + 1) - part(a.partB, passB)); ++passB; }
+    if (--leftB == 0) { leftB = slabs; sb.again(a.B, slabs, part(a.partB, passB + 1) - part(a.partB, passB)); ++passB; }
   };
   const int c = lane & 31, g = lane >> 5;
   Frag fa[2][T], fb[2][T];
@@ -1044,7 +1046,7 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   for (int i = 0; i < NL; ++i) { sa.load(i, lds_at, wave); sb.load(i, lds_at + 3 * SLAB, wave); }
   nextA();
   nextB();
-  if (t0 + 1 < t1) {
+  if (total > 1) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) sa.load(i, lds_at + SLAB, wave);
 #pragma unroll
@@ -1059,7 +1061,7 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   // Part i of an operand is kept 256^i times as large.  Passes come in the order of their scale, the largest first, and the sums are
   // brought to that of the next pass where it is another, at last to 1: exact, and every bit of a float arrives (4096 x 1024 x 4096 float rows
   // on bf16 weights 107 us without, 110 so; two float operands 186 and 190).
-  int pass = t0 / a.slabs, left = a.slabs - t0 % a.slabs;         // of the slab that is multiplied, and how many of it are left
+  int pass = 0, left = slabs;                                     // of the slab that is multiplied, and how many of it are left
   auto scale_of = [&](int p) { return part(a.partA, p) + part(a.partB, p); };
   auto shrink = [&]() {
     const float f = 0x1p-8f;
@@ -1088,23 +1090,21 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   };
   auto done = [&]() {
     if (--left) return;
-    left = a.slabs;
+    left = slabs;
     if constexpr (sizeof(CT) == 2) {                              // (float operands have one part)
       if (scale_of(pass + 1) < scale_of(pass)) shrink();          // (by one step: see wide_args)
     }
     ++pass;
   };
-  for (int t = t0; t < t1 - 2; ++t) {
+  for (int t = 0; t < total - 2; ++t) {
     multiply(yes, no);
     done();
   }
-  if (t0 + 1 < t1) {
+  if (total > 1) {
     multiply(no, no);
     done();
   }
   multiply(no, yes);
-  const int last_scale = sizeof(CT) == 2 ? scale_of(pass) : 0;
-  const float unscale = last_scale == 0 ? 1.0f : last_scale == 1 ? 0x1p-8f : 0x1p-16f;
 
   // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands.  With B as the
   // instructions' first operand a lane has four consecutive columns of one row of every tile, which it writes at once.  Strips are
@@ -1140,7 +1140,7 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<floatx4*>(strip + c * PITCH + j * 32 + 8 * q + 4 * g) =
-              floatx4{acc[m][j][4 * q] * unscale, acc[m][j][4 * q + 1] * unscale, acc[m][j][4 * q + 2] * unscale, acc[m][j][4 * q + 3] * unscale};
+              floatx4{acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
     }
     __builtin_amdgcn_wave_barrier();
     const float* from = strip + lr * PITCH + lc;
@@ -1401,15 +1401,14 @@ WidePlan wide_plan(const Product& q) {
   w.bf16 = q.A.type != 0;                                       // (they are planes of one type)
   w.passes = q.B.parts > 1 ? 6 : q.A.parts > 1 ? q.A.parts : 1;
   w.slabs = (int)((q.Kc + slab_of(w.bf16) - 1) / slab_of(w.bf16));
-  const int total = w.slabs * w.passes;
   double best = 0.0;
   for (int bt = whole_slabs(q.A, w.bf16) && whole_slabs(q.B, w.bf16) ? 256 : 128; bt >= 64; bt /= 2) {
     const long long tiles = (q.I + bt - 1) / bt * ((q.J + bt - 1) / bt);
     if (tiles > MOST_TILES) continue;
     const double slab = w.bf16 ? (bt == 256 ? 1.6 : bt == 128 ? 0.55 : 0.2) : (bt == 256 ? 7.2 : bt == 128 ? 1.9 : 0.55), ends = bt == 256 ? 6.0 : bt == 128 ? 3.0 : 2.0;
-    for (int parts = 1; parts <= 32 && (parts == 1 || (2 * parts <= total && tiles * parts <= 2048)); ++parts) {
-      const int per = (total + parts - 1) / parts;
-      if (parts > 1 && (total + per - 1) / per != parts) continue;
+    for (int parts = 1; parts <= 32 && (parts == 1 || (parts <= w.slabs && 2 * parts <= w.slabs * w.passes && tiles * parts <= 2048)); ++parts) {
+      const int piece = (w.slabs + parts - 1) / parts, per = piece * w.passes;
+      if (parts > 1 && (w.slabs + piece - 1) / piece != parts) continue;
       const long long rounds = (tiles * parts + 255) / 256;
       const double join = parts > 1 ? 4.0 + (double)q.I * q.J * 4.0 * (2 * parts) / 4.0e6 : 0.0;
       const double us = (double)rounds * (per * slab + (bt == 256 ? ends : 0.0)) + (bt == 256 ? 0.0 : ends) + join;
@@ -1465,7 +1464,7 @@ WideArgs wide_args(const Product& q, const WidePlan& w, void* partial) {
   // up to its scale, which falls by one at a time.
   a.partA = w.passes == 6 ? 0x001120u : w.passes == 3 ? 0x012u : w.passes == 2 ? 0x01u : 0u;
   a.partB = w.passes == 6 ? 0x010102u : 0u;
-  a.per = (w.slabs * w.passes + w.parts - 1) / w.parts;
+  a.per = (w.slabs + w.parts - 1) / w.parts;
   a.partial = w.parts > 1 ? static_cast<float*>(partial) : nullptr;
   return a;
 }
