@@ -34,14 +34,21 @@ __device__ __forceinline__ float tanh_with_slope(float z, float* slope) {
   return a < 0.35f ? series : copysignf((1.0f - e) * r, z);
 }
 
-// v = hi + lo / 256, both representable in bf16 if v has 16 significant bits.  lo is 256 times what hi leaves so that it is about as large
-// as v: what is left of small values would be below bf16's range otherwise (floats below 2^-110 lost bits).  What overflows by
-// rounding is cut instead; an infinity or a NaN stays in hi.
-__device__ __forceinline__ void split2(float v, float* hi, float* lo) {
-  float h = widen(narrow<__bf16>(v));
-  if (fabsf(h) == INFINITY && fabsf(v) < INFINITY) h = copysignf(0x1.fep127f, v);
+// The parts of a value are bf16 values, each kept 2^s times as large (S0, S1, S2).  The second and the third so that they are about as large
+// as the value: what is left of small values would be below bf16's range otherwise (floats below 2^-110 lost bits).  The first at one
+// half: rounded up it can be past the largest float, or its product with the other operand's, where the whole value or product is not;
+// and so that two products of the same scale stay in range together.  Two parts: the product of two bf16 values, which has 16
+// significant bits.  Three: a float.
+template <int PARTS> struct Scale;
+template <> struct Scale<2> { static constexpr int S0 = -1, S1 = 8, S2 = 0; };
+template <> struct Scale<3> { static constexpr int S0 = -1, S1 = 7, S2 = 16; };
+__device__ __forceinline__ constexpr float two_to(int s) { return __builtin_bit_cast(float, (127 + s) << 23); }
+
+// hi = v 2^s rounded to bf16, and what it leaves of v, 2^t times as large (nothing of an infinity or a NaN)
+__device__ __forceinline__ void split2(float v, int s, int t, float* hi, float* lo) {
+  const float h = widen(narrow<__bf16>(v * two_to(s)));
   *hi = h;
-  *lo = fabsf(h) < INFINITY ? (v - h) * 256.0f : 0.0f;
+  *lo = fabsf(h) < INFINITY ? (v - h * two_to(-s)) * two_to(t) : 0.0f;
 }
 
 struct Out { float y, d; };
@@ -858,6 +865,7 @@ struct WideArgs {
   int slabs;                   // of the contraction
   int passes;                  // pairs of parts that are multiplied
   unsigned partA, partB;       // of pass s: bits 4 s .. 4 s + 3
+  unsigned scales;             // of pass s: its products are 2^(n - 2) times as large, n in bits 5 s .. 5 s + 4
   int per;                     // slabs that one workgroup takes, in all passes
   float* partial;              // several workgroups: their sums
 };
@@ -1058,13 +1066,14 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   }
 #pragma unroll
   for (int i = 0; i < T; ++i) read(pa, pb, 0, i);
-  // Part i of an operand is kept 256^i times as large.  Passes come in the order of their scale, the largest first, and the sums are
-  // brought to that of the next pass where it is another, at last to 1: exact, and every bit of a float arrives (4096 x 1024 x 4096 float rows
-  // on bf16 weights 107 us without, 110 so; two float operands 186 and 190).
+  // Passes come in the order of their scale, the largest first, and the sums are brought to that of the next pass where it is another,
+  // at last to 1: exact, and every bit of a float arrives (4096 x 1024 x 4096 float rows on bf16
+  // weights 107 us without, 112 so; two float operands 186 and 190).
   int pass = 0, left = slabs;                                     // of the slab that is multiplied, and how many of it are left
-  auto scale_of = [&](int p) { return part(a.partA, p) + part(a.partB, p); };
-  auto shrink = [&]() {
-    const float f = 0x1p-8f;
+  auto scale_of = [&](int p) { return (int)(a.scales >> (5 * p) & 31u) - 2; };
+  auto shrink = [&](int by) {
+    if (by == 0) return;
+    const float f = two_to(-by);
     // Where all accumulation registers are taken the compiler moves them to vector registers at once, and that through memory; so in
     // assembly, four at a time.  It does not see to the waits there: they stand before the first and behind the last.
     if constexpr (T == 4) asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
@@ -1091,9 +1100,7 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
   auto done = [&]() {
     if (--left) return;
     left = slabs;
-    if constexpr (sizeof(CT) == 2) {                              // (float operands have one part)
-      if (scale_of(pass + 1) < scale_of(pass)) shrink();          // (by one step: see wide_args)
-    }
+    if constexpr (sizeof(CT) == 2) shrink(scale_of(pass) - scale_of(pass + 1));          // (float operands have one part)
     ++pass;
   };
   for (int t = 0; t < total - 2; ++t) {
@@ -1105,6 +1112,7 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
     done();
   }
   multiply(no, yes);
+  const float unscale = two_to(sizeof(CT) == 2 ? -scale_of(pass) : 0);
 
   // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands.  With B as the
   // instructions' first operand a lane has four consecutive columns of one row of every tile, which it writes at once.  Strips are
@@ -1140,7 +1148,7 @@ __device__ __forceinline__ void product_wide(const WideArgs& a, long long L, int
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<floatx4*>(strip + c * PITCH + j * 32 + 8 * q + 4 * g) =
-              floatx4{acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
+              floatx4{acc[m][j][4 * q] * unscale, acc[m][j][4 * q + 1] * unscale, acc[m][j][4 * q + 2] * unscale, acc[m][j][4 * q + 3] * unscale};
     }
     __builtin_amdgcn_wave_barrier();
     const float* from = strip + lr * PITCH + lc;
@@ -1194,8 +1202,8 @@ __global__ __launch_bounds__(256, wide_waves(BT)) void product_pair_kernel(WideA
 }
 
 // Operand -> planes of CT: rows x (k padded to ldo with zeros), PARTS of them: 1 as it is (or widened); 2: the product of two bf16
-// values, which has 16 significant bits, as the sum of two; 3: a float as the sum of three; part i is kept 256^i times as
-// large (the bf16 instructions take subnormal values as they are).  A thread has eight columns of every eighth row of a workgroup's
+// values, which has 16 significant bits, as the sum of two; 3: a float as the sum of three, all as large as Scale says
+// (the bf16 instructions take subnormal values as they are).  A thread has eight columns of every eighth row of a workgroup's
 // span x 256 entries.  With `sums` the columns' sums over the span as well (of the gradient, for the bias), and PARTS = 0 is
 // those alone.  Bound by memory: 8192 x 4096 bf16 with factors into two parts, with sums, 268 MB in 45 us.  All that a call lays out goes in one launch, one job for each array.
 struct LayJob {
@@ -1242,8 +1250,8 @@ __device__ __forceinline__ void lay_out(const LayJob& a, unsigned block, float (
           float lo[8], least[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            split2(v[j], &v[j], &lo[j]);
-            if (PARTS == 3) split2(lo[j], &lo[j], &least[j]);
+            split2(v[j], Scale<PARTS>::S0, Scale<PARTS>::S1, &v[j], &lo[j]);
+            if constexpr (PARTS == 3) split2(lo[j], 0, Scale<3>::S2 - Scale<3>::S1, &lo[j], &least[j]);
           }
           store8(o + a.rows * ldo, lo);
           if (PARTS == 3) store8(o + 2 * a.rows * ldo, least);
@@ -1460,10 +1468,16 @@ WideArgs wide_args(const Product& q, const WidePlan& w, void* partial) {
   a.passes = w.passes;
   // A's parts each against B; of three parts each, the six pairs that make up a float product: the three that are left out are
   // at most 2^-23 of it together.  The smallest first: added to the sum of the large ones, each of them would round that once
-  // more (1024^3 float: 6.7e-7 off with the largest first, 1.8e-7 so, the float instructions 5.7e-7).  The numbers of a pass's parts add
-  // up to its scale, which falls by one at a time.
+  // more (1024^3 float: 6.7e-7 off with the largest first, 1.8e-7 so, the float instructions 5.7e-7).
   a.partA = w.passes == 6 ? 0x001120u : w.passes == 3 ? 0x012u : w.passes == 2 ? 0x01u : 0u;
   a.partB = w.passes == 6 ? 0x010102u : 0u;
+  auto scale = [](int parts, unsigned i) {
+    if (parts < 2) return 0;
+    const int s[2][3] = {{Scale<2>::S0, Scale<2>::S1, Scale<2>::S2}, {Scale<3>::S0, Scale<3>::S1, Scale<3>::S2}};
+    return s[parts - 2][i];
+  };
+  for (int i = 0; i < w.passes; ++i)
+    a.scales |= (unsigned)(scale(q.A.parts, a.partA >> (4 * i) & 15u) + scale(q.B.parts, a.partB >> (4 * i) & 15u) + 2) << (5 * i);
   a.per = (w.slabs + w.parts - 1) / w.parts;
   a.partial = w.parts > 1 ? static_cast<float*>(partial) : nullptr;
   return a;

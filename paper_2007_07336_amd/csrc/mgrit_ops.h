@@ -13,7 +13,7 @@ struct Operand {
   long long ld;
   int type;                          // 0 float, 1 bf16
   int kslow;
-  // set for planes in the workspace: rows end in zeros up to ld, and the operand is the sum of `parts` planes, `part` entries apart, plane i 256^i times as large
+  // set for planes in the workspace: rows end in zeros up to ld, and the operand is the sum of `parts` planes, `part` entries apart, each on its scale
   int padded, parts;
   long long part;
 };

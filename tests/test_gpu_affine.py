@@ -443,3 +443,42 @@ def test_tanh_of_what_is_not_finite():
 def test_few_rows_with_a_long_contraction(few, many, K, types):
     Affine(few, K, many, types, "tanh", 0.5, residual=True).check_forward(factor=True)
     Affine(many, K, few, types, "relu", 2.0, bias=False, seed=7).check_forward()
+
+
+@pytest.mark.parametrize("types,rows,K,F", PARTED)
+def test_products_near_the_largest_float(types, rows, K, F):
+    """Single products in [2^127, 2^128) of values half a bf16 step from the next ones: what the first parts leave is as large as it gets."""
+    g = torch.Generator().manual_seed(1)
+
+    def values(shape, odd):                                       # 257 .. 361 (odd) or 129 .. 181, by 2^-8 or 2^-7, either sign
+        n = torch.randint(128, 181, shape, generator=g, dtype=torch.int64)
+        n = (2 * n + 1).double() / 256 if odd else (n + 1).double() / 128
+        return (n * (2 * torch.randint(0, 2, shape, generator=g) - 1).double()).cuda()
+
+    a = Affine(rows, K, F, types, bias=False)
+    v = values((rows, K), True) * 2.0 ** 64
+    a.X.copy_(v)
+    w = _picks(F, K, 1.0, torch.float64, 2) * values((F, 1), types == "fff") * 2.0 ** 63
+    a.W.copy_(w)
+    want = v @ w.T
+    assert bool((a.W.double() == w).all()) and float(want.abs().max()) < 2.0 ** 128 and float(want.abs().min()) >= 2.0 ** 127
+    assert torch.equal(a.forward()[0].double(), want)
+
+
+@pytest.mark.parametrize("types,rows,K,F", PARTED)
+def test_products_whose_first_parts_pass_the_largest_float(types, rows, K, F):
+    """Values a little below powers of two, which bf16 rounds up to those: the product of the first parts alone is 2^128, the whole one is not."""
+    g = torch.Generator().manual_seed(1)
+
+    def values(shape):                                            # 1 - n 2^-12, n = 1 .. 7, either sign
+        n = torch.randint(1, 8, shape, generator=g, dtype=torch.int64).double()
+        return ((1.0 - n * 2.0 ** -12) * (2 * torch.randint(0, 2, shape, generator=g) - 1).double()).cuda()
+
+    a = Affine(rows, K, F, types, bias=False)
+    v = values((rows, K)) * 2.0 ** 65
+    a.X.copy_(v)
+    w = _picks(F, K, 1.0, torch.float64, 2) * (values((F, 1)) if types == "fff" else 1.0) * 2.0 ** 63
+    a.W.copy_(w)
+    want = v @ w.T
+    assert bool((a.X.bfloat16().double().abs() == 2.0 ** 65).all()) and float(want.abs().max()) < 2.0 ** 128
+    assert torch.equal(a.forward()[0].double(), want)
