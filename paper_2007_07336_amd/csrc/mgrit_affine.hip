@@ -183,7 +183,8 @@ typedef int int4v __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void to_lds(const char* base, int offset, int along, unsigned room, unsigned to) {
   const unsigned long long b = reinterpret_cast<unsigned long long>(base);
   const int4v rsrc = {(int)(unsigned)b, (int)(unsigned)(b >> 32), (int)room, 0x00020000};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" :: "s"(to), "v"(offset), "s"(rsrc), "s"(along) : "m0", "memory");
+  unsigned m0;                       // (an output, so that the compiler knows that it changes; named as overwritten it brings a warning each)
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(rsrc), "s"(along) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------ any size, any order
