@@ -1334,7 +1334,7 @@ int lay_span(long long rows, long long tiles) {
 }
 
 // ---- which matrix instructions, and which operands have to be laid out
-// Two bf16 operands go to the bf16 instructions, and a float A against a bf16 B does if the product is large: three parts hold
+// Two bf16 operands go to the bf16 instructions, and a float A against a bf16 B may if the product is large: three parts hold
 // a float's 24 bits, and three passes of the bf16 instructions take less than one of the float ones, by more than the two planes' worth
 // of bytes that laying it out in parts costs over widening B.
 // us on the float / the bf16 instructions, float rows on bf16 weights: 256 x 1024 x 1024 18.1 / 18.0, 512 x 1024 x 1024 24.7 / 22.0, 1024^3
@@ -1343,10 +1343,16 @@ constexpr double SPLIT = 1.0e9;
 // Two float operands, six passes, on the float / the bf16 instructions: 2048 x 1024 x 2048 70 / 70, 2048^3 129 / 123 and its backward pass
 // 258 / 228, 4096 x 1024 x 4096 273 / 195, 4096^3 936 / 656; backward of 2048 x 1000 x 1000 82 / 131.
 constexpr double SPLIT2 = 6.0e9;
-inline bool on_bf16(const Product& q) {                         // of a product whose operands are not laid out yet, or both
+// Beyond these sizes the estimates of both ways decide (product_us), because parts are bytes, too: where a side is short they cost more than
+// the instructions save (us on the float / the bf16 instructions: 8192 x 8192 x 100 float 142 / 305, backward of 6282 x 56 x 20295 with factors
+// 640 / 1010, of 8192 x 56 x 8192 float states on bf16 weights 297 / 538, but of 8192 x 256 x 8192 float 656 / 599).
+inline bool may_bf16(const Product& q) {                        // of a product whose operands are not laid out yet
   const double size = (double)q.I * (double)q.J * (double)q.Kc;
   return q.A.type ? q.B.type : size >= (q.B.type ? SPLIT : SPLIT2);
 }
+inline bool may_float(const Product& q) { return !q.A.type || !q.B.type; }
+constexpr double COPY = 5.3e6;                                  // bytes a us that layouts and reads of whole operands reach
+constexpr double AHEAD = 1.03;                                  // by which the float instructions have to be ahead, which are less exact
 inline int bf16_parts(int type, const void* factors) { return type ? (factors ? 2 : 1) : 3; }
 inline int slab_of(bool bf16) { return bf16 ? 64 : 32; }
 // Rows along k need whole 16-byte pieces, and whole slabs where 256 x 256 tiles read them: a product with few of those takes smaller ones
@@ -1363,12 +1369,16 @@ struct Layout {
   char* base;
   size_t bytes;
   long long blocks;
+  double moved;                       // bytes read and written
 
   char* take(size_t n) { char* p = base + bytes; bytes += up(n); return p; }
+  // (ldo 0: no planes, sums only.  Not `out`, which may be null where sizes alone are asked for)
   void add(const void* p, const void* f, int type, bool bf16, long long rows, long long K, void* out, long long ldo, int span, float scale, float* sums) {
+    const bool planes = ldo > 0;
     LayJob& j = jobs.j[jobs.n++];
-    j = LayJob{p, f, out, sums, rows, K, ldo, span, type + 2 * (out && bf16) + (f ? 4 : 0) + (out ? 0 : 8), scale, (unsigned)blocks};
-    blocks += ((out ? ldo : K) + 255) / 256 * ((rows + span - 1) / span);
+    j = LayJob{p, f, out, sums, rows, K, ldo, span, type + 2 * (planes && bf16) + (f ? 4 : 0) + (planes ? 0 : 8), scale, (unsigned)blocks};
+    blocks += ((planes ? ldo : K) + 255) / 256 * ((rows + span - 1) / span);
+    moved += (double)rows * ((double)K * (type ? 2 : 4) * (f ? 2 : 1) + (double)ldo * (bf16 ? 2 * bf16_parts(type, f) : 4));
   }
   // the operand itself, or its plane in the workspace
   Operand plane(const Operand& o, bool bf16, long long rows, long long Kc, bool any_pieces) {
@@ -1401,6 +1411,7 @@ struct WidePlan {
   bool bf16;
   int bt, slabs, passes, parts;       // parts: workgroups that share a tile's contraction
   size_t bytes;                       // of their sums
+  double us;                          // the estimate
 };
 // The tile and the number of parts whose time is estimated lowest: tiles run one to a compute unit at a time or share it without
 // getting faster; us for a slab by what the loop reaches (256: 1380 TFLOP/s bf16, 150 float), the start and end of a tile, and the
@@ -1425,8 +1436,19 @@ WidePlan wide_plan(const Product& q) {
     }
   }
   w.bytes = w.parts > 1 ? (size_t)w.parts * q.I * q.J * sizeof(float) : 0;
+  w.us = best;
   return w;
 }
+// Estimated time of a product of planes, for the choice of instructions: the tiles' or that of the planes' bytes, each read once in
+// every pass.  The large tiles' results are written with nothing beside them, which tells where the contraction is short.
+double product_us(const Product& q) {
+  const WidePlan w = wide_plan(q);
+  const long long rounds = ((q.I + 255) / 256 * ((q.J + 255) / 256) * w.parts + 255) / 256;
+  const double tiles = w.us + (w.bt == 256 ? 6.0 * (double)rounds : 0.0);
+  const double bytes = (double)w.passes * (w.bf16 ? 2.0 : 4.0) * (double)q.Kc * (double)(q.I + q.J) / COPY;
+  return tiles > bytes ? tiles : bytes;
+}
+double layout_us(const Layout& l) { return l.jobs.n ? 3.0 + l.moved / COPY : 0.0; }
 
 // Room for the sums of the parts of a product whose operands are where they will be read
 size_t parts_workspace(const Product& q) {
@@ -1527,6 +1549,18 @@ hipError_t launch_wide_pair(const Product& qw, const Product& qx, char* partial_
   return e;
 }
 
+// Which instructions a single product takes
+double forward_us(const Product& q, bool bf16) {
+  Layout l = {};
+  Product p = q;
+  p.A = l.plane(q.A, bf16, q.I, q.Kc, few_tiles(q));
+  p.B = l.plane(q.B, bf16, q.J, q.Kc, few_tiles(q));
+  return layout_us(l) + product_us(p);
+}
+bool forward_bf16(const Product& q) {
+  return may_bf16(q) && (!may_float(q) || forward_us(q, true) <= AHEAD * forward_us(q, false));
+}
+
 // ---- the backward pass: G = dY * D is laid out once for both products where a large tile reads it and it is not there already
 Product input_product(const BackwardArgs& b) {
   Product q = {};
@@ -1553,8 +1587,8 @@ struct BackwardPlan {
   char *partial_x, *partial_w;
   size_t bytes;
 };
-// base: the workspace, or null for the size alone
-BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
+// Operands and layouts with the given instructions.  base: the workspace, or null for sizes alone
+BackwardPlan lay_backward(const BackwardArgs& b, char* base, bool x_bf16, bool w_bf16) {
   BackwardPlan p = {};
   p.lay.base = base;
   p.x = input_product(b);
@@ -1562,7 +1596,6 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
   p.chunks = chunks_of(b.M);
   p.sums = p.chunks > 1 ? reinterpret_cast<float*>(p.lay.take((size_t)p.chunks * b.F * sizeof(float))) : b.db;
   const bool x = b.dX && wide_sizes(p.x), w = b.dW && wide_sizes(p.w);
-  const bool x_bf16 = on_bf16(p.x), w_bf16 = on_bf16(p.w);      // (before the planes' types take the operands' place)
   bool summed = !b.db;
   Operand G[2] = {};                  // [bf16]
   for (int bf16 = 0; bf16 < 2; ++bf16) {
@@ -1583,6 +1616,26 @@ BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
   if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums);
   if (x) p.x.B = p.lay.plane(p.x.B, x_bf16, p.x.J, p.x.Kc, few_tiles(p.x));
   if (w) p.w.B = p.lay.plane(p.w.B, w_bf16, p.w.J, p.w.Kc, few_tiles(p.w));
+  return p;
+}
+BackwardPlan backward_plan(const BackwardArgs& b, char* base) {
+  const Product qx = input_product(b), qw = weight_product(b);
+  const bool x = b.dX && wide_sizes(qx), w = b.dW && wide_sizes(qw);
+  // the instructions of both products together: they share the layouts of G
+  bool x_bf16 = may_bf16(qx), w_bf16 = may_bf16(qw);
+  if ((x && x_bf16 && may_float(qx)) || (w && w_bf16 && may_float(qw))) {
+    double best = 0.0;
+    for (int c = 3; c >= 0; --c) {
+      const bool xb = c & 1, wb = c & 2;
+      if (x ? !(xb ? may_bf16(qx) : may_float(qx)) : xb) continue;
+      if (w ? !(wb ? may_bf16(qw) : may_float(qw)) : wb) continue;
+      const BackwardPlan p = lay_backward(b, nullptr, xb, wb);
+      const double us = (layout_us(p.lay) + (x ? product_us(p.x) : 0.0) + (w ? product_us(p.w) : 0.0)) *
+                        ((x && !xb && may_bf16(qx)) || (w && !wb && may_bf16(qw)) ? AHEAD : 1.0);
+      if (best == 0.0 || us < best) { best = us; x_bf16 = xb; w_bf16 = wb; }
+    }
+  }
+  BackwardPlan p = lay_backward(b, base, x_bf16, w_bf16);
   p.pair = x && w && pairs(p.w, p.x);
   const size_t nx = b.dX ? up(parts_workspace(p.x)) : 0, nw = b.dW ? up(parts_workspace(p.w)) : 0;
   p.partial_x = base + p.lay.bytes;
@@ -1664,7 +1717,7 @@ size_t product_workspace(const Product& q) {
   if (!wide_sizes(q)) return parts_workspace(q);
   Layout l = {};
   Product p = q;
-  const bool bf16 = on_bf16(q);
+  const bool bf16 = forward_bf16(q);
   p.A = l.plane(q.A, bf16, q.I, q.Kc, few_tiles(q));
   p.B = l.plane(q.B, bf16, q.J, q.Kc, few_tiles(q));
   return l.bytes + parts_workspace(p);
@@ -1680,7 +1733,7 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s) {
   Layout l = {};
   l.base = static_cast<char*>(ws);
   Product p = q;
-  const bool bf16 = on_bf16(q);
+  const bool bf16 = forward_bf16(q);
   p.A = l.plane(q.A, bf16, q.I, q.Kc, few_tiles(q));
   p.B = l.plane(q.B, bf16, q.J, q.Kc, few_tiles(q));
   const hipError_t e = l.launch(s);

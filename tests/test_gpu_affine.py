@@ -482,3 +482,13 @@ def test_products_whose_first_parts_pass_the_largest_float(types, rows, K, F):
     want = v @ w.T
     assert bool((a.X.bfloat16().double().abs() == 2.0 ** 65).all()) and float(want.abs().max()) < 2.0 ** 128
     assert torch.equal(a.forward()[0].double(), want)
+
+
+# large products with a short side, where the instructions are chosen by bytes as well: either way, mixed within a backward pass
+@pytest.mark.parametrize("types", ["fff", "fbf"])
+@pytest.mark.parametrize("rows,K,F", [(6300, 56, 20300), (4100, 300, 5000), (110, 8200, 8300), (8200, 8300, 110), (20000, 200, 600)])
+def test_large_products_with_a_short_side(rows, K, F, types):
+    a = Affine(rows, K, F, types, "tanh", 0.5, residual=True)
+    _, D = a.check_forward(factor=True)
+    a.check_backward(D)
+    Affine(rows, K, F, types, "identity", 0.7, seed=3).check_backward(None)
