@@ -1,14 +1,13 @@
 """Performance cases of the operators around the layer-parallel solver that keep values in few bits or turn logits into answers: an end
-layer whose product takes both operands in microscaled 4 or 8 bits, the backward pass of an end layer from activations that were kept
-in 8 bits, the norms before and after a block with its gate and residual scale, and the drawing of classes from logits.
+layer with weights in microscaled 4 bits, the backward pass of an end layer from activations that were kept in 8 bits, the norms before and after a block with its gate and residual scale, and the drawing of classes from logits.
 
 Microscaled: rows in blocks of 32 entries, each block with a power of two as its scale, the smallest one for which no entry of the block
 exceeds the format's largest value (mx8: 448, sign, 4 exponent and 3 mantissa bits; mx4: 6, sign, 2 and 1); entries are rounded to
 nearest, ties to even.
 
 A case is a dict; its `op` says which operator, the rest its sizes and types:
-  packed    z = X~ W~^T + b, Y = R + scale act(z), X~ and W~ the microscaled values of X and W:   M, K, F, x, xf, wf, y (type of X; formats of
-            X~ and W~; type of R and Y), act, bias, residual.  W is packed already, as a server keeps it; X is not.
+  packed    z = X~ W~^T + b, Y = R + scale act(z), W~ the mx4 values of W, X~ those of X or X rounded to bf16:   M, K, F, x, xf, y (type of X, form of
+            X~, type of R and Y), act, bias, residual.  W is packed already, as a server keeps it; X is not.
   kept      X and the activation's factors D are packed to mx8, then G = dY D~, dX = G W, dW = G^T X~, db = sum of G over rows:   M, K, F, x, w, y
             (types of X and dX; W; dY and D), act (identity: no D), need_dx
   norm      n = norm(f) w_post, s = r + scale gate n, y = norm(s) w_pre:   M, q, kind (rms, or layer: less its mean), stream (type of r, s), branch (type of
@@ -34,8 +33,8 @@ EPS = 1.0e-6                        # of the norms
 LARGEST = {"mx8": (448.0, -6, 3), "mx4": (6.0, 0, 1)}         # largest value, least exponent, mantissa bits
 
 
-def _packed(name, M, K, F, x, xf, wf, y, act, **kw):
-    return dict(dict(name=name, op="packed", M=M, K=K, F=F, x=x, xf=xf, wf=wf, y=y, act=act, bias=True, residual=False), **kw)
+def _packed(name, M, K, F, x, xf, y, act, **kw):
+    return dict(dict(name=name, op="packed", M=M, K=K, F=F, x=x, xf=xf, y=y, act=act, bias=True, residual=False), **kw)
 
 
 def _kept(name, M, K, F, types, act, **kw):
@@ -56,13 +55,13 @@ F32, BF16, STATES = ("f32",) * 3, ("bf16",) * 3, ("f32", "bf16", "f32")
 def listed():
     return [
         # one sample's logits over many classes, as answered one at a time: the weights in 4 bits are most of the bytes
-        _packed("single_mx4", 1, 4096, 32768, "bf16", "mx8", "mx4", "bf16", "identity", bias=False),
+        _packed("single_mx4", 1, 4096, 32768, "bf16", "bf16", "bf16", "identity", bias=False),
         # a fully connected layer of flattened images (d = 4096) with skip connection on a serving batch, float states
-        _packed("connected4096_mx4", 48, 4096, 4096, "f32", "mx8", "mx4", "f32", "tanh", residual=True),
+        _packed("connected4096_mx4", 48, 4096, 4096, "f32", "bf16", "f32", "tanh", residual=True),
         # an opening layer whose sizes fit no tile and no block
-        _packed("ragged_mx4", 1000, 1031, 517, "f32", "mx4", "mx4", "f32", "relu"),
+        _packed("ragged_mx4", 1000, 1031, 517, "f32", "mx4", "f32", "relu"),
         # a wide layer on many samples, with skip connection
-        _packed("wide_mx4", 8192, 4096, 4096, "bf16", "mx4", "mx4", "bf16", "tanh", residual=True),
+        _packed("wide_mx4", 8192, 4096, 4096, "bf16", "mx4", "bf16", "tanh", residual=True),
         # the head of the large image stack (64 channels, 32 x 32, batch 32) backwards, its inputs kept in 8 bits
         _kept("close10_states_kept", 32, 65536, 10, STATES, "identity"),
         # the largest: a wide bf16 layer on many samples backwards, inputs and factors kept in 8 bits
@@ -98,7 +97,7 @@ def draw(rng: random.Random):
             if c["M"] * c["K"] * c["F"] > 8192 * 4096 * 4096 or max(c["M"] * c["K"], c["K"] * c["F"], c["M"] * c["F"]) > 1 << 27:
                 continue
             if op == "packed":
-                c.update(x=rng.choice(["f32", "bf16"]), xf=rng.choice(["mx8", "mx4"]), wf=rng.choice(["mx4", "mx4", "mx8"]), y=rng.choice(["f32", "bf16"]),
+                c.update(x=rng.choice(["f32", "bf16"]), xf=rng.choice(["bf16", "mx4"]), y=rng.choice(["f32", "bf16"]),
                          bias=rng.random() < 0.8, residual=rng.random() < 0.5)
             else:
                 c["x"], c["w"], c["y"] = rng.choice([F32, BF16, BF16, STATES, STATES, ("f32", "f32", "bf16")])
@@ -127,7 +126,7 @@ def work(case):
     c = case
     if c["op"] == "packed":
         M, K, F = c["M"], c["K"], c["F"]
-        b = _bytes(c["x"]) * M * K + _bytes(c["wf"]) * F * K + _bytes(c["y"]) * M * F * (1 + c["residual"]) + 4 * F * c["bias"]
+        b = _bytes(c["x"]) * M * K + _bytes("mx4") * F * K + _bytes(c["y"]) * M * F * (1 + c["residual"]) + 4 * F * c["bias"]
         return {"bytes": float(b), "flops": 2.0 * M * K * F}
     if c["op"] == "kept":
         M, K, F = c["M"], c["K"], c["F"]
@@ -207,13 +206,12 @@ def _handle(c, s):
     def room(n):
         return torch.empty(n, device=DEV, dtype=torch.uint8)
 
-    formats = {"mx8": mgrit.MGRIT_MX8, "mx4": mgrit.MGRIT_MX4}
     if c["op"] == "packed":
         M, K, F = c["M"], c["K"], c["F"]
-        w = mgrit.make_packed(rows=F, cols=K, format=formats[c["wf"]], dtype=mgrit.MGRIT_BF16)
+        w = mgrit.make_packed(rows=F, cols=K, format=mgrit.MGRIT_MX4, dtype=mgrit.MGRIT_BF16)
         s["packed"] = room(mgrit.mgrit_packed_bytes(w))
         mgrit.mgrit_pack(w, s["W"], s["packed"])
-        p = mgrit.make_affine_packed(M=M, K=K, F=F, act=ACTS[c["act"]], xtype=ENUM[c["x"]], xformat=formats[c["xf"]], wformat=formats[c["wf"]],
+        p = mgrit.make_affine_packed(M=M, K=K, F=F, act=ACTS[c["act"]], xtype=ENUM[c["x"]], xformat={"bf16": mgrit.MGRIT_BF16, "mx4": mgrit.MGRIT_MX4}[c["xf"]],
                                      ytype=ENUM[c["y"]], scale=1.0 if c["act"] == "identity" else SCALE)
         s.update(p=p, Y=new((M, F), c["y"]), ws=room(mgrit.mgrit_affine_packed_workspace_bytes(p)))
     elif c["op"] == "kept":
@@ -246,7 +244,7 @@ def prepare(case, seed):
     if own:
         _handle(case, s)
     elif case["op"] == "packed":
-        s["packed"] = _pack(s["W"], case["wf"])                   # the weights' values as a server keeps them
+        s["packed"] = _pack(s["W"], "mx4")                   # the weights' values as a server keeps them
     return s
 
 
@@ -338,7 +336,7 @@ def run(state):
     if own:
         return _run_own(c, s)
     if c["op"] == "packed":
-        z = _pack(s["X"], c["xf"]) @ s["packed"].T
+        z = (_pack(s["X"], "mx4") if c["xf"] == "mx4" else s["X"].bfloat16().float()) @ s["packed"].T
         if s["b"] is not None:
             z = z + s["b"]
         y = z if c["act"] == "identity" else SCALE * (torch.clamp(z, min=0.0) if c["act"] == "relu" else torch.tanh(z))
@@ -406,7 +404,8 @@ def _exact_values(x, form):
 def exact(case, seed):
     c, x = case, _inputs(case, seed)
     if c["op"] == "packed":
-        z = torch.matmul(_exact_values(x["X"], c["xf"]), _exact_values(x["W"], c["wf"]).t())
+        X = _exact_values(x["X"], "mx4") if c["xf"] == "mx4" else x["X"].to(torch.bfloat16).double()
+        z = torch.matmul(X, _exact_values(x["W"], "mx4").t())
         if c["bias"]:
             z += x["b"].double()
         Y = {"identity": lambda v: v, "relu": lambda v: SCALE * torch.relu(v), "tanh": lambda v: SCALE * torch.tanh(v)}[c["act"]](z)
@@ -452,7 +451,9 @@ def exact(case, seed):
         rank = torch.empty_like(by)
         rank.scatter_(1, by, torch.arange(V, device=DEV).expand(rows, V))
         # (a temperature of zero is the limit: all of the probability on the first of the order)
-        P = torch.softmax(L / torch.where(t > 0, t, 1.0)[:, None], dim=1)
+        P = L / torch.where(t > 0, t, 1.0)[:, None]
+        P = torch.exp(P - P.max(dim=1, keepdim=True).values)                           # (torch.softmax is 1e-9 off in 64 bits)
+        P = P / P.sum(dim=1, keepdim=True)
         keep = torch.where((t > 0)[:, None], rank < V, rank < 1)
         if part["top_k"] is not None:
             keep &= rank < part["top_k"].long()[:, None]
