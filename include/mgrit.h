@@ -318,6 +318,110 @@ size_t  mgrit_clip_workspace_bytes(const mgrit_tensor_t* tensors, int32_t n);
 int32_t mgrit_clip_gradients(const mgrit_tensor_t* tensors, int32_t n, float max_norm, float* norm, double* norm_host,
                              void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- Values in few bits.  A packed array holds rows in blocks of 32 entries, each block with a power of two as its scale: the smallest
+ * 2^s, s >= -127, for which no entry of the block exceeds the format's largest value times 2^s.  Entries are divided by it (exactly) and rounded
+ * to nearest, ties to even; nothing is cut off.  A block that holds an infinity or a NaN is NaN throughout.
+ *   MGRIT_MX8   sign, 4 exponent and 3 mantissa bits (bias 7), largest value 448, smallest 2^-9; a byte each
+ *   MGRIT_MX4   sign, 2 exponent and 1 mantissa bits (bias 1): 0 .5 1 1.5 2 3 4 6; two in a byte, the first in its low half
+ * Layout, with C = cols rounded up to a multiple of 256: codes [rows][C] (MX4: C / 2 bytes a row), and from the next multiple of 256 bytes on
+ * scales [C / 256][rows][8], a byte s + 127 each (255: NaN), the eight in the order of blocks 0 2 4 6 1 3 5 7.  Entries
+ * behind the last column are zero.  Scales lie so that the matrix instructions' lanes find theirs side by side. */
+enum { MGRIT_MX8 = 8, MGRIT_MX4 = 4 };
+typedef struct mgrit_packed {
+  int32_t rows, cols;  /* rows >= 0, cols >= 1                                                                   */
+  int32_t format;      /* MGRIT_MX8 or MGRIT_MX4                                                                 */
+  int32_t dtype;       /* of the unpacked values: MGRIT_FP32 or MGRIT_BF16                                       */
+} mgrit_packed_t;
+
+/* Bytes of the packed array, a multiple of 256; 0 if it is invalid or has no rows. */
+size_t  mgrit_packed_bytes(const mgrit_packed_t* p);
+/* packed (device, aligned to 256 bytes) <- X [rows][cols], and back (to bf16 a value below 2^-126 in magnitude is rounded, and
+ * a largest float that was rounded up to 2^128 is an infinity; everything else is exact).
+ * Errors: MGRIT_ERR_POINTER, _PROBLEM, _HIP; MGRIT_ERR_UNSUPPORTED if rows * (cols rounded up to a multiple of 256) exceeds 2^38. */
+int32_t mgrit_pack(const mgrit_packed_t* p, const void* X, void* packed, void* hip_stream);
+int32_t mgrit_unpack(const mgrit_packed_t* p, const void* packed, void* X, void* hip_stream);
+
+/* The affine layer of mgrit_affine_forward with packed weights:
+ *   z = X~ W~^T + b,  Y = R + scale act(z),  D = scale act'(z)
+ * W~ the values of W [F][K] packed as MGRIT_MX4.  X [M][K] is of type xtype; X~ are with xformat = MGRIT_BF16 its values rounded to bf16 (of bf16
+ * arrays: as they are), with MGRIT_MX4 the values that packing it would give (then the products are those of 4-bit values, and exact).
+ * Sums are float.  R, Y, D ytype, b float, as there. */
+typedef struct mgrit_affine_packed {
+  int32_t M;           /* rows (samples), >= 0                                                                   */
+  int32_t K, F;        /* inputs and outputs per row, >= 1                                                       */
+  int32_t act;         /* MGRIT_ACT_TANH, _RELU or _IDENTITY                                                     */
+  int32_t xtype, xformat, ytype;
+  float   scale;       /* finite                                                                                 */
+} mgrit_affine_packed_t;
+
+size_t  mgrit_affine_packed_workspace_bytes(const mgrit_affine_packed_t* p);
+/*   W   device, packed, read only (256-byte aligned)      X, b, R, Y, D as in mgrit_affine_forward
+ * Errors as there, and MGRIT_ERR_UNSUPPORTED if K exceeds 2^22. */
+int32_t mgrit_affine_packed_forward(const mgrit_affine_packed_t* p, const void* X, const void* W, const float* b, const void* R,
+                                    void* Y, void* D, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The backward pass of an affine layer from activations that were kept in 8 bits: mgrit_affine_backward with X [M][K] and D [M][F]
+ * packed as MGRIT_MX8 (a quarter of a float state's memory between the passes, half of a bf16 one's), p->xtype the type of dX alone.
+ *   G = dY * D~ (D NULL: G = scale dY, for the identity only),  dX = G W,  dW = G^T X~,  db = sum over the rows of G
+ * X~ and D~ enter as they are packed, but that values of X~ below 2^-126 are rounded to bf16. */
+size_t  mgrit_affine_kept_workspace_bytes(const mgrit_affine_t* p);
+int32_t mgrit_affine_kept_backward(const mgrit_affine_t* p, const void* X, const void* W, const void* D, const void* dY,
+                                   void* dX, float* dW, float* db, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- The norms after and before a block, with its gate and residual step: from the stream r and a block's result f
+ *   n = norm(f) w_post,   S = r + scale gate n,   Y = norm(S) w_pre                 f, r, S, Y [M][q], w_post, w_pre [q]
+ * S is the stream behind the block, Y what the next block takes.  norm(x) = x / sqrt(mean(x^2) + eps), or with MGRIT_NORM_LAYER the same of
+ * x less its mean, over the q features of a row.  w_post NULL: n = f; w_pre NULL: no Y.  The gate is absent, one value a feature
+ * (float [q]) or one an entry ([M][q], type ftype).  r, S (and dS, dr) are of type stype, f, Y (and df, dY) of type ftype, weights and their
+ * gradients float.  Y comes from S before that is rounded to its type.  With eps = 0 a row without deviation gives NaN. */
+enum { MGRIT_NORM_ROOT = 0, MGRIT_NORM_LAYER = 1 };
+enum { MGRIT_GATE_NONE = 0, MGRIT_GATE_FEATURE = 1, MGRIT_GATE_ENTRY = 2 };
+typedef struct mgrit_block_norm {
+  int32_t M, q;        /* rows >= 0, features >= 1                                                               */
+  int32_t kind;        /* MGRIT_NORM_ROOT or MGRIT_NORM_LAYER                                                    */
+  int32_t gate;        /* MGRIT_GATE_NONE, _FEATURE or _ENTRY                                                    */
+  int32_t stype, ftype;
+  float   eps;         /* >= 0, finite                                                                           */
+  float   scale;       /* finite                                                                                 */
+} mgrit_block_norm_t;
+
+/*   S    device, out; may be r                    Y    device, out; NULL exactly if w_pre is.  May be f
+ * Errors: MGRIT_ERR_POINTER, _PROBLEM, _HIP; MGRIT_ERR_UNSUPPORTED if M * q exceeds 2^38. */
+int32_t mgrit_block_norm_forward(const mgrit_block_norm_t* p, const void* f, const void* r, const void* gate, const float* w_post,
+                                 const float* w_pre, void* S, void* Y, void* hip_stream);
+/* Backwards, from f, gate, S and the gradients by S (from what else uses the stream; NULL: none) and by Y (NULL exactly if w_pre is):
+ *   dr = dS + the gradient by S through Y,   df, dgate (type and shape of the gate), dw_post, dw_pre float [q]
+ * dr is the whole gradient by S, which is that by r.  Each output may be NULL if it is not wanted.  dr may be dS, df may be dY or f.
+ * Without rows the gradients of vectors are written as zero. */
+size_t  mgrit_block_norm_workspace_bytes(const mgrit_block_norm_t* p);
+int32_t mgrit_block_norm_backward(const mgrit_block_norm_t* p, const void* f, const void* S, const void* gate, const float* w_post,
+                                  const float* w_pre, const void* dS, const void* dY, void* df, void* dr, void* dgate, float* dw_post,
+                                  float* dw_pre, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- Answers: one class for each row of logits x [B][V] from a given random number u in [0, 1).  With the row's temperature t the
+ * weights are w_v = exp((x_v - max x) / t).  The classes in falling order of their logits, equal ones lowest index first, are narrowed to
+ *   top_k   the first k (k <= 0 or k >= V: all)
+ *   top_p   of these the first ones up to where their weights reach p times the sum of all of these (p >= 1: all; p <= 0: the first)
+ *   min_p   those with w_v >= min_p (<= 0: all; above 1: as 1)
+ * all three; index <- the first class v in the order of indices for which the kept weights up to and with v sum to more than u times all
+ * kept weights, logprob <- log(w_v / the sum of the kept weights).  t = 0: the largest logit, lowest index first, logprob 0.
+ * Logits of minus infinity have weight zero.  A row that holds a NaN, +infinity or nothing but minus infinity, or whose t is negative, infinite or NaN, whose u is
+ * not in [0, 1), or whose top_p or min_p is NaN, gives index -1 and logprob NaN.
+ * Weights are computed to 1e-13 and summed as integers, 2^-(62 - log2 V) each: the same class every time, however the sums are formed. */
+typedef struct mgrit_sample {
+  int32_t B, V;        /* rows >= 0, classes >= 1                                                                */
+  int32_t dtype;       /* of the logits: MGRIT_FP32 or MGRIT_BF16                                                */
+} mgrit_sample_t;
+
+/* 0: none is needed in this build (then the workspace pointer may be NULL) */
+size_t  mgrit_sample_workspace_bytes(const mgrit_sample_t* p);
+/*   logits  device, read only                     u          device float [B]
+ *   temperature, top_p, min_p  device float [B], top_k  device int32 [B], each NULL if no row asks for it (t = 1)
+ *   index   device int64 [B], out                 logprob    device float [B] or NULL
+ * Errors: MGRIT_ERR_POINTER, _PROBLEM, _WORKSPACE, _HIP; MGRIT_ERR_UNSUPPORTED if B * V exceeds 2^38. */
+int32_t mgrit_sample(const mgrit_sample_t* p, const void* logits, const float* u, const float* temperature, const int32_t* top_k, const float* top_p,
+                     const float* min_p, int64_t* index, float* logprob, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Diagnostic launch tracing, off by default and the one piece of state the library keeps: between
  * mgrit_trace_begin() and mgrit_trace_end() every layer-step and gradient launch is bracketed by a
  * pair of HIP events on its stream.  mgrit_trace_end synchronises on the last event and returns,

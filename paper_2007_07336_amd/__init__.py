@@ -15,4 +15,10 @@ from .binding import (  # noqa: F401
     mgrit_affine_forward, mgrit_affine_backward,
     mgrit_loss_t, make_loss, mgrit_cross_entropy_workspace_bytes, mgrit_cross_entropy,
     mgrit_tensor_t, make_tensor_list, mgrit_clip_workspace_bytes, mgrit_clip_gradients,
+    MGRIT_MX8, MGRIT_MX4, mgrit_packed_t, make_packed, mgrit_packed_bytes, mgrit_pack, mgrit_unpack,
+    mgrit_affine_packed_t, make_affine_packed, mgrit_affine_packed_workspace_bytes, mgrit_affine_packed_forward,
+    mgrit_affine_kept_workspace_bytes, mgrit_affine_kept_backward,
+    MGRIT_NORM_ROOT, MGRIT_NORM_LAYER, MGRIT_GATE_NONE, MGRIT_GATE_FEATURE, MGRIT_GATE_ENTRY,
+    mgrit_block_norm_t, make_block_norm, mgrit_block_norm_workspace_bytes, mgrit_block_norm_forward, mgrit_block_norm_backward,
+    mgrit_sample_t, make_sample, mgrit_sample_workspace_bytes, mgrit_sample,
 )

@@ -56,6 +56,24 @@ class mgrit_tensor_t(ctypes.Structure):
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
+class mgrit_packed_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("format", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class mgrit_affine_packed_t(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int32), ("K", ctypes.c_int32), ("F", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("xtype", ctypes.c_int32), ("xformat", ctypes.c_int32), ("ytype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class mgrit_block_norm_t(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int32), ("q", ctypes.c_int32), ("kind", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("stype", ctypes.c_int32), ("ftype", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class mgrit_sample_t(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -106,6 +124,18 @@ def lib() -> ctypes.CDLL:
         L.mgrit_cross_entropy_workspace_bytes.restype = ctypes.c_size_t
         L.mgrit_cross_entropy.argtypes = [X, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.mgrit_cross_entropy.restype = ctypes.c_int32
+        Q, E, N, S = (ctypes.POINTER(t) for t in (mgrit_packed_t, mgrit_affine_packed_t, mgrit_block_norm_t, mgrit_sample_t))
+        for name, arg in (("mgrit_packed_bytes", Q), ("mgrit_affine_packed_workspace_bytes", E), ("mgrit_affine_kept_workspace_bytes", A),
+                          ("mgrit_block_norm_workspace_bytes", N), ("mgrit_sample_workspace_bytes", S)):
+            getattr(L, name).argtypes = [arg]
+            getattr(L, name).restype = ctypes.c_size_t
+        for name, args in (("mgrit_pack", [Q] + [vp] * 3), ("mgrit_unpack", [Q] + [vp] * 3),
+                           ("mgrit_affine_packed_forward", [E] + [vp] * 7 + [ctypes.c_size_t, vp]),
+                           ("mgrit_affine_kept_backward", [A] + [vp] * 8 + [ctypes.c_size_t, vp]),
+                           ("mgrit_block_norm_forward", [N] + [vp] * 8), ("mgrit_block_norm_backward", [N] + [vp] * 13 + [ctypes.c_size_t, vp]),
+                           ("mgrit_sample", [S] + [vp] * 9 + [ctypes.c_size_t, vp])):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = ctypes.c_int32
         L.mgrit_clip_workspace_bytes.argtypes = [T, ctypes.c_int32]
         L.mgrit_clip_workspace_bytes.restype = ctypes.c_size_t
         L.mgrit_clip_gradients.argtypes = [T, ctypes.c_int32, ctypes.c_float, vp, dp, vp, ctypes.c_size_t, vp]
@@ -469,6 +499,130 @@ def mgrit_clip_gradients(tensors: TensorList, max_norm: float, norm, workspace, 
     rc = _call(where, device, stream, check, lambda s: lib().mgrit_clip_gradients(
         tensors.array, len(tensors), max_norm, _ptr(norm), None if host is None else ctypes.byref(host), _ptr(workspace), _size(workspace), s))
     return rc, None if host is None else host.value
+
+
+# ---- values in few bits, norms around blocks, answers
+MGRIT_MX8, MGRIT_MX4 = 8, 4
+MGRIT_NORM_ROOT, MGRIT_NORM_LAYER = 0, 1
+MGRIT_GATE_NONE, MGRIT_GATE_FEATURE, MGRIT_GATE_ENTRY = 0, 1, 2
+
+
+def _bytes_type():
+    import torch
+    return torch.uint8
+
+
+def make_packed(*, rows, cols, format, dtype=MGRIT_FP32) -> mgrit_packed_t:
+    return mgrit_packed_t(rows=rows, cols=cols, format=format, dtype=dtype)
+
+
+def mgrit_packed_bytes(p: mgrit_packed_t) -> int:
+    return int(lib().mgrit_packed_bytes(ctypes.byref(p)))
+
+
+def _packed_bytes_of(rows, cols, format) -> int:
+    return mgrit_packed_bytes(make_packed(rows=rows, cols=cols, format=format))
+
+
+def mgrit_pack(p: mgrit_packed_t, X, packed, *, stream=None, check=True):
+    """packed (uint8, mgrit_packed_bytes values) <- X [rows][cols]."""
+    where, T = "mgrit_pack", _torch_types()
+    device = _check(where, (("X", X, p.rows * p.cols, _type(T, p.dtype)), ("packed", packed, mgrit_packed_bytes(p), _bytes_type())))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_pack(p, _ptr(X), _ptr(packed), s))
+
+
+def mgrit_unpack(p: mgrit_packed_t, packed, X, *, stream=None, check=True):
+    """X [rows][cols] <- the values of packed."""
+    where, T = "mgrit_unpack", _torch_types()
+    device = _check(where, (("packed", packed, mgrit_packed_bytes(p), _bytes_type()), ("X", X, p.rows * p.cols, _type(T, p.dtype))))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_unpack(p, _ptr(packed), _ptr(X), s))
+
+
+def make_affine_packed(*, M, K, F, act=MGRIT_ACT_IDENTITY, xtype=MGRIT_FP32, xformat=MGRIT_BF16, ytype=MGRIT_FP32, scale=1.0) -> mgrit_affine_packed_t:
+    return mgrit_affine_packed_t(M=M, K=K, F=F, act=act, xtype=xtype, xformat=xformat, ytype=ytype, scale=scale)
+
+
+def mgrit_affine_packed_workspace_bytes(p: mgrit_affine_packed_t) -> int:
+    return int(lib().mgrit_affine_packed_workspace_bytes(ctypes.byref(p)))
+
+
+def mgrit_affine_packed_forward(p: mgrit_affine_packed_t, X, W, b, R, Y, D, workspace, *, stream=None, check=True):
+    """mgrit_affine_forward with W [F][K] packed as MGRIT_MX4; X as its type, rounded to bf16 or packed on the way as p.xformat says."""
+    where, T = "mgrit_affine_packed_forward", _torch_types()
+    M, K, F, y = p.M, p.K, p.F, _type(T, p.ytype)
+    device = _check(where, (("X", X, M * K, _type(T, p.xtype)), ("W", W, _packed_bytes_of(F, K, MGRIT_MX4), _bytes_type()), ("b", b, F, T[0]),
+                            ("R", R, M * F, y), ("Y", Y, M * F, y), ("D", D, M * F, y), _workspace(workspace)))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_affine_packed_forward(
+        p, _ptr(X), _ptr(W), _ptr(b), _ptr(R), _ptr(Y), _ptr(D), _ptr(workspace), _size(workspace), s))
+
+
+def mgrit_affine_kept_workspace_bytes(p: mgrit_affine_t) -> int:
+    return int(lib().mgrit_affine_kept_workspace_bytes(ctypes.byref(p)))
+
+
+def mgrit_affine_kept_backward(p: mgrit_affine_t, X, W, D, dY, dX, dW, db, workspace, *, stream=None, check=True):
+    """mgrit_affine_backward with X [M][K] and D [M][F] (None: identity only) packed as MGRIT_MX8."""
+    where, T = "mgrit_affine_kept_backward", _torch_types()
+    M, K, F, y = p.M, p.K, p.F, _type(T, p.ytype)
+    device = _check(where, (("X", X, _packed_bytes_of(M, K, MGRIT_MX8), _bytes_type()), ("W", W, F * K, _type(T, p.wtype)),
+                            ("D", D, _packed_bytes_of(M, F, MGRIT_MX8), _bytes_type()), ("dY", dY, M * F, y), ("dX", dX, M * K, _type(T, p.xtype)),
+                            ("dW", dW, F * K, T[0]), ("db", db, F, T[0]), _workspace(workspace)))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_affine_kept_backward(
+        p, _ptr(X), _ptr(W), _ptr(D), _ptr(dY), _ptr(dX), _ptr(dW), _ptr(db), _ptr(workspace), _size(workspace), s))
+
+
+def make_block_norm(*, M, q, kind=MGRIT_NORM_ROOT, gate=MGRIT_GATE_NONE, stype=MGRIT_FP32, ftype=MGRIT_FP32, eps=1.0e-6, scale=1.0) -> mgrit_block_norm_t:
+    return mgrit_block_norm_t(M=M, q=q, kind=kind, gate=gate, stype=stype, ftype=ftype, eps=eps, scale=scale)
+
+
+def _gate(p, T):
+    """Number of values and type of the gate."""
+    return (p.q, T[0]) if p.gate == MGRIT_GATE_FEATURE else (p.M * p.q, _type(T, p.ftype))
+
+
+def mgrit_block_norm_forward(p: mgrit_block_norm_t, f, r, gate, w_post, w_pre, S, Y, *, stream=None, check=True):
+    """S = r + scale gate norm(f) w_post, Y = norm(S) w_pre: w_post may be None (no norm of f), w_pre and Y (no norm of S), gate as p.gate says."""
+    where, T = "mgrit_block_norm_forward", _torch_types()
+    n, s_, f_ = p.M * p.q, _type(T, p.stype), _type(T, p.ftype)
+    device = _check(where, (("f", f, n, f_), ("r", r, n, s_), ("gate", gate) + _gate(p, T), ("w_post", w_post, p.q, T[0]), ("w_pre", w_pre, p.q, T[0]),
+                            ("S", S, n, s_), ("Y", Y, n, f_)))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_block_norm_forward(
+        p, _ptr(f), _ptr(r), _ptr(gate), _ptr(w_post), _ptr(w_pre), _ptr(S), _ptr(Y), s))
+
+
+def mgrit_block_norm_workspace_bytes(p: mgrit_block_norm_t) -> int:
+    return int(lib().mgrit_block_norm_workspace_bytes(ctypes.byref(p)))
+
+
+def mgrit_block_norm_backward(p: mgrit_block_norm_t, f, S, gate, w_post, w_pre, dS, dY, df, dr, dgate, dw_post, dw_pre, workspace, *, stream=None, check=True):
+    """The gradients by f, r, gate, w_post and w_pre from those by S (dS, None: zero) and Y (dY, None exactly if w_pre is); each may be None."""
+    where, T = "mgrit_block_norm_backward", _torch_types()
+    n, s_, f_ = p.M * p.q, _type(T, p.stype), _type(T, p.ftype)
+    device = _check(where, (("f", f, n, f_), ("S", S, n, s_), ("gate", gate) + _gate(p, T), ("w_post", w_post, p.q, T[0]), ("w_pre", w_pre, p.q, T[0]),
+                            ("dS", dS, n, s_), ("dY", dY, n, f_), ("df", df, n, f_), ("dr", dr, n, s_), ("dgate", dgate) + _gate(p, T),
+                            ("dw_post", dw_post, p.q, T[0]), ("dw_pre", dw_pre, p.q, T[0]), _workspace(workspace)))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_block_norm_backward(
+        p, _ptr(f), _ptr(S), _ptr(gate), _ptr(w_post), _ptr(w_pre), _ptr(dS), _ptr(dY), _ptr(df), _ptr(dr), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre),
+        _ptr(workspace), _size(workspace), s))
+
+
+def make_sample(*, B, V, dtype=MGRIT_FP32) -> mgrit_sample_t:
+    return mgrit_sample_t(B=B, V=V, dtype=dtype)
+
+
+def mgrit_sample_workspace_bytes(p: mgrit_sample_t) -> int:
+    return int(lib().mgrit_sample_workspace_bytes(ctypes.byref(p)))
+
+
+def mgrit_sample(p: mgrit_sample_t, logits, u, temperature, top_k, top_p, min_p, index, logprob, workspace, *, stream=None, check=True):
+    """index [B] (int64) <- a class for each row, by u [B] in [0, 1); temperature, top_k (int32), top_p, min_p [B] and logprob [B] may be None."""
+    import torch
+    where, T, B = "mgrit_sample", _torch_types(), p.B
+    device = _check(where, (("logits", logits, B * p.V, _type(T, p.dtype)), ("u", u, B, T[0]), ("temperature", temperature, B, T[0]),
+                            ("top_k", top_k, B, torch.int32), ("top_p", top_p, B, T[0]), ("min_p", min_p, B, T[0]), ("index", index, B, T[2]),
+                            ("logprob", logprob, B, T[0]), _workspace(workspace)))
+    return _call(where, device, stream, check, lambda s: lib().mgrit_sample(
+        p, _ptr(logits), _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(index), _ptr(logprob), _ptr(workspace), _size(workspace), s))
 
 
 TRACE_CLASSES = ("dense_step_kernel<float,64,64>", "dense_step_kernel<float,128,128>",

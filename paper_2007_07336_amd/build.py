@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmgrit.so")
 SOURCES = ["mgrit_api.hip", "mgrit_kernels.hip", "mgrit_conv_grad.hip", "mgrit_sweep.hip", "mgrit_wave.hip", "mgrit_wide.hip",
-           "mgrit_ops_api.hip", "mgrit_affine.hip", "mgrit_loss.hip", "mgrit_clip.hip"]
+           "mgrit_ops_api.hip", "mgrit_affine.hip", "mgrit_loss.hip", "mgrit_clip.hip", "mgrit_packed.hip", "mgrit_norm.hip",
+           "mgrit_sample.hip"]
 
 
 def hipcc() -> str:

@@ -1,0 +1,418 @@
+// The norms after and before a block with its gate and residual step, and their backward pass.
+#include "mgrit_epilogue.h"
+
+namespace mgrit {
+
+namespace {
+
+constexpr long long MOST_ROWS = 1LL << 21;                       // of one launch: fewer than 2^32 threads
+
+// Sums over the TH threads of a workgroup; all threads get them.  sh: two places in turn (one barrier each).
+template <int TH, int N> __device__ __forceinline__ void sum_threads(float (&v)[N], float (&sh)[2][TH / 64][4], int& place) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d);
+  if constexpr (TH > 64) {
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) sh[place][threadIdx.x >> 6][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = sh[place][0][i];
+#pragma unroll
+    for (int w = 1; w < TH / 64; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += sh[place][w][i];
+    place ^= 1;
+  }
+}
+// Eight entries of a row from column k on; zeros where there are none
+template <typename T> __device__ __forceinline__ void take8(const T* p, long long k, long long q, float (&v)[8]) {
+  if (k + 8 <= q) {
+    load8(p + k, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = k + j < q ? widen(p[k + j]) : 0.0f;
+  }
+}
+template <typename T> __device__ __forceinline__ void give8(T* p, long long k, long long q, const float (&v)[8]) {
+  if (k < q) put8(p + k, v, k + 8 <= q, q - k);
+}
+// d for entries that exist, zero behind them (of sums of deviations, which are not zero there)
+__device__ __forceinline__ float there(float d, long long k, long long q) { return k < q ? d : 0.0f; }
+
+// One row per workgroup of TH threads.  NV > 0: the row's eights fit NV registers sets of each thread and are read once; NV = 0: they are read again
+// for every step.  A row's entries are only ever touched by the thread that writes them, so S may take r's place and Y f's.
+template <typename ST, typename FT, int TH, int NV>
+__global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long long first) {
+  __shared__ float sh[2][TH / 64][4];
+  int place = 0;
+  const long long row = first + blockIdx.x, q = a.q;
+  const FT* f = static_cast<const FT*>(a.f) + row * q;
+  const ST* r = static_cast<const ST*>(a.r) + row * q;
+  const FT* entry = a.gate_kind == MGRIT_GATE_ENTRY ? static_cast<const FT*>(a.gate) + row * q : nullptr;
+  const float* feature = a.gate_kind == MGRIT_GATE_FEATURE ? static_cast<const float*>(a.gate) : nullptr;
+  const int n = NV > 0 ? NV : (int)((q + 8 * TH - 1) / (8 * TH));
+  constexpr int HELD = NV > 0 ? NV : 1, U = HELD;
+  const float inv = 1.0f / (float)q;
+  float x[HELD][8], y[HELD][8];
+  auto at = [&](int i) { return ((long long)i * TH + threadIdx.x) * 8; };
+  auto read_f = [&](int i) { if (NV == 0) take8(f, at(i), q, x[0]); };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) take8(f, at(i), q, x[i]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) take8(r, at(i), q, y[i]);
+  }
+  float mean = 0.0f, dev = 1.0f;
+  if (a.post) {
+    if (a.layer) {
+      float s[1] = {};
+#pragma unroll U
+      for (int i = 0; i < n; ++i) {
+        read_f(i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] += x[NV ? i : 0][j];
+      }
+      sum_threads<TH>(s, sh, place);
+      mean = s[0] * inv;
+    }
+    float s[1] = {};
+#pragma unroll U
+    for (int i = 0; i < n; ++i) {
+      read_f(i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { const float d = there(x[NV ? i : 0][j] - mean, at(i) + j, q); s[0] += d * d; }
+    }
+    sum_threads<TH>(s, sh, place);
+    dev = 1.0f / sqrtf(s[0] * inv + a.eps);
+  }
+  // y <- S
+  auto stream = [&](int i) {
+    const int h = NV ? i : 0;
+    float g[8], w[8];
+    if (NV == 0) { take8(f, at(i), q, x[0]); take8(r, at(i), q, y[0]); }
+    if (a.post) take8(a.post, at(i), q, w);
+    if (entry) take8(entry, at(i), q, g);
+    if (feature) take8(feature, at(i), q, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float m = a.post ? (x[h][j] - mean) * dev * w[j] : x[h][j];
+      y[h][j] += a.scale * (entry || feature ? g[j] * m : m);
+    }
+  };
+  float smean = 0.0f, sdev = 1.0f;
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      stream(i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[i][j] = there(y[i][j], at(i) + j, q);
+    }
+  }
+  if (a.pre) {
+    if (a.layer) {
+      float s[1] = {};
+#pragma unroll U
+      for (int i = 0; i < n; ++i) {
+        if (NV == 0) stream(i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] += there(y[NV ? i : 0][j], at(i) + j, q);
+      }
+      sum_threads<TH>(s, sh, place);
+      smean = s[0] * inv;
+    }
+    float s[1] = {};
+#pragma unroll U
+    for (int i = 0; i < n; ++i) {
+      if (NV == 0) stream(i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { const float d = there(y[NV ? i : 0][j] - smean, at(i) + j, q); s[0] += d * d; }
+    }
+    sum_threads<TH>(s, sh, place);
+    sdev = 1.0f / sqrtf(s[0] * inv + a.eps);
+  }
+#pragma unroll U
+  for (int i = 0; i < n; ++i) {
+    const int h = NV ? i : 0;
+    if (NV == 0) stream(i);
+    give8(static_cast<ST*>(a.S) + row * q, at(i), q, y[h]);
+    if (!a.pre) continue;
+    float w[8];
+    take8(a.pre, at(i), q, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] *= (y[h][j] - smean) * sdev;
+    give8(static_cast<FT*>(a.Y) + row * q, at(i), q, w);
+  }
+}
+
+// The backward pass.  With x^ the normalised rows, h the gradient by x^ and d the reciprocal deviation, the gradient by x is
+// d (h - x^ mean(h x^)), with MGRIT_NORM_LAYER less mean(h) inside the brackets too.  A workgroup takes the rows b, b + G, .. and keeps the columns' sums
+// of its rows in registers; they go to part[array][b][q] and are added up by a second launch.
+struct ColumnSums { float* part[3]; };                           // of dw_pre, dw_post, dgate; null where not wanted
+template <typename ST, typename FT, int TH, int NV>
+__global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, ColumnSums sums) {
+  __shared__ float sh[2][TH / 64][4];
+  int place = 0;
+  const long long q = a.q;
+  const float* feature = a.gate_kind == MGRIT_GATE_FEATURE ? static_cast<const float*>(a.gate) : nullptr;
+  const bool entries = a.gate_kind == MGRIT_GATE_ENTRY, gated = entries || feature;
+  const int n = NV > 0 ? NV : (int)((q + 8 * TH - 1) / (8 * TH));
+  constexpr int HELD = NV > 0 ? NV : 1, U = HELD;
+  const float inv = 1.0f / (float)q;
+  float x[HELD][8], s[HELD][8], ds[HELD][8], h[HELD][8];         // f, S, the gradient by S, that by S's normalised row
+  float cpre[HELD][8] = {}, cpost[HELD][8] = {}, cgate[HELD][8] = {};
+  auto at = [&](int i) { return ((long long)i * TH + threadIdx.x) * 8; };
+  for (long long row = blockIdx.x; row < a.M; row += gridDim.x) {
+    const FT* f = static_cast<const FT*>(a.f) + row * q;
+    const ST* S = static_cast<const ST*>(a.r) + row * q;
+    const ST* dS = a.dS ? static_cast<const ST*>(a.dS) + row * q : nullptr;
+    const FT* dY = a.dY ? static_cast<const FT*>(a.dY) + row * q : nullptr;
+    const FT* entry = entries ? static_cast<const FT*>(a.gate) + row * q : nullptr;
+    const bool first = row == blockIdx.x;
+    auto load = [&](int i) {
+      const int k = NV ? i : 0;
+      take8(f, at(i), q, x[k]);
+      if (dS) take8(dS, at(i), q, ds[k]);
+      if (!a.pre) return;
+      take8(S, at(i), q, s[k]);
+      take8(dY, at(i), q, h[k]);
+    };
+    auto weigh = [&](int i) {                                    // h <- dY w_pre
+      const int k = NV ? i : 0;
+      float w[8];
+      take8(a.pre, at(i), q, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[k][j] *= w[j];
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) load(i);
+    }
+    // sums of f and S (layer), and of h
+    float fmean = 0.0f, smean = 0.0f, hmean = 0.0f;
+    if (a.layer) {
+      float v[3] = {};
+#pragma unroll U
+      for (int i = 0; i < n; ++i) {
+        const int k = NV ? i : 0;
+        if (NV == 0) load(i);
+        float w[8];
+        if (a.pre) take8(a.pre, at(i), q, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[0] += x[k][j];
+          if (a.pre) { v[1] += s[k][j]; v[2] += h[k][j] * w[j]; }
+        }
+      }
+      sum_threads<TH>(v, sh, place);
+      fmean = v[0] * inv; smean = v[1] * inv; hmean = v[2] * inv;
+    }
+    float fdev = 1.0f, sdev = 1.0f, hs = 0.0f;
+    {
+      float v[3] = {};
+#pragma unroll U
+      for (int i = 0; i < n; ++i) {
+        const int k = NV ? i : 0;
+        if (NV == 0) load(i);
+        float w[8];
+        if (a.pre) take8(a.pre, at(i), q, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float d = there(x[k][j] - fmean, at(i) + j, q);
+          v[0] += d * d;
+          if (a.pre) {
+            const float e = there(s[k][j] - smean, at(i) + j, q);
+            v[1] += e * e;
+            v[2] += h[k][j] * w[j] * e;
+          }
+        }
+      }
+      sum_threads<TH>(v, sh, place);
+      if (a.post) fdev = 1.0f / sqrtf(v[0] * inv + a.eps);
+      if (a.pre) { sdev = 1.0f / sqrtf(v[1] * inv + a.eps); hs = v[2] * inv * sdev; }
+    }
+    // ds <- the gradient by S, h <- that by w_pre
+    auto by_stream = [&](int i) {
+      const int k = NV ? i : 0;
+      float w[8];
+      if (a.pre) take8(a.pre, at(i), q, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float d = dS ? ds[k][j] : 0.0f;
+        if (a.pre) {
+          const float sn = (s[k][j] - smean) * sdev, g = h[k][j] * w[j];
+          d += sdev * (g - sn * hs - hmean);
+          h[k][j] *= sn;
+        }
+        ds[k][j] = d;
+      }
+    };
+    // what a block's result gets of it, dn (times w_post): x <- normalised f
+    auto by_block = [&](int i, float (&dn)[8], float (&t)[8]) {
+      const int k = NV ? i : 0;
+      float g[8], w[8];
+      if (entry) take8(entry, at(i), q, g);
+      if (feature) take8(feature, at(i), q, g);
+      if (a.post) take8(a.post, at(i), q, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        t[j] = a.scale * ds[k][j];
+        dn[j] = gated ? t[j] * g[j] : t[j];
+        if (a.post) {
+          x[k][j] = there((x[k][j] - fmean) * fdev, at(i) + j, q);
+          t[j] *= x[k][j] * w[j];                                // dgate
+          h[k][j] = dn[j] * x[k][j];                             // dw_post
+          dn[j] *= w[j];
+        } else {
+          t[j] *= x[k][j];
+        }
+      }
+    };
+    auto add = [&](int array, float (&c)[8], const float (&v)[8], int i) {       // column sums
+      if (NV > 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] += v[j];
+      } else {
+        float* p = sums.part[array] + blockIdx.x * q;
+        float old[8] = {};
+        if (!first) take8(p, at(i), q, old);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) old[j] += v[j];
+        give8(p, at(i), q, old);
+      }
+    };
+    float kf[2] = {};                                            // sums of dn x^ and of dn
+    float dns[HELD][8];
+#pragma unroll U
+    for (int i = 0; i < n; ++i) {
+      const int k = NV ? i : 0;
+      if (NV == 0) load(i);
+      by_stream(i);
+      if (sums.part[0]) add(0, cpre[k], h[k], i);
+      float t[8];
+      by_block(i, dns[k], t);
+      if (sums.part[1]) add(1, cpost[k], h[k], i);
+      if (sums.part[2]) add(2, cgate[k], t, i);
+      if (entries && a.dgate) give8(static_cast<FT*>(a.dgate) + row * q, at(i), q, t);
+      if (NV > 0 && a.dr) give8(static_cast<ST*>(a.dr) + row * q, at(i), q, ds[k]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        kf[0] += there(dns[k][j] * x[k][j], at(i) + j, q);
+        kf[1] += there(dns[k][j], at(i) + j, q);
+      }
+    }
+    if (a.post) sum_threads<TH>(kf, sh, place);
+    const float kx = kf[0] * inv, km = a.layer ? kf[1] * inv : 0.0f;
+#pragma unroll U
+    for (int i = 0; i < n; ++i) {
+      const int k = NV ? i : 0;
+      float t[8];
+      if (NV == 0) {
+        load(i);
+        by_stream(i);
+        by_block(i, dns[0], t);
+        if (a.dr) give8(static_cast<ST*>(a.dr) + row * q, at(i), q, ds[0]);
+      }
+      if (a.post) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dns[k][j] = fdev * (dns[k][j] - x[k][j] * kx - km);
+      }
+      if (a.df) give8(static_cast<FT*>(a.df) + row * q, at(i), q, dns[k]);
+    }
+  }
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (sums.part[0]) give8(sums.part[0] + blockIdx.x * q, at(i), q, cpre[i]);
+      if (sums.part[1]) give8(sums.part[1] + blockIdx.x * q, at(i), q, cpost[i]);
+      if (sums.part[2]) give8(sums.part[2] + blockIdx.x * q, at(i), q, cgate[i]);
+    }
+  }
+}
+
+// out[col] = sum over the workgroups; 64 columns and sixteen sets of workgroups each, blockIdx.y: the array
+struct ColumnOuts { float* out[3]; };
+__global__ __launch_bounds__(1024) void norm_columns_kernel(ColumnSums sums, int groups, long long q, ColumnOuts outs) {
+  __shared__ float sh[16][64];
+  const float* part = sums.part[blockIdx.y];
+  if (!part) return;
+  const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
+  for (long long col0 = blockIdx.x * 64LL; col0 < q; col0 += gridDim.x * 64LL) {
+    const long long col = col0 + lane;
+    float s = 0.0f;
+    if (col < q) {
+#pragma unroll 4
+      for (int g = set; g < groups; g += 16) s += part[g * q + col];
+    }
+    sh[set][lane] = s;
+    __syncthreads();
+    if (set == 0 && col < q) {
+#pragma unroll
+      for (int i = 1; i < 16; ++i) s += sh[i][lane];
+      outs.out[blockIdx.y][col] = s;
+    }
+    __syncthreads();
+  }
+}
+
+// Workgroups of the backward pass: their columns' sums are written and read once more, so about a thousand, with eight rows each where there are many
+int groups_of(const BlockNormArgs& a) {
+  const long long g = a.M <= 512 ? a.M : a.M / 8 > 512 ? a.M / 8 : 512;
+  return (int)(g < 1024 ? g : 1024);
+}
+inline size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+template <typename ST, typename FT, int TH, int NV>
+hipError_t forward_rows(const BlockNormArgs& a, hipStream_t s) {
+  for (long long r = 0; r < a.M; r += MOST_ROWS)
+    hipLaunchKernelGGL((norm_forward_kernel<ST, FT, TH, NV>), dim3((unsigned)(a.M - r < MOST_ROWS ? a.M - r : MOST_ROWS)), dim3(TH), 0, s, a, r);
+  return hipGetLastError();
+}
+template <typename ST, typename FT>
+hipError_t forward_sizes(const BlockNormArgs& a, hipStream_t s) {
+  if (a.q <= 512) return forward_rows<ST, FT, 64, 1>(a, s);
+  if (a.q <= 2048) return forward_rows<ST, FT, 256, 1>(a, s);
+  if (a.q <= 4096) return forward_rows<ST, FT, 512, 1>(a, s);
+  if (a.q <= 8192) return forward_rows<ST, FT, 512, 2>(a, s);
+  if (a.q <= 16384) return forward_rows<ST, FT, 1024, 2>(a, s);
+  return forward_rows<ST, FT, 1024, 0>(a, s);
+}
+template <typename ST, typename FT>
+hipError_t backward_sizes(const BlockNormArgs& a, const ColumnSums& c, int groups, hipStream_t s) {
+#define NORM_BACKWARD(TH, NV) hipLaunchKernelGGL((norm_backward_kernel<ST, FT, TH, NV>), dim3((unsigned)groups), dim3(TH), 0, s, a, c)
+  if (a.q <= 512) NORM_BACKWARD(64, 1);
+  else if (a.q <= 2048) NORM_BACKWARD(256, 1);
+  else if (a.q <= 4096) NORM_BACKWARD(512, 1);
+  else if (a.q <= 8192) NORM_BACKWARD(512, 2);
+  else NORM_BACKWARD(1024, 0);
+#undef NORM_BACKWARD
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t s) {
+  if (a.stype) return a.ftype ? forward_sizes<__bf16, __bf16>(a, s) : forward_sizes<__bf16, float>(a, s);
+  return a.ftype ? forward_sizes<float, __bf16>(a, s) : forward_sizes<float, float>(a, s);
+}
+size_t block_norm_workspace(const BlockNormArgs& a) { return 3 * up((size_t)groups_of(a) * a.q * sizeof(float)); }
+hipError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, hipStream_t s) {
+  const int groups = groups_of(a);
+  const size_t each = up((size_t)groups * a.q * sizeof(float));
+  ColumnOuts outs = {{a.dpre, a.dpost, a.gate_kind == MGRIT_GATE_FEATURE ? static_cast<float*>(a.dgate) : nullptr}};
+  ColumnSums sums = {};
+  bool any = false;
+  for (int i = 0; i < 3; ++i)
+    if (outs.out[i]) { sums.part[i] = reinterpret_cast<float*>(static_cast<char*>(ws) + i * each); any = true; }
+  hipError_t e;
+  if (a.stype) e = a.ftype ? backward_sizes<__bf16, __bf16>(a, sums, groups, s) : backward_sizes<__bf16, float>(a, sums, groups, s);
+  else e = a.ftype ? backward_sizes<float, __bf16>(a, sums, groups, s) : backward_sizes<float, float>(a, sums, groups, s);
+  if (e != hipSuccess || !any) return e;
+  const long long blocks = (a.q + 63) / 64;
+  hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536), 3), dim3(1024), 0, s, sums, groups, a.q, outs);
+  return hipGetLastError();
+}
+
+}  // namespace mgrit

@@ -35,11 +35,14 @@ struct Product {
 size_t     product_workspace(const Product& q);
 hipError_t launch_product(const Product& q, void* ws, hipStream_t s);
 
+// out = what e makes of the sums of `parts` arrays [I][J], one behind the other
+hipError_t join_parts(const Epilogue& e, const float* partial, int parts, long long I, long long J, hipStream_t s);
+
 // The backward pass of an end layer: G = dY * D (D null: dY, with `scale` on every result), dX = G W, dW = G^T X, db = column
 // sums of G; dX, dW, db null where they are not wanted.
 struct BackwardArgs {
   long long M, K, F;
-  int xtype, wtype, ytype;
+  int xtype, wtype, ytype, dxtype;
   float scale;
   const void* X;  const void* W;  const void* D;  const void* dY;
   void* dX;  float* dW;  float* db;
@@ -47,6 +50,55 @@ struct BackwardArgs {
 size_t     backward_workspace(const BackwardArgs& b);
 hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s);
 hipError_t launch_zero(float* out, long long n, hipStream_t s);
+
+// out[col] = sum over the chunks of part[chunk][col]
+hipError_t add_chunks(const float* part, int chunks, long long F, float* out, hipStream_t s);
+
+// A packed array: codes [rows][pitch bytes], scales [slabs][rows][8] (a slab is 256 columns)
+struct Packed {
+  unsigned char* codes;
+  unsigned char* scales;
+  long long rows, cols, slabs, pitch;
+  int format;
+};
+Packed     packed_view(long long rows, long long cols, int format, void* p);
+size_t     packed_bytes(long long rows, long long cols, int format);
+// rows at X, cols entries each
+hipError_t launch_pack(const Packed& p, const void* X, int type, hipStream_t s);
+// out: rows `ld` entries apart, zeros from cols on
+hipError_t launch_unpack(const Packed& p, void* out, int type, long long ld, hipStream_t s);
+struct PackedProduct {
+  long long M, K, F;
+  int xtype, xformat;
+  const void* X;
+  const void* W;                     // packed
+  Epilogue e;
+};
+size_t     packed_product_workspace(const PackedProduct& q);
+hipError_t launch_packed_product(const PackedProduct& q, void* ws, hipStream_t s);
+
+struct BlockNormArgs {
+  long long M, q;
+  int layer, gate_kind, stype, ftype;
+  float eps, scale;
+  const void* f;  const void* r;  const void* gate;  const float* post;  const float* pre;     // r: S in the backward pass
+  void* S;  void* Y;
+  const void* dS;  const void* dY;
+  void* df;  void* dr;  void* dgate;  float* dpost;  float* dpre;
+};
+hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t s);
+size_t     block_norm_workspace(const BlockNormArgs& a);
+hipError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, hipStream_t s);
+
+struct SampleArgs {
+  const void* logits;
+  const float *u, *temperature;
+  const int32_t* top_k;
+  const float *top_p, *min_p;
+  int64_t* index;  float* logprob;
+  int B, V, dtype;
+};
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
 
 struct LossArgs {
   const void* logits;

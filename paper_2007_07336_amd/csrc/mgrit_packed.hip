@@ -1,0 +1,442 @@
+// Values in few bits: packing and unpacking of microscaled arrays, and products with weights in 4 bits.
+#include "mgrit_epilogue.h"
+
+namespace mgrit {
+
+namespace {
+
+constexpr long long MOST_BLOCKS = 1LL << 22;                     // of one launch: fewer than 2^32 threads
+constexpr int MX8 = MGRIT_MX8, MX4 = MGRIT_MX4;
+constexpr int SLAB = 256;                                        // columns of a slab: 8 blocks, 128 bytes of 4-bit codes
+
+inline size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+// Where block b's scale lies among its slab's eight: lanes of one half of a wavefront take blocks 0 2 4 6 in turn, those of the other 1 3 5 7
+__device__ __forceinline__ int place_of(int b) { return (b & 1) * 4 + (b >> 1); }
+// 2^(byte - 127) as a float (byte 0: a subnormal one)
+__device__ __forceinline__ float scale_of(unsigned byte) { return __builtin_bit_cast(float, byte ? byte << 23 : 0x00400000u); }
+// The scale of a block whose largest magnitude has these bits: with top = m 2^x, 1 <= m < 2, and the largest value l 2^e it is 2^(x - e),
+// twice that if m > l; subnormal tops get the least scale, for which everything is small enough
+template <int FORMAT> __device__ __forceinline__ unsigned scale_byte(unsigned top) {
+  constexpr unsigned E = FORMAT == MX8 ? 8 : 2, L = FORMAT == MX8 ? 0x600000u : 0x400000u;
+  if (top >= 0x7f800000u) return 255u;
+  const unsigned x = (top >> 23) + ((top & 0x7fffffu) > L ? 1u : 0u);
+  return x > E ? x - E : 0u;
+}
+__device__ __forceinline__ unsigned codes4(const float (&v)[8], float scale) {                     // eight 4-bit codes
+  unsigned c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+}
+typedef short short2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned codes8(float a, float b, float c, float d, float scale) {     // four 8-bit codes
+  short2v r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true);
+  return __builtin_bit_cast(unsigned, r);
+}
+
+// Eight columns a thread, four lanes a block.  Bound by memory.
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(256) void pack_kernel(Packed p, const T* X, long long first) {
+  const unsigned per = (unsigned)(p.slabs * (SLAB / 8));         // eights of a row
+  const long long base = (first + blockIdx.x) * 256;
+  const unsigned off = (unsigned)(base % per) + threadIdx.x;
+  const long long row = base / per + off / per;
+  if (row >= p.rows) return;                                     // (whole blocks of 32 at a time: rows have a multiple of them)
+  const unsigned e = off % per;
+  const long long k = e * 8LL, left = p.cols - k;
+  const T* x = X + row * p.cols + k;
+  float v[8];
+  if (left >= 8) {
+    load8(x, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < left ? widen(x[j]) : 0.0f;
+  }
+  unsigned top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const unsigned u = __builtin_bit_cast(unsigned, v[j]) & 0x7fffffffu;
+    top = u > top ? u : top;
+  }
+#pragma unroll
+  for (int d = 1; d < 4; d <<= 1) {
+    const unsigned u = (unsigned)__shfl_xor((int)top, d);
+    top = u > top ? u : top;
+  }
+  const unsigned byte = scale_byte<FORMAT>(top);
+  if (byte == 255u) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+  }
+  const float scale = scale_of(byte == 255u ? 127u : byte);
+  if constexpr (FORMAT == MX4) {
+    *reinterpret_cast<unsigned*>(p.codes + row * p.pitch + e * 4LL) = codes4(v, scale);
+  } else {
+    *reinterpret_cast<uint2*>(p.codes + row * p.pitch + e * 8LL) = make_uint2(codes8(v[0], v[1], v[2], v[3], scale), codes8(v[4], v[5], v[6], v[7], scale));
+  }
+  if ((e & 3) == 0) {
+    const unsigned b = e / 4;
+    p.scales[((long long)(b / 8) * p.rows + row) * 8 + place_of(b & 7)] = (unsigned char)byte;
+  }
+}
+
+typedef float floatx2v __attribute__((ext_vector_type(2)));
+// Eight values of codes, in float
+template <int FORMAT> __device__ __forceinline__ void values8(const unsigned char* at, unsigned byte, float (&v)[8]) {
+  const float scale = byte == 255u ? NAN : scale_of(byte);
+  floatx2v a[4];
+  if constexpr (FORMAT == MX4) {
+    const unsigned c = *reinterpret_cast<const unsigned*>(at);
+    a[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0);
+    a[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1);
+    a[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2);
+    a[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3);
+  } else {
+    const uint2 c = *reinterpret_cast<const uint2*>(at);
+    a[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.x, 1.0f, false);
+    a[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.x, 1.0f, true);
+    a[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.y, 1.0f, false);
+    a[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.y, 1.0f, true);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = a[j / 2][j % 2] * scale;    // (by the instructions of ordinary floats, which keep subnormal results)
+}
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(256) void unpack_kernel(Packed p, T* out, long long ld, long long first) {
+  const unsigned per = (unsigned)((ld + 7) / 8);                 // eights of a row of out
+  const long long base = (first + blockIdx.x) * 256;
+  const unsigned off = (unsigned)(base % per) + threadIdx.x;
+  const long long row = base / per + off / per;
+  if (row >= p.rows) return;
+  const unsigned e = off % per;
+  float v[8] = {};
+  if (e * 8LL < p.cols) {
+    const unsigned b = e / 4;
+    const unsigned byte = p.scales[((long long)(b / 8) * p.rows + row) * 8 + place_of(b & 7)];
+    values8<FORMAT>(p.codes + row * p.pitch + e * (FORMAT == MX4 ? 4LL : 8LL), byte, v);
+    if (byte == 255u) {                                          // (what lies behind the last column is zero all the same)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (e * 8LL + j >= p.cols) v[j] = 0.0f;
+    }
+  }
+  put8(out + row * ld + e * 8LL, v, ld - e * 8LL >= 8, ld - e * 8LL);
+}
+
+// out[row][0 .. ld) <- X rounded to bf16, zeros from cols on (ld a multiple of 8)
+template <typename T>
+__global__ __launch_bounds__(256) void round_kernel(const T* X, __bf16* out, long long rows, long long cols, long long ld, long long first) {
+  const unsigned per = (unsigned)(ld / 8);
+  const long long base = (first + blockIdx.x) * 256;
+  const unsigned off = (unsigned)(base % per) + threadIdx.x;
+  const long long row = base / per + off / per;
+  if (row >= rows) return;
+  const long long k = (off % per) * 8LL, left = cols - k;
+  float v[8];
+  if (left >= 8) {
+    load8(X + row * cols + k, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < left ? widen(X[row * cols + k + j]) : 0.0f;
+  }
+  store8(out + row * ld + k, v);
+}
+template <typename F> hipError_t in_launches(long long threads, F launch) {
+  const long long blocks = (threads + 255) / 256;
+  for (long long b = 0; b < blocks; b += MOST_BLOCKS) launch(dim3((unsigned)(blocks - b < MOST_BLOCKS ? blocks - b : MOST_BLOCKS)), b);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------ both operands in 4 bits
+typedef int int8v __attribute__((ext_vector_type(8)));
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+// One operand's codes or scales: rows `ld` bytes apart
+struct Codes {
+  const char* p;
+  const char* scales;
+  long long rows;
+};
+struct FourArgs {
+  Codes A, B;                // X and W
+  Epilogue e;
+  long long I, J, pitch;     // pitch: bytes of a row of codes of either
+  int slabs, per;            // of the contraction; of one workgroup
+  float* partial;            // several workgroups share a tile: their sums
+};
+template <int STEP> __device__ __forceinline__ void multiply4(uint4v a, uint4v b, unsigned sa, unsigned sb, floatx16& c) {
+  const int8v x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+  c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, STEP, (int)sa, STEP, (int)sb);
+}
+
+// Tile of BT x BT outputs, four wavefronts with a quarter each.  A slab is 256 k: 128 bytes of a row, in LDS in the order piece ^ (row / 2 & 7),
+// as the larger types' (so that 16 rows' pieces of one k meet different banks), and 8 scales of a row, one behind the other as they lie in memory.
+// While one slab is multiplied the next one is on its way.
+template <int BT, typename OT>
+__global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void product_four_kernel(FourArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  constexpr int T = BT / 64, NL = BT / 32, CODES = BT * 128, SC = BT * 8 < 1024 ? 1024 : BT * 8, PLACE = 2 * (CODES + SC);     // NL: loads of either's codes per wavefront
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wi = wave >> 1, wj = wave & 1;
+  const int c = lane & 31, g = lane >> 5;
+  constexpr int GM = 4;                                           // tiles in groups of GM rows of tiles: few panels of both operands at a time
+  const long long L = logical_block(), ti = (a.I + BT - 1) / BT, tj = (a.J + BT - 1) / BT;
+  const long long group = L / (GM * tj), firstg = group * GM, size = ti - firstg < GM ? ti - firstg : GM, in = L - group * GM * tj;
+  const long long i0 = (firstg + in % size) * BT, j0 = in / size * BT;
+  const int s0 = (int)blockIdx.y * a.per, slabs = s0 + a.per < a.slabs ? a.per : a.slabs - s0;
+
+  // rows behind the last one read as zeros
+  int offA[NL], offB[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int r = wave * (BT / 4) + i * 8 + (lane >> 3), piece = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    offA[i] = i0 + r < a.I ? (int)(r * a.pitch) + piece : 0x7ffffff0;
+    offB[i] = j0 + r < a.J ? (int)(r * a.pitch) + piece : 0x7ffffff0;
+  }
+  const char *pa = a.A.p + i0 * a.pitch, *pb = a.B.p + j0 * a.pitch;
+  const char *qa = a.A.scales + i0 * 8, *qb = a.B.scales + j0 * 8;
+  const long long stepA = a.A.rows * 8, stepB = a.B.rows * 8;
+  // bytes of a slab's scales, in whole loads (the array has room for that; what belongs to no row meets codes that are zero and results that are not written)
+  const unsigned roomA = (unsigned)((a.I - i0 < BT ? a.I - i0 : BT) * 8 + 15) & ~15u, roomB = (unsigned)((a.J - j0 < BT ? a.J - j0 : BT) * 8 + 15) & ~15u;
+  const unsigned lds_at = (unsigned)(unsigned long long)(LdsPtr*)lds;
+  auto load = [&](int t, int place) {
+    const unsigned to = lds_at + place * PLACE;
+    const int along = (s0 + t) * 128;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      to_lds(pa, offA[i], along, 0x7fff0000u, to + (wave * NL + i) * 1024);
+      to_lds(pb, offB[i], along, 0x7fff0000u, to + CODES + (wave * NL + i) * 1024);
+    }
+    // scales: BT rows of 8 bytes are BT / 128 instructions for either operand
+    if (wave < SC / 1024) to_lds(qa + (s0 + t) * stepA, wave * 1024 + lane * 16, 0, roomA, to + 2 * CODES + wave * 1024);
+    else if (wave - 2 >= 0 && wave - 2 < SC / 1024) to_lds(qb + (s0 + t) * stepB, (wave - 2) * 1024 + lane * 16, 0, roomB, to + 2 * CODES + SC + (wave - 2) * 1024);
+  };
+  floatx16 acc[T][T];
+#pragma unroll
+  for (int i = 0; i < T; ++i)
+#pragma unroll
+    for (int j = 0; j < T; ++j) acc[i][j] = zero16();
+  const int rowA = wi * (BT / 2) + c, rowB = wj * (BT / 2) + c, turn = (c >> 1) & 7;
+  load(0, 0);
+  for (int t = 0; t < slabs; ++t) {
+    // the slab has arrived, for all wavefronts, and nobody reads the other place any more
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 1 < slabs) load(t + 1, (t + 1) & 1);
+    const unsigned char* at = lds + (t & 1) * PLACE;
+    unsigned sa[T], sb[T];
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      sa[i] = *reinterpret_cast<const unsigned*>(at + 2 * CODES + (rowA + i * 32) * 8 + g * 4);
+      sb[i] = *reinterpret_cast<const unsigned*>(at + 2 * CODES + SC + (rowB + i * 32) * 8 + g * 4);
+    }
+    auto step = [&](auto number) {
+      constexpr int STEP = decltype(number)::value;
+      uint4v fa[T], fb[T];
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        fa[i] = *reinterpret_cast<const uint4v*>(at + (rowA + i * 32) * 128 + (((2 * STEP + g) ^ turn) << 4));
+        fb[i] = *reinterpret_cast<const uint4v*>(at + CODES + (rowB + i * 32) * 128 + (((2 * STEP + g) ^ turn) << 4));
+      }
+#pragma unroll
+      for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int j = 0; j < T; ++j) multiply4<STEP>(fb[j], fa[i], sb[j], sa[i], acc[i][j]);      // (B first: a lane has four columns of a row, see the end)
+    };
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 3>{});
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+  // Through LDS, 32 rows of the wavefront's quarter at a time, so that a lane has eight entries of a row in its hands
+  constexpr int W = BT / 2, PITCH = W + 4, STEP = 512 / W, IT = 32 / STEP;
+  const int lc = lane % (W / 8) * 8, lr = lane / (W / 8);
+  const long long col = j0 + wj * W + lc, n = a.I * a.J;
+  const bool whole = col + 8 <= a.J, residual = a.e.R && whole;
+  const bool inside = i0 + BT <= a.I && j0 + BT <= a.J && !a.partial;
+  float bias[8] = {};
+  if (a.e.bias && !a.partial) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) bias[k] = a.e.bias[col + k < a.J ? col + k : a.J - 1];
+  }
+#pragma unroll 1
+  for (int i = 0; i < T; ++i) {
+    const long long row0 = i0 + wi * W + i * 32 + lr;
+    Raw8<OT> ahead[IT];
+    if (inside && residual) {
+#pragma unroll
+      for (int k = 0; k < IT; ++k) ahead[k].load(static_cast<const OT*>(a.e.R) + (row0 + k * STEP) * a.J + col);
+    }
+    float* strip = reinterpret_cast<float*>(lds) + (wave * 2 + (i & 1)) * 32 * PITCH;
+#pragma unroll
+    for (int m = 0; m < T; ++m) {
+      if (m != i) continue;                                       // (registers have no index)
+#pragma unroll
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<floatx4*>(strip + c * PITCH + j * 32 + 8 * q + 4 * g) =
+              floatx4{acc[m][j][4 * q], acc[m][j][4 * q + 1], acc[m][j][4 * q + 2], acc[m][j][4 * q + 3]};
+    }
+    __builtin_amdgcn_wave_barrier();
+    const float* from = strip + lr * PITCH + lc;
+    if (inside) {
+      auto rows = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+#pragma unroll
+        for (int k = 0; k < IT; ++k) {
+          float v[8];
+          *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(from + k * STEP * PITCH);
+          *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(from + k * STEP * PITCH + 4);
+          finish8_whole<OT, KIND>(a.e, (row0 + k * STEP) * a.J + col, v, bias, ahead[k]);
+        }
+      };
+      if (a.e.act == ACT_TANH) rows(std::integral_constant<int, ACT_TANH>{});
+      else if (a.e.act == ACT_RELU) rows(std::integral_constant<int, ACT_RELU>{});
+      else rows(std::integral_constant<int, ACT_IDENT>{});
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < IT; ++k) {
+        const long long row = row0 + k * STEP, at = row * a.J + col;
+        if (row >= a.I) continue;
+        Raw8<OT> r = {};
+        if (residual && !a.partial) r.load(static_cast<const OT*>(a.e.R) + at);
+        float v[8];
+        *reinterpret_cast<floatx4*>(v) = *reinterpret_cast<const floatx4*>(from + k * STEP * PITCH);
+        *reinterpret_cast<floatx4*>(v + 4) = *reinterpret_cast<const floatx4*>(from + k * STEP * PITCH + 4);
+        if (a.partial) put8(a.partial + blockIdx.y * n + at, v, whole, a.J - col);
+        else finish8<OT>(a.e, at, v, bias, r, whole, a.J - col);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+constexpr size_t four_lds(int bt) {
+  const int sc = bt * 8 < 1024 ? 1024 : bt * 8, slabs = 4 * (bt * 128 + sc), strips = 8 * 32 * (bt / 2 + 4) * 4;
+  return slabs > strips ? slabs : strips;
+}
+
+struct FourPlan { int bt, parts; };
+// The tile and the number of workgroups that share its contraction whose time is estimated lowest
+FourPlan four_plan(long long I, long long J, int slabs) {
+  FourPlan p = {};
+  double best = 0.0;
+  for (int bt = 256; bt >= 64; bt /= 2) {
+    const long long tiles = (I + bt - 1) / bt * ((J + bt - 1) / bt);
+    if (tiles > (1LL << 24) - 1) continue;
+    const int fit = bt == 256 ? 1 : bt == 128 ? 2 : 4;            // workgroups on a compute unit
+    const double slab = bt == 256 ? 1.5 : bt == 128 ? 0.6 : 0.3, ends = bt == 256 ? 20.0 : bt == 128 ? 5.0 : 3.0;
+    for (int parts = 1; parts <= 32 && parts <= slabs && (parts == 1 || tiles * parts <= 1024); ++parts) {
+      const int per = (slabs + parts - 1) / parts;
+      if ((slabs + per - 1) / per != parts) continue;
+      const double rounds = (double)((tiles * parts + 255) / 256);
+      const double join = parts > 1 ? 4.0 + (double)I * J * 8.0 * parts / 4.0e6 : 0.0;
+      const double us = rounds * per * slab + ends * (rounds > fit ? rounds / fit : 1.0) + join;
+      if (best == 0.0 || us < best) { best = us; p.bt = bt; p.parts = parts; }
+    }
+  }
+  return p;
+}
+template <int BT, typename OT>
+hipError_t launch_four_tiles(const FourArgs& a, int parts, hipStream_t s) {
+  static LdsOptIn opt;
+  const hipError_t e = opt.raise(reinterpret_cast<const void*>(&product_four_kernel<BT, OT>), four_lds(BT));
+  if (e != hipSuccess) return e;
+  const long long tiles = (a.I + BT - 1) / BT * ((a.J + BT - 1) / BT);
+  hipLaunchKernelGGL((product_four_kernel<BT, OT>), dim3((unsigned)tiles, (unsigned)parts), dim3(256), four_lds(BT), s, a);
+  return hipGetLastError();
+}
+template <typename OT>
+hipError_t launch_four(const FourArgs& a, const FourPlan& p, hipStream_t s) {
+  return p.bt == 256 ? launch_four_tiles<256, OT>(a, p.parts, s) : p.bt == 128 ? launch_four_tiles<128, OT>(a, p.parts, s) : launch_four_tiles<64, OT>(a, p.parts, s);
+}
+
+// ------------------------------------------------------------------------------------------ bf16 rows on 4-bit weights
+inline bool bf16_in_place(const PackedProduct& q) { return q.xtype && q.K % 8 == 0; }
+struct WidePlaces { size_t W, X, bytes; long long ld; Product p; };
+// The weights unpacked to bf16 planes in the workspace, and the product of planes
+WidePlaces wide_places(const PackedProduct& q, char* base) {
+  WidePlaces w = {};
+  w.ld = (q.K + 63) / 64 * 64;
+  w.W = 0;
+  w.X = up((size_t)q.F * w.ld * 2);
+  w.bytes = w.X + (q.xtype ? 0 : up((size_t)q.M * w.ld * 2));
+  w.p.e = q.e;
+  w.p.I = q.M; w.p.J = q.F; w.p.Kc = q.K;
+  w.p.A = Operand{q.xtype ? q.X : base + w.X, nullptr, q.xtype ? q.K : w.ld, 1, 0, !q.xtype, 1, 0};
+  w.p.B = Operand{base + w.W, nullptr, w.ld, 1, 0, 1, 1, 0};
+  return w;
+}
+
+}  // namespace
+
+size_t packed_bytes(long long rows, long long cols, int format) {
+  const Packed p = packed_view(rows, cols, format, nullptr);
+  return up((size_t)rows * p.pitch) + up((size_t)rows * p.slabs * 8);
+}
+Packed packed_view(long long rows, long long cols, int format, void* at) {
+  Packed p = {};
+  p.rows = rows; p.cols = cols; p.format = format;
+  p.slabs = (cols + SLAB - 1) / SLAB;
+  p.pitch = p.slabs * (format == MX4 ? SLAB / 2 : SLAB);
+  p.codes = static_cast<unsigned char*>(at);
+  p.scales = p.codes + up((size_t)rows * p.pitch);
+  return p;
+}
+hipError_t launch_pack(const Packed& p, const void* X, int type, hipStream_t s) {
+  return in_launches(p.rows * p.slabs * (SLAB / 8), [&](dim3 grid, long long b) {
+    if (type && p.format == MX8) hipLaunchKernelGGL((pack_kernel<__bf16, MX8>), grid, dim3(256), 0, s, p, static_cast<const __bf16*>(X), b);
+    else if (type) hipLaunchKernelGGL((pack_kernel<__bf16, MX4>), grid, dim3(256), 0, s, p, static_cast<const __bf16*>(X), b);
+    else if (p.format == MX8) hipLaunchKernelGGL((pack_kernel<float, MX8>), grid, dim3(256), 0, s, p, static_cast<const float*>(X), b);
+    else hipLaunchKernelGGL((pack_kernel<float, MX4>), grid, dim3(256), 0, s, p, static_cast<const float*>(X), b);
+  });
+}
+hipError_t launch_unpack(const Packed& p, void* out, int type, long long ld, hipStream_t s) {
+  return in_launches(p.rows * ((ld + 7) / 8), [&](dim3 grid, long long b) {
+    if (type && p.format == MX8) hipLaunchKernelGGL((unpack_kernel<__bf16, MX8>), grid, dim3(256), 0, s, p, static_cast<__bf16*>(out), ld, b);
+    else if (type) hipLaunchKernelGGL((unpack_kernel<__bf16, MX4>), grid, dim3(256), 0, s, p, static_cast<__bf16*>(out), ld, b);
+    else if (p.format == MX8) hipLaunchKernelGGL((unpack_kernel<float, MX8>), grid, dim3(256), 0, s, p, static_cast<float*>(out), ld, b);
+    else hipLaunchKernelGGL((unpack_kernel<float, MX4>), grid, dim3(256), 0, s, p, static_cast<float*>(out), ld, b);
+  });
+}
+
+size_t packed_product_workspace(const PackedProduct& q) {
+  if (q.xformat == MX4) {
+    const Packed x = packed_view(q.M, q.K, MX4, nullptr);
+    const FourPlan f = four_plan(q.M, q.F, (int)x.slabs);
+    return up(packed_bytes(q.M, q.K, MX4)) + (f.parts > 1 ? (size_t)f.parts * q.M * q.F * sizeof(float) : 0);
+  }
+  const WidePlaces w = wide_places(q, nullptr);
+  return w.bytes + product_workspace(w.p);
+}
+hipError_t launch_packed_product(const PackedProduct& q, void* ws, hipStream_t s) {
+  char* base = static_cast<char*>(ws);
+  const Packed W = packed_view(q.F, q.K, MX4, const_cast<void*>(q.W));
+  if (q.xformat == MX4) {
+    const Packed X = packed_view(q.M, q.K, MX4, ws);
+    const FourPlan f = four_plan(q.M, q.F, (int)X.slabs);
+    hipError_t e = launch_pack(X, q.X, q.xtype, s);
+    if (e != hipSuccess) return e;
+    FourArgs a = {};
+    a.A = Codes{reinterpret_cast<const char*>(X.codes), reinterpret_cast<const char*>(X.scales), q.M};
+    a.B = Codes{reinterpret_cast<const char*>(W.codes), reinterpret_cast<const char*>(W.scales), q.F};
+    a.e = q.e;
+    a.I = q.M; a.J = q.F; a.pitch = X.pitch;
+    a.slabs = (int)X.slabs;
+    a.per = (a.slabs + f.parts - 1) / f.parts;
+    a.partial = f.parts > 1 ? reinterpret_cast<float*>(base + up(packed_bytes(q.M, q.K, MX4))) : nullptr;
+    e = q.e.otype ? launch_four<__bf16>(a, f, s) : launch_four<float>(a, f, s);
+    return e != hipSuccess || f.parts == 1 ? e : join_parts(q.e, a.partial, f.parts, q.M, q.F, s);
+  }
+  const WidePlaces w = wide_places(q, base);
+  hipError_t e = launch_unpack(W, base + w.W, 1, w.ld, s);
+  if (e == hipSuccess && !q.xtype)
+    e = in_launches(q.M * (w.ld / 8), [&](dim3 grid, long long b) {
+      hipLaunchKernelGGL(round_kernel<float>, grid, dim3(256), 0, s, static_cast<const float*>(q.X), reinterpret_cast<__bf16*>(base + w.X), q.M, q.K, w.ld, b);
+    });
+  return e != hipSuccess ? e : launch_product(w.p, base + w.bytes, s);
+}
+
+}  // namespace mgrit
