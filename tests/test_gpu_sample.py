@@ -189,3 +189,23 @@ def test_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(index, want[0]) and torch.equal(logprob, want[1]), replay
+
+
+@pytest.mark.parametrize("dtype", ["f", "b"])
+@pytest.mark.parametrize("V", [600, 5000, 30000, 90000])
+def test_rows_that_crowd_into_few_bins(dtype, V):
+    """Masks of large negative numbers and of the type's lowest one, values that spread over many magnitudes, many equal ones."""
+    x = normal((8, V), 2.0, dtype, V)
+    x[0, ::2] = -1.0e4
+    x[1, ::2] = torch.finfo(x.dtype).min
+    x[2] = (-(torch.arange(V, dtype=torch.float64) % 300) / 3).exp2().to(x.dtype).cuda()
+    x[3] = -torch.exp2((torch.arange(V, dtype=torch.float64) % 120)).to(x.dtype).cuda()
+    x[4] = 1.5
+    x[5, : V - 3] = 0.25
+    x[6] = 1.0 + normal((V,), 1.0e-6, dtype, 2)
+    x[7, 5] = 60.0
+    u = uniform(8, 1)
+    for k in (2, 40, V // 2, V - 1):
+        check(x, u, k=torch.full((8,), k, dtype=torch.int32, device="cuda"))
+    check(x, u, p=uniform(8, 2, 0.1, 1.0))
+    check(x, u, t=uniform(8, 3, 0.01, 3.0), p=uniform(8, 2, 0.5, 1.0), k=torch.full((8,), V // 3, dtype=torch.int32, device="cuda"))
