@@ -353,7 +353,142 @@ hipError_t launch_four(const FourArgs& a, const FourPlan& p, hipStream_t s) {
   return p.bt == 256 ? launch_four_tiles<256, OT>(a, p.parts, s) : p.bt == 128 ? launch_four_tiles<128, OT>(a, p.parts, s) : launch_four_tiles<64, OT>(a, p.parts, s);
 }
 
+// ------------------------------------------------------------------------------------------ few bf16 rows on 4-bit weights
+struct FewArgs {
+  const char* X;             // bf16, rows `ldx` bytes apart of which `row` count, whole 16-byte pieces
+  const char* W;
+  const char* scales;
+  Epilogue e;
+  long long M, F, ldx, pitch;
+  int row, slabs, per;       // slabs of the contraction; of one workgroup
+  float* partial;
+};
+template <int SEL> __device__ __forceinline__ void widen2(unsigned c, float scale, bf16x8& v) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, SEL);
+  v[2 * SEL] = p[0];
+  v[2 * SEL + 1] = p[1];
+}
+// At most 16 FB rows on many weights.  Bound by reading the weights once: a workgroup has 64 of their rows, 16 for each wavefront, and slabs of 256 k
+// of them, of their scales and of all of X on their way into LDS, PLACES of them in turn.  A lane takes a whole block of 32 codes of its row and widens
+// it to bf16 (exact) for four matrix instructions; their k are in another order, which is X's too.
+// 1 row on 32768 x 4096 weights: 71 MB.
+template <int FB> constexpr int few_places() { return FB == 1 ? 3 : FB == 2 ? 2 : 3; }
+template <int FB> constexpr int few_place() { return 64 * 128 + 4 * 1024 + FB * 8192; }
+template <int FB>
+__global__ __launch_bounds__(256, FB <= 2 ? 2 : 1) void product_few_four_kernel(FewArgs a, int first) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  constexpr int PLACES = few_places<FB>(), PLACE = few_place<FB>(), SCALES = 64 * 128, XS = SCALES + 4096, LOADS = 3 + 2 * FB;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+  const long long j0 = ((long long)first + logical_block()) * 64;
+  const int s0 = (int)blockIdx.y * a.per, slabs = s0 + a.per < a.slabs ? a.per : a.slabs - s0;
+  // rows behind the last one, and pieces behind the end of X's, read as zeros
+  int offW[2], offX[2 * FB], pieceX[2 * FB];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = wave * 16 + 8 * h + (lane >> 3), piece = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    offW[h] = j0 + r < a.F ? (int)(r * a.pitch) + piece : 0x7ffffff0;
+  }
+  // X's instruction n of 8 FB: 8 rows of one panel of 64 k; wavefront w takes 2 FB w ..
+#pragma unroll
+  for (int i = 0; i < 2 * FB; ++i) {
+    const int n = wave * 2 * FB + i, block = n >> 3, panel = n >> 1 & 3, r = 8 * (n & 1) + (lane >> 3);
+    pieceX[i] = panel * 128 + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    offX[i] = block * 16 + r < a.M ? (int)((block * 16 + r) * a.ldx) + pieceX[i] : 0x7ffffff0;
+  }
+  const char* pw = a.W + j0 * a.pitch;
+  const char* ps = a.scales + (j0 + wave * 16) * 8;
+  const unsigned room = j0 + wave * 16 < a.F ? (unsigned)((a.F - j0 - wave * 16 < 16 ? a.F - j0 - wave * 16 : 16) * 8 + 15) & ~15u : 0u;
+  const unsigned lds_at = (unsigned)(unsigned long long)(LdsPtr*)lds;
+  auto load = [&](int t) {
+    const unsigned to = lds_at + t % PLACES * PLACE;
+    const int k = s0 + t;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) to_lds(pw, offW[h], k * 128, 0x7fff0000u, to + wave * 2048 + h * 1024);
+    to_lds(ps + (long long)k * a.F * 8, lane * 16, 0, room, to + SCALES + wave * 1024);
+#pragma unroll
+    for (int i = 0; i < 2 * FB; ++i)
+      to_lds(a.X, k * 512 + pieceX[i] < a.row ? offX[i] : 0x7ffffff0, k * 512, 0x7fff0000u, to + XS + (wave * 2 * FB + i) * 1024);
+  };
+  floatx4 acc[FB];
+#pragma unroll
+  for (int i = 0; i < FB; ++i) acc[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  unsigned nans = 0;                 // whether a block of this lane's row is NaN
+#pragma unroll
+  for (int t = 0; t < PLACES - 1; ++t)
+    if (t < slabs) load(t);
+  const int turn = (r16 >> 1) & 7;
+  for (int t = 0; t < slabs; ++t) {
+    // slab t has arrived, for all wavefronts, and nobody reads the one before it any more
+    if (t + PLACES - 2 < slabs) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LOADS * (PLACES - 2)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + PLACES - 1 < slabs) load(t + PLACES - 1);
+    const unsigned char* at = lds + t % PLACES * PLACE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint4v codes = *reinterpret_cast<const uint4v*>(at + wave * 2048 + r16 * 128 + (((4 * h + g) ^ turn) << 4));
+      const unsigned byte = at[SCALES + wave * 1024 + r16 * 8 + (g & 1) * 4 + 2 * h + (g >> 1)];
+      nans |= byte == 255u;
+      const float scale = scale_of(byte == 255u ? 127u : byte);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 w;
+        widen2<0>(codes[j], scale, w);
+        widen2<1>(codes[j], scale, w);
+        widen2<2>(codes[j], scale, w);
+        widen2<3>(codes[j], scale, w);
+#pragma unroll
+        for (int b = 0; b < FB; ++b) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8*>(at + XS + (b * 4 + 2 * h + (g >> 1)) * 2048 + r16 * 128 + ((((g & 1) * 4 + j) ^ turn) << 4));
+          acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, acc[b], 0, 0, 0);
+        }
+      }
+    }
+  }
+  nans |= __shfl_xor(nans, 16);
+  nans |= __shfl_xor(nans, 32);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  // lane: row r16 of the weights, four rows of X
+  float* sums = reinterpret_cast<float*>(lds);
+  constexpr int PITCH = 64 + 4;
+#pragma unroll
+  for (int b = 0; b < FB; ++b)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sums[(b * 16 + 4 * g + r) * PITCH + wave * 16 + r16] = nans ? NAN : acc[b][r];
+  __syncthreads();
+  for (int n = threadIdx.x; n < FB * 16 * 64; n += 256) {
+    const int m = n >> 6, f = n & 63;
+    if (m >= a.M || j0 + f >= a.F) continue;
+    const float v = sums[m * PITCH + f];
+    const long long col = j0 + f, to = m * a.F + col;
+    if (a.partial) a.partial[blockIdx.y * a.M * a.F + to] = v;
+    else if (a.e.otype) finish<__bf16>(a.e, to, col, v);
+    else finish<float>(a.e, to, col, v);
+  }
+}
+template <int FB>
+hipError_t launch_few_four(const FewArgs& a, int parts, hipStream_t s) {
+  static LdsOptIn opt;
+  constexpr size_t smem = few_places<FB>() * few_place<FB>();
+  const hipError_t e = opt.raise(reinterpret_cast<const void*>(&product_few_four_kernel<FB>), smem);
+  if (e != hipSuccess) return e;
+  const long long blocks = (a.F + 63) / 64;
+  for (long long b = 0; b < blocks; b += MOST_BLOCKS)
+    hipLaunchKernelGGL(product_few_four_kernel<FB>, dim3((unsigned)(blocks - b < MOST_BLOCKS ? blocks - b : MOST_BLOCKS), (unsigned)parts), dim3(256), smem, s, a,
+                       (int)b);
+  return hipGetLastError();
+}
+// Workgroups that share the contraction where there are fewer than one for each of the 256 compute units, two slabs each at least
+int few_parts(long long F, int slabs) {
+  const long long blocks = (F + 63) / 64;
+  if (blocks >= 256) return 1;
+  const long long want = (256 + blocks - 1) / blocks, most = slabs / 2 > 1 ? slabs / 2 : 1, parts = want < most ? want : most;
+  const int per = (int)((slabs + parts - 1) / parts);
+  return (slabs + per - 1) / per;
+}
+
 // ------------------------------------------------------------------------------------------ bf16 rows on 4-bit weights
+constexpr long long FEW = 64;
+// (whole 16-byte pieces of rows, and offsets of 31 bits)
 inline bool bf16_in_place(const PackedProduct& q) { return q.xtype && q.K % 8 == 0; }
 struct WidePlaces { size_t W, X, bytes; long long ld; Product p; };
 // The weights unpacked to bf16 planes in the workspace, and the product of planes
@@ -408,6 +543,10 @@ size_t packed_product_workspace(const PackedProduct& q) {
     const FourPlan f = four_plan(q.M, q.F, (int)x.slabs);
     return up(packed_bytes(q.M, q.K, MX4)) + (f.parts > 1 ? (size_t)f.parts * q.M * q.F * sizeof(float) : 0);
   }
+  if (q.M <= FEW) {
+    const int parts = few_parts(q.F, (int)packed_view(q.F, q.K, MX4, nullptr).slabs);
+    return (bf16_in_place(q) ? 0 : up((size_t)q.M * ((q.K + 7) / 8 * 8) * 2)) + (parts > 1 ? (size_t)parts * q.M * q.F * sizeof(float) : 0);
+  }
   const WidePlaces w = wide_places(q, nullptr);
   return w.bytes + product_workspace(w.p);
 }
@@ -430,12 +569,37 @@ hipError_t launch_packed_product(const PackedProduct& q, void* ws, hipStream_t s
     e = q.e.otype ? launch_four<__bf16>(a, f, s) : launch_four<float>(a, f, s);
     return e != hipSuccess || f.parts == 1 ? e : join_parts(q.e, a.partial, f.parts, q.M, q.F, s);
   }
+  // X as bf16 with rows of ld entries, zeros behind the last one
+  auto lay_out = [&](char* to, long long ld) {
+    return in_launches(q.M * (ld / 8), [&](dim3 grid, long long b) {
+      __bf16* out = reinterpret_cast<__bf16*>(to);
+      if (q.xtype) hipLaunchKernelGGL(round_kernel<__bf16>, grid, dim3(256), 0, s, static_cast<const __bf16*>(q.X), out, q.M, q.K, ld, b);
+      else hipLaunchKernelGGL(round_kernel<float>, grid, dim3(256), 0, s, static_cast<const float*>(q.X), out, q.M, q.K, ld, b);
+    });
+  };
+  if (q.M <= FEW) {
+    const long long ld = (q.K + 7) / 8 * 8;
+    const size_t laid = bf16_in_place(q) ? 0 : up((size_t)q.M * ld * 2);
+    hipError_t e = laid ? lay_out(base, ld) : hipSuccess;
+    if (e != hipSuccess) return e;
+    const int parts = few_parts(q.F, (int)W.slabs);
+    FewArgs a = {};
+    a.X = laid ? base : static_cast<const char*>(q.X);
+    a.W = reinterpret_cast<const char*>(W.codes);
+    a.scales = reinterpret_cast<const char*>(W.scales);
+    a.e = q.e;
+    a.M = q.M; a.F = q.F; a.ldx = ld * 2; a.pitch = W.pitch;
+    a.row = (int)(ld * 2);
+    a.slabs = (int)W.slabs;
+    a.per = (a.slabs + parts - 1) / parts;
+    a.partial = parts > 1 ? reinterpret_cast<float*>(base + laid) : nullptr;
+    e = q.M <= 16 ? launch_few_four<1>(a, parts, s) : q.M <= 32 ? launch_few_four<2>(a, parts, s) : q.M <= 48 ? launch_few_four<3>(a, parts, s)
+                                                                                                  : launch_few_four<4>(a, parts, s);
+    return e != hipSuccess || parts == 1 ? e : join_parts(q.e, a.partial, parts, q.M, q.F, s);
+  }
   const WidePlaces w = wide_places(q, base);
   hipError_t e = launch_unpack(W, base + w.W, 1, w.ld, s);
-  if (e == hipSuccess && !q.xtype)
-    e = in_launches(q.M * (w.ld / 8), [&](dim3 grid, long long b) {
-      hipLaunchKernelGGL(round_kernel<float>, grid, dim3(256), 0, s, static_cast<const float*>(q.X), reinterpret_cast<__bf16*>(base + w.X), q.M, q.K, w.ld, b);
-    });
+  if (e == hipSuccess && !q.xtype) e = lay_out(base + w.X, w.ld);
   return e != hipSuccess ? e : launch_product(w.p, base + w.bytes, s);
 }
 
