@@ -556,6 +556,23 @@ template <typename T> __device__ __forceinline__ void store4(T* p, floatx4 v, lo
       if (j < n) p[j] = narrow<T>(v[j]);
   }
 }
+// X in 8 bits: four entries from a multiple of 4 on are within a block, whose scale lies with its slab's
+struct Mx8 {};
+typedef float floatx2p __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ floatx4 load4(const Packed& p, long long row, long long k, long long n) {
+  floatx4 r = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (n <= 0) return r;              // (codes behind the last column are zero)
+  const int block = (int)(k >> 5) & 7;
+  const unsigned c = *reinterpret_cast<const unsigned*>(p.codes + row * p.pitch + k);
+  const unsigned byte = p.scales[((k >> 8) * p.rows + row) * 8 + (block & 1) * 4 + (block >> 1)];
+  const float scale = byte == 255u ? NAN : __builtin_bit_cast(float, byte ? byte << 23 : 0x00400000u);
+  const floatx2p a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.0f, true);
+  return floatx4{a[0] * scale, a[1] * scale, b[0] * scale, b[1] * scale};
+}
+template <typename T> __device__ __forceinline__ floatx4 load4_of(const void* p, const Packed& kept, long long row, long long K, long long k, long long n) {
+  if constexpr (std::is_same<T, Mx8>::value) return load4(kept, row, k, n);
+  else return load4(static_cast<const T*>(p) + row * K + k, n);
+}
 struct ThinArgs {
   const void* S;  const void* T;  const void* g;  const void* f;
   void* outS;  void* outT;            // outT: float sums of every chunk if there are several
@@ -565,6 +582,7 @@ struct ThinArgs {
   int chunk, chunks;                  // rows of a workgroup, at most THIN_ROWS
   int outS_type, outT_type;
   float scale;
+  Packed kept;                        // S or T, whichever is Mx8
 };
 constexpr int THIN_ROWS = 256;
 
@@ -583,7 +601,7 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
   floatx4 x[2][U];
   auto load = [&](int set, int r) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[set][u] = load4(static_cast<const TS*>(a.S) + (r0 + r + 4 * u) * a.K + k, r + 4 * u < n ? left : 0);
+    for (int u = 0; u < U; ++u) x[set][u] = load4_of<TS>(a.S, a.kept, r0 + r + 4 * u, a.K, k, r + 4 * u < n ? left : 0);
   };
   if (a.outT && wave < n) load(0, wave);         // (before anything is waited for)
   for (int i = t; i < n * NT; i += 256) {
@@ -600,7 +618,7 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
 #pragma unroll
   for (int e = 0; e < NT; ++e) {
     w[e] = s[e] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (a.outS && e < a.nt) w[e] = load4(static_cast<const TT*>(a.T) + e * a.K + k, left);
+    if (a.outS && e < a.nt) w[e] = load4_of<TT>(a.T, a.kept, e, a.K, k, left);
   }
   __syncthreads();
   auto multiply = [&](int set, int r) {
@@ -1526,7 +1544,11 @@ hipError_t launch_thin(const BackwardArgs& b, const ThinPlan& p, char* ws, hipSt
   a.outS_type = c ? b.dxtype : 0;  a.outT_type = c ? 0 : b.dxtype;
   a.scale = b.scale;
   const int ts = c ? b.xtype : b.wtype, tt = c ? b.wtype : b.xtype;
-  hipError_t e = ts ? (tt ? launch_thin_y<__bf16, __bf16>(a, b.ytype, s) : launch_thin_y<__bf16, float>(a, b.ytype, s))
+  a.kept = b.kept;
+  hipError_t e;
+  if (b.kept.codes) e = c ? (tt ? launch_thin_y<Mx8, __bf16>(a, b.ytype, s) : launch_thin_y<Mx8, float>(a, b.ytype, s))
+                          : (ts ? launch_thin_y<__bf16, Mx8>(a, b.ytype, s) : launch_thin_y<float, Mx8>(a, b.ytype, s));
+  else e = ts ? (tt ? launch_thin_y<__bf16, __bf16>(a, b.ytype, s) : launch_thin_y<__bf16, float>(a, b.ytype, s))
                     : (tt ? launch_thin_y<float, __bf16>(a, b.ytype, s) : launch_thin_y<float, float>(a, b.ytype, s));
   if (e != hipSuccess || p.chunks == 1) return e;
   if (outT) {
@@ -1599,6 +1621,8 @@ size_t backward_workspace(const BackwardArgs& b) {
   }
   return n;
 }
+
+bool backward_reads_kept(const BackwardArgs& b) { return thin_plan(b).thin; }
 
 hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s) {
   const ThinPlan t = thin_plan(b);

@@ -39,6 +39,17 @@ template <typename T> __device__ __forceinline__ void take8(const T* p, long lon
 template <typename T> __device__ __forceinline__ void give8(T* p, long long k, long long q, const float (&v)[8]) {
   if (k < q) put8(p + k, v, k + 8 <= q, q - k);
 }
+// The same as they were loaded, to be on their way while something else is computed
+template <typename T> __device__ __forceinline__ void take_raw(const T* p, long long k, long long q, Raw8<T>& v) {
+  if (k + 8 <= q) {
+    v.load(p + k);
+  } else {
+    T e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = k + j < q ? p[k + j] : T(0.0f);
+    __builtin_memcpy(&v, e, sizeof(e));
+  }
+}
 // d for entries that exist, zero behind them (of sums of deviations, which are not zero there)
 __device__ __forceinline__ float there(float d, long long k, long long q) { return k < q ? d : 0.0f; }
 
@@ -164,6 +175,29 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
   float x[HELD][8], s[HELD][8], ds[HELD][8], h[HELD][8];         // f, S, the gradient by S, that by S's normalised row
   float cpre[HELD][8] = {}, cpost[HELD][8] = {}, cgate[HELD][8] = {};
   auto at = [&](int i) { return ((long long)i * TH + threadIdx.x) * 8; };
+  // NV = 1: the vectors stay in registers, and the next row is on its way while this one is computed (8192 x 4096 with all of it: one workgroup to a
+  // compute unit, 229 us without, 172 so, 153 with half as many workgroups)
+  constexpr bool AHEAD = NV == 1;
+  float wpre[8] = {}, wpost[8] = {}, wfeature[8] = {}, wentry[8] = {};
+  Raw8<FT> nf = {}, nY = {}, ng = {};
+  Raw8<ST> nS = {}, ndS = {};
+  auto fetch = [&](long long row) {
+    const long long k = at(0);
+    take_raw(static_cast<const FT*>(a.f) + row * q, k, q, nf);
+    if (a.dS) take_raw(static_cast<const ST*>(a.dS) + row * q, k, q, ndS);
+    if (entries) take_raw(static_cast<const FT*>(a.gate) + row * q, k, q, ng);
+    if (!a.pre) return;
+    take_raw(static_cast<const ST*>(a.r) + row * q, k, q, nS);
+    take_raw(static_cast<const FT*>(a.dY) + row * q, k, q, nY);
+  };
+  if constexpr (AHEAD) {
+    fetch(blockIdx.x);
+    if (a.pre) take8(a.pre, at(0), q, wpre);
+    if (a.post) take8(a.post, at(0), q, wpost);
+    if (feature) take8(feature, at(0), q, wfeature);
+  }
+  auto get_pre = [&](int i, float (&w)[8]) { if constexpr (AHEAD) __builtin_memcpy(w, wpre, sizeof(w)); else if (a.pre) take8(a.pre, at(i), q, w); };
+  auto get_post = [&](int i, float (&w)[8]) { if constexpr (AHEAD) __builtin_memcpy(w, wpost, sizeof(w)); else if (a.post) take8(a.post, at(i), q, w); };
   for (long long row = blockIdx.x; row < a.M; row += gridDim.x) {
     const FT* f = static_cast<const FT*>(a.f) + row * q;
     const ST* S = static_cast<const ST*>(a.r) + row * q;
@@ -179,14 +213,22 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
       take8(S, at(i), q, s[k]);
       take8(dY, at(i), q, h[k]);
     };
-    auto weigh = [&](int i) {                                    // h <- dY w_pre
-      const int k = NV ? i : 0;
-      float w[8];
-      take8(a.pre, at(i), q, w);
+    auto get_gate = [&](int i, float (&g)[8]) {
+      if constexpr (AHEAD) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[k][j] *= w[j];
+        for (int j = 0; j < 8; ++j) g[j] = entries ? wentry[j] : wfeature[j];
+      } else {
+        if (entry) take8(entry, at(i), q, g);
+        if (feature) take8(feature, at(i), q, g);
+      }
     };
-    if constexpr (NV > 0) {
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[0][j] = nf.at(j); s[0][j] = nS.at(j); ds[0][j] = ndS.at(j); h[0][j] = nY.at(j); wentry[j] = ng.at(j);
+      }
+      if (row + gridDim.x < a.M) fetch(row + gridDim.x);
+    } else if constexpr (NV > 0) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) load(i);
     }
@@ -199,7 +241,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
         const int k = NV ? i : 0;
         if (NV == 0) load(i);
         float w[8];
-        if (a.pre) take8(a.pre, at(i), q, w);
+        get_pre(i, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           v[0] += x[k][j];
@@ -217,7 +259,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
         const int k = NV ? i : 0;
         if (NV == 0) load(i);
         float w[8];
-        if (a.pre) take8(a.pre, at(i), q, w);
+        get_pre(i, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float d = there(x[k][j] - fmean, at(i) + j, q);
@@ -237,7 +279,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
     auto by_stream = [&](int i) {
       const int k = NV ? i : 0;
       float w[8];
-      if (a.pre) take8(a.pre, at(i), q, w);
+      get_pre(i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float d = dS ? ds[k][j] : 0.0f;
@@ -253,9 +295,8 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
     auto by_block = [&](int i, float (&dn)[8], float (&t)[8]) {
       const int k = NV ? i : 0;
       float g[8], w[8];
-      if (entry) take8(entry, at(i), q, g);
-      if (feature) take8(feature, at(i), q, g);
-      if (a.post) take8(a.post, at(i), q, w);
+      get_gate(i, g);
+      get_post(i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         t[j] = a.scale * ds[k][j];
@@ -332,35 +373,38 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
   }
 }
 
-// out[col] = sum over the workgroups; 64 columns and sixteen sets of workgroups each, blockIdx.y: the array
+// out[col] = sum over the workgroups; 32 columns and 32 sets of workgroups each, blockIdx.y: the array
 struct ColumnOuts { float* out[3]; };
 __global__ __launch_bounds__(1024) void norm_columns_kernel(ColumnSums sums, int groups, long long q, ColumnOuts outs) {
-  __shared__ float sh[16][64];
+  __shared__ float sh[32][33];
   const float* part = sums.part[blockIdx.y];
   if (!part) return;
-  const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
-  for (long long col0 = blockIdx.x * 64LL; col0 < q; col0 += gridDim.x * 64LL) {
+  const int lane = threadIdx.x & 31, set = threadIdx.x >> 5;
+  for (long long col0 = blockIdx.x * 32LL; col0 < q; col0 += gridDim.x * 32LL) {
     const long long col = col0 + lane;
     float s = 0.0f;
     if (col < q) {
-#pragma unroll 4
-      for (int g = set; g < groups; g += 16) s += part[g * q + col];
+#pragma unroll 8
+      for (int g = set; g < groups; g += 32) s += part[g * q + col];
     }
     sh[set][lane] = s;
     __syncthreads();
-    if (set == 0 && col < q) {
+    if (threadIdx.x < 32 && col < q) {
 #pragma unroll
-      for (int i = 1; i < 16; ++i) s += sh[i][lane];
+      for (int i = 1; i < 32; ++i) s += sh[i][lane];
       outs.out[blockIdx.y][col] = s;
     }
     __syncthreads();
   }
 }
 
-// Workgroups of the backward pass: their columns' sums are written and read once more, so about a thousand, with eight rows each where there are many
+// Threads of a row, and workgroups of the backward pass: about 2048 wavefronts, which is what the compute units hold at once, and two rows each at least.  Their
+// columns' sums are written and read once more (us with 256 / 512 / 1024 / 2048 workgroups: 8192 x 4096 170 / 171 / 185 / -, 4000 x 1024 61 / 42 / 44 / -,
+// 20000 x 300 309 / 170 / 97 / 62).
+inline int threads_of(long long q) { return q <= 512 ? 64 : q <= 2048 ? 256 : q <= 8192 ? 512 : 1024; }
 int groups_of(const BlockNormArgs& a) {
-  const long long g = a.M <= 512 ? a.M : a.M / 8 > 512 ? a.M / 8 : 512;
-  return (int)(g < 1024 ? g : 1024);
+  const long long most = a.q > 8192 ? 256 : 131072 / threads_of(a.q), g = (a.M + 1) / 2;
+  return (int)(g < most ? g : most);
 }
 inline size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -410,7 +454,7 @@ hipError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, hipStrea
   if (a.stype) e = a.ftype ? backward_sizes<__bf16, __bf16>(a, sums, groups, s) : backward_sizes<__bf16, float>(a, sums, groups, s);
   else e = a.ftype ? backward_sizes<float, __bf16>(a, sums, groups, s) : backward_sizes<float, float>(a, sums, groups, s);
   if (e != hipSuccess || !any) return e;
-  const long long blocks = (a.q + 63) / 64;
+  const long long blocks = (a.q + 31) / 32;
   hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536), 3), dim3(1024), 0, s, sums, groups, a.q, outs);
   return hipGetLastError();
 }

@@ -38,6 +38,13 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s);
 // out = what e makes of the sums of `parts` arrays [I][J], one behind the other
 hipError_t join_parts(const Epilogue& e, const float* partial, int parts, long long I, long long J, hipStream_t s);
 
+// A packed array: codes [rows][pitch bytes], scales [slabs][rows][8] (a slab is 256 columns)
+struct Packed {
+  unsigned char* codes;
+  unsigned char* scales;
+  long long rows, cols, slabs, pitch;
+  int format;
+};
 // The backward pass of an end layer: G = dY * D (D null: dY, with `scale` on every result), dX = G W, dW = G^T X, db = column
 // sums of G; dX, dW, db null where they are not wanted.
 struct BackwardArgs {
@@ -46,27 +53,23 @@ struct BackwardArgs {
   float scale;
   const void* X;  const void* W;  const void* D;  const void* dY;
   void* dX;  float* dW;  float* db;
+  Packed kept;                       // X in 8 bits (xtype and X count no more), for products that read it so
 };
 size_t     backward_workspace(const BackwardArgs& b);
+bool       backward_reads_kept(const BackwardArgs& b);
 hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s);
 hipError_t launch_zero(float* out, long long n, hipStream_t s);
 
 // out[col] = sum over the chunks of part[chunk][col]
 hipError_t add_chunks(const float* part, int chunks, long long F, float* out, hipStream_t s);
 
-// A packed array: codes [rows][pitch bytes], scales [slabs][rows][8] (a slab is 256 columns)
-struct Packed {
-  unsigned char* codes;
-  unsigned char* scales;
-  long long rows, cols, slabs, pitch;
-  int format;
-};
 Packed     packed_view(long long rows, long long cols, int format, void* p);
 size_t     packed_bytes(long long rows, long long cols, int format);
 // rows at X, cols entries each
 hipError_t launch_pack(const Packed& p, const void* X, int type, hipStream_t s);
-// out: rows `ld` entries apart, zeros from cols on
-hipError_t launch_unpack(const Packed& p, void* out, int type, long long ld, hipStream_t s);
+// out: rows `ld` entries apart, zeros from cols on; rows without entries (0) are passed over
+struct Unpack { Packed from; void* out; int type; long long ld; };
+hipError_t launch_unpack(const Unpack* arrays, int n, hipStream_t s);      // one or two in one launch
 struct PackedProduct {
   long long M, K, F;
   int xtype, xformat;

@@ -92,11 +92,12 @@ PackedProduct packed_product(const mgrit_affine_packed_t* p, const void* X, cons
   q.e = Epilogue{1, p->act, p->ytype, p->scale, b, R, Y, D};
   return q;
 }
-// What a backward pass from kept activations unpacks: X as bf16 (its values are some), D as its type; the rest of the workspace behind them
-struct KeptPlaces { size_t D, bytes; };
+// What a backward pass from kept activations unpacks: D as its type and, where it is not read as it is, X as bf16; the rest of the workspace behind them
+struct KeptPlaces { bool reads; size_t D, bytes; };
 KeptPlaces kept_places(const mgrit_affine_t* p) {
   KeptPlaces k = {};
-  k.D = up((size_t)p->M * p->K * 2);
+  k.reads = backward_reads_kept(BackwardArgs{p->M, p->K, p->F});
+  k.D = k.reads ? 0 : up((size_t)p->M * p->K * 2);
   k.bytes = k.D + up((size_t)p->M * p->F * (p->ytype ? 2 : 4));
   return k;
 }
@@ -236,8 +237,8 @@ int32_t mgrit_unpack(const mgrit_packed_t* p, const void* packed, void* X, void*
   if (rc != MGRIT_OK) return rc;
   if (p->rows == 0) return MGRIT_OK;
   if (!X || !packed || !aligned_to(X, 16) || !aligned_to(packed, 256)) return MGRIT_ERR_POINTER;
-  const Packed v = packed_view(p->rows, p->cols, p->format, const_cast<void*>(packed));
-  return launch_unpack(v, X, p->dtype, p->cols, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
+  const Unpack u = {packed_view(p->rows, p->cols, p->format, const_cast<void*>(packed)), X, p->dtype, p->cols};
+  return launch_unpack(&u, 1, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
 }
 
 size_t mgrit_affine_packed_workspace_bytes(const mgrit_affine_packed_t* p) {
@@ -284,11 +285,16 @@ int32_t mgrit_affine_kept_backward(const mgrit_affine_t* p, const void* X, const
   if (!dX && !dW && !db) return MGRIT_OK;
   const KeptPlaces at = kept_places(p);
   char* base = static_cast<char*>(workspace);
-  hipError_t e = hipSuccess;
-  if (dW) e = launch_unpack(packed_view(p->M, p->K, MGRIT_MX8, const_cast<void*>(X)), base, 1, p->K, s);
-  if (e == hipSuccess && D) e = launch_unpack(packed_view(p->M, p->F, MGRIT_MX8, const_cast<void*>(D)), base + at.D, p->ytype, p->F, s);
-  if (e == hipSuccess) e = launch_backward(kept_args(p, base, W, D ? base + at.D : nullptr, dY, dX, dW, db), base + at.bytes, s);
-  return e == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
+  const Packed X8 = packed_view(p->M, p->K, MGRIT_MX8, const_cast<void*>(X));
+  Unpack u[2];
+  int n = 0;
+  if (dW && !at.reads) u[n++] = Unpack{X8, base, MGRIT_BF16, p->K};
+  if (D) u[n++] = Unpack{packed_view(p->M, p->F, MGRIT_MX8, const_cast<void*>(D)), base + at.D, p->ytype, p->F};
+  hipError_t e = n ? launch_unpack(u, n, s) : hipSuccess;
+  if (e != hipSuccess) return MGRIT_ERR_HIP;
+  BackwardArgs b = kept_args(p, base, W, D ? base + at.D : nullptr, dY, dX, dW, db);
+  if (at.reads) b.kept = X8;
+  return launch_backward(b, base + at.bytes, s) == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
 }
 
 int32_t mgrit_block_norm_forward(const mgrit_block_norm_t* p, const void* f, const void* r, const void* gate, const float* w_post,

@@ -105,9 +105,9 @@ template <int FORMAT> __device__ __forceinline__ void values8(const unsigned cha
   for (int j = 0; j < 8; ++j) v[j] = a[j / 2][j % 2] * scale;    // (by the instructions of ordinary floats, which keep subnormal results)
 }
 template <typename T, int FORMAT>
-__global__ __launch_bounds__(256) void unpack_kernel(Packed p, T* out, long long ld, long long first) {
-  const unsigned per = (unsigned)((ld + 7) / 8);                 // eights of a row of out
-  const long long base = (first + blockIdx.x) * 256;
+__device__ __forceinline__ void unpack(const Unpack& u, long long base) {
+  const Packed& p = u.from;
+  const unsigned per = (unsigned)((u.ld + 7) / 8);               // eights of a row of out
   const unsigned off = (unsigned)(base % per) + threadIdx.x;
   const long long row = base / per + off / per;
   if (row >= p.rows) return;
@@ -123,7 +123,17 @@ __global__ __launch_bounds__(256) void unpack_kernel(Packed p, T* out, long long
         if (e * 8LL + j >= p.cols) v[j] = 0.0f;
     }
   }
-  put8(out + row * ld + e * 8LL, v, ld - e * 8LL >= 8, ld - e * 8LL);
+  put8(static_cast<T*>(u.out) + row * u.ld + e * 8LL, v, u.ld - e * 8LL >= 8, u.ld - e * 8LL);
+}
+// Two arrays: the second one's workgroups from `second` on
+struct Unpacks { Unpack u[2]; long long second; };
+__global__ __launch_bounds__(256) void unpack_kernel(Unpacks a, long long first) {
+  const long long block = first + blockIdx.x;
+  const bool other = block >= a.second;
+  const Unpack& u = a.u[other ? 1 : 0];
+  const long long base = (other ? block - a.second : block) * 256;
+  if (u.from.format == MX8) { if (u.type) unpack<__bf16, MX8>(u, base); else unpack<float, MX8>(u, base); }
+  else { if (u.type) unpack<__bf16, MX4>(u, base); else unpack<float, MX4>(u, base); }
 }
 
 // out[row][0 .. ld) <- X rounded to bf16, zeros from cols on (ld a multiple of 8)
@@ -528,13 +538,15 @@ hipError_t launch_pack(const Packed& p, const void* X, int type, hipStream_t s) 
     else hipLaunchKernelGGL((pack_kernel<float, MX4>), grid, dim3(256), 0, s, p, static_cast<const float*>(X), b);
   });
 }
-hipError_t launch_unpack(const Packed& p, void* out, int type, long long ld, hipStream_t s) {
-  return in_launches(p.rows * ((ld + 7) / 8), [&](dim3 grid, long long b) {
-    if (type && p.format == MX8) hipLaunchKernelGGL((unpack_kernel<__bf16, MX8>), grid, dim3(256), 0, s, p, static_cast<__bf16*>(out), ld, b);
-    else if (type) hipLaunchKernelGGL((unpack_kernel<__bf16, MX4>), grid, dim3(256), 0, s, p, static_cast<__bf16*>(out), ld, b);
-    else if (p.format == MX8) hipLaunchKernelGGL((unpack_kernel<float, MX8>), grid, dim3(256), 0, s, p, static_cast<float*>(out), ld, b);
-    else hipLaunchKernelGGL((unpack_kernel<float, MX4>), grid, dim3(256), 0, s, p, static_cast<float*>(out), ld, b);
-  });
+hipError_t launch_unpack(const Unpack* arrays, int n, hipStream_t s) {
+  Unpacks a = {};
+  long long blocks[2] = {};
+  for (int i = 0; i < n; ++i) {
+    a.u[i] = arrays[i];
+    blocks[i] = (arrays[i].from.rows * ((arrays[i].ld + 7) / 8) + 255) / 256;
+  }
+  a.second = blocks[0];
+  return in_launches((blocks[0] + blocks[1]) * 256, [&](dim3 grid, long long b) { hipLaunchKernelGGL(unpack_kernel, grid, dim3(256), 0, s, a, b); });
 }
 
 size_t packed_product_workspace(const PackedProduct& q) {
@@ -598,7 +610,8 @@ hipError_t launch_packed_product(const PackedProduct& q, void* ws, hipStream_t s
     return e != hipSuccess || parts == 1 ? e : join_parts(q.e, a.partial, parts, q.M, q.F, s);
   }
   const WidePlaces w = wide_places(q, base);
-  hipError_t e = launch_unpack(W, base + w.W, 1, w.ld, s);
+  const Unpack weights = {W, base + w.W, 1, w.ld};
+  hipError_t e = launch_unpack(&weights, 1, s);
   if (e == hipSuccess && !q.xtype) e = lay_out(base + w.X, w.ld);
   return e != hipSuccess ? e : launch_product(w.p, base + w.bytes, s);
 }
