@@ -7,10 +7,10 @@ namespace {
 
 constexpr long long MOST_ROWS = 1LL << 21;                       // of one launch: fewer than 2^32 threads
 
-// Sums over the TH threads of a workgroup; all threads get them.  sh: two places in turn (one barrier each).
-template <int TH, int N> __device__ __forceinline__ void sum_threads(float (&v)[N], float (&sh)[2][TH / 64][4], int& place) {
+// Sums over the LANES lanes of a row, or the TH threads of a workgroup (LANES = 64); all of them get them.  sh: two places in turn (one barrier each).
+template <int TH, int LANES, int N> __device__ __forceinline__ void sum_threads(float (&v)[N], float (&sh)[2][TH / 64][4], int& place) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1)
+  for (int d = LANES / 2; d; d >>= 1)
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d);
   if constexpr (TH > 64) {
@@ -53,13 +53,16 @@ template <typename T> __device__ __forceinline__ void take_raw(const T* p, long 
 // d for entries that exist, zero behind them (of sums of deviations, which are not zero there)
 __device__ __forceinline__ float there(float d, long long k, long long q) { return k < q ? d : 0.0f; }
 
-// One row per workgroup of TH threads.  NV > 0: the row's eights fit NV registers sets of each thread and are read once; NV = 0: they are read again
+// One row per workgroup of TH threads, or (LANES < 64) 64 / LANES rows, LANES lanes each.  NV > 0: the row's eights fit NV registers sets of each thread and are read once; NV = 0: they are read again
 // for every step.  A row's entries are only ever touched by the thread that writes them, so S may take r's place and Y f's.
-template <typename ST, typename FT, int TH, int NV>
+template <typename ST, typename FT, int TH, int NV, int LANES>
 __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long long first) {
   __shared__ float sh[2][TH / 64][4];
   int place = 0;
-  const long long row = first + blockIdx.x, q = a.q;
+  constexpr int ROWS = LANES < 64 ? 64 / LANES : 1;
+  const long long row = first + (long long)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0), q = a.q;
+  const unsigned thread = ROWS > 1 ? threadIdx.x % LANES : threadIdx.x;
+  if (row >= a.M) return;
   const FT* f = static_cast<const FT*>(a.f) + row * q;
   const ST* r = static_cast<const ST*>(a.r) + row * q;
   const FT* entry = a.gate_kind == MGRIT_GATE_ENTRY ? static_cast<const FT*>(a.gate) + row * q : nullptr;
@@ -68,7 +71,7 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
   constexpr int HELD = NV > 0 ? NV : 1, U = HELD;
   const float inv = 1.0f / (float)q;
   float x[HELD][8], y[HELD][8];
-  auto at = [&](int i) { return ((long long)i * TH + threadIdx.x) * 8; };
+  auto at = [&](int i) { return ((long long)i * TH + thread) * 8; };
   auto read_f = [&](int i) { if (NV == 0) take8(f, at(i), q, x[0]); };
   if constexpr (NV > 0) {
 #pragma unroll
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[0] += x[NV ? i : 0][j];
       }
-      sum_threads<TH>(s, sh, place);
+      sum_threads<TH, LANES>(s, sh, place);
       mean = s[0] * inv;
     }
     float s[1] = {};
@@ -96,7 +99,7 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
 #pragma unroll
       for (int j = 0; j < 8; ++j) { const float d = there(x[NV ? i : 0][j] - mean, at(i) + j, q); s[0] += d * d; }
     }
-    sum_threads<TH>(s, sh, place);
+    sum_threads<TH, LANES>(s, sh, place);
     dev = 1.0f / sqrtf(s[0] * inv + a.eps);
   }
   // y <- S
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[0] += there(y[NV ? i : 0][j], at(i) + j, q);
       }
-      sum_threads<TH>(s, sh, place);
+      sum_threads<TH, LANES>(s, sh, place);
       smean = s[0] * inv;
     }
     float s[1] = {};
@@ -141,7 +144,7 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
 #pragma unroll
       for (int j = 0; j < 8; ++j) { const float d = there(y[NV ? i : 0][j] - smean, at(i) + j, q); s[0] += d * d; }
     }
-    sum_threads<TH>(s, sh, place);
+    sum_threads<TH, LANES>(s, sh, place);
     sdev = 1.0f / sqrtf(s[0] * inv + a.eps);
   }
 #pragma unroll U
@@ -162,11 +165,14 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
 // d (h - x^ mean(h x^)), with MGRIT_NORM_LAYER less mean(h) inside the brackets too.  A workgroup takes the rows b, b + G, .. and keeps the columns' sums
 // of its rows in registers; they go to part[array][b][q] and are added up by a second launch.
 struct ColumnSums { float* part[3]; };                           // of dw_pre, dw_post, dgate; null where not wanted
-template <typename ST, typename FT, int TH, int NV>
+template <typename ST, typename FT, int TH, int NV, int LANES>
 __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, ColumnSums sums) {
   __shared__ float sh[2][TH / 64][4];
   int place = 0;
   const long long q = a.q;
+  constexpr int ROWS = LANES < 64 ? 64 / LANES : 1;
+  const unsigned thread = ROWS > 1 ? threadIdx.x % LANES : threadIdx.x;
+  const long long row0 = (long long)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0), step = (long long)gridDim.x * ROWS;
   const float* feature = a.gate_kind == MGRIT_GATE_FEATURE ? static_cast<const float*>(a.gate) : nullptr;
   const bool entries = a.gate_kind == MGRIT_GATE_ENTRY, gated = entries || feature;
   const int n = NV > 0 ? NV : (int)((q + 8 * TH - 1) / (8 * TH));
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
   const float inv = 1.0f / (float)q;
   float x[HELD][8], s[HELD][8], ds[HELD][8], h[HELD][8];         // f, S, the gradient by S, that by S's normalised row
   float cpre[HELD][8] = {}, cpost[HELD][8] = {}, cgate[HELD][8] = {};
-  auto at = [&](int i) { return ((long long)i * TH + threadIdx.x) * 8; };
+  auto at = [&](int i) { return ((long long)i * TH + thread) * 8; };
   // NV = 1: the vectors stay in registers, and the next row is on its way while this one is computed (8192 x 4096 with all of it: one workgroup to a
   // compute unit, 229 us without, 172 so, 153 with half as many workgroups)
   constexpr bool AHEAD = NV == 1;
@@ -191,20 +197,20 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
     take_raw(static_cast<const FT*>(a.dY) + row * q, k, q, nY);
   };
   if constexpr (AHEAD) {
-    fetch(blockIdx.x);
+    if (row0 < a.M) fetch(row0);
     if (a.pre) take8(a.pre, at(0), q, wpre);
     if (a.post) take8(a.post, at(0), q, wpost);
     if (feature) take8(feature, at(0), q, wfeature);
   }
   auto get_pre = [&](int i, float (&w)[8]) { if constexpr (AHEAD) __builtin_memcpy(w, wpre, sizeof(w)); else if (a.pre) take8(a.pre, at(i), q, w); };
   auto get_post = [&](int i, float (&w)[8]) { if constexpr (AHEAD) __builtin_memcpy(w, wpost, sizeof(w)); else if (a.post) take8(a.post, at(i), q, w); };
-  for (long long row = blockIdx.x; row < a.M; row += gridDim.x) {
+  for (long long row = row0; row < a.M; row += step) {
     const FT* f = static_cast<const FT*>(a.f) + row * q;
     const ST* S = static_cast<const ST*>(a.r) + row * q;
     const ST* dS = a.dS ? static_cast<const ST*>(a.dS) + row * q : nullptr;
     const FT* dY = a.dY ? static_cast<const FT*>(a.dY) + row * q : nullptr;
     const FT* entry = entries ? static_cast<const FT*>(a.gate) + row * q : nullptr;
-    const bool first = row == blockIdx.x;
+    const bool first = row == row0;
     auto load = [&](int i) {
       const int k = NV ? i : 0;
       take8(f, at(i), q, x[k]);
@@ -227,7 +233,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
       for (int j = 0; j < 8; ++j) {
         x[0][j] = nf.at(j); s[0][j] = nS.at(j); ds[0][j] = ndS.at(j); h[0][j] = nY.at(j); wentry[j] = ng.at(j);
       }
-      if (row + gridDim.x < a.M) fetch(row + gridDim.x);
+      if (row + step < a.M) fetch(row + step);
     } else if constexpr (NV > 0) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) load(i);
@@ -248,7 +254,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
           if (a.pre) { v[1] += s[k][j]; v[2] += h[k][j] * w[j]; }
         }
       }
-      sum_threads<TH>(v, sh, place);
+      sum_threads<TH, LANES>(v, sh, place);
       fmean = v[0] * inv; smean = v[1] * inv; hmean = v[2] * inv;
     }
     float fdev = 1.0f, sdev = 1.0f, hs = 0.0f;
@@ -271,7 +277,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
           }
         }
       }
-      sum_threads<TH>(v, sh, place);
+      sum_threads<TH, LANES>(v, sh, place);
       if (a.post) fdev = 1.0f / sqrtf(v[0] * inv + a.eps);
       if (a.pre) { sdev = 1.0f / sqrtf(v[1] * inv + a.eps); hs = v[2] * inv * sdev; }
     }
@@ -344,7 +350,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
         kf[1] += there(dns[k][j], at(i) + j, q);
       }
     }
-    if (a.post) sum_threads<TH>(kf, sh, place);
+    if (a.post) sum_threads<TH, LANES>(kf, sh, place);
     const float kx = kf[0] * inv, km = a.layer ? kf[1] * inv : 0.0f;
 #pragma unroll U
     for (int i = 0; i < n; ++i) {
@@ -362,6 +368,17 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
       }
       if (a.df) give8(static_cast<FT*>(a.df) + row * q, at(i), q, dns[k]);
     }
+  }
+  if constexpr (ROWS > 1) {          // the rows' lanes, in a fixed order
+#pragma unroll
+    for (int d = LANES; d < 64; d <<= 1)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        cpre[0][j] += __shfl_xor(cpre[0][j], d);
+        cpost[0][j] += __shfl_xor(cpost[0][j], d);
+        cgate[0][j] += __shfl_xor(cgate[0][j], d);
+      }
+    if (threadIdx.x >= LANES) return;
   }
   if constexpr (NV > 0) {
 #pragma unroll
@@ -402,20 +419,28 @@ __global__ __launch_bounds__(1024) void norm_columns_kernel(ColumnSums sums, int
 // columns' sums are written and read once more (us with 256 / 512 / 1024 / 2048 workgroups: 8192 x 4096 170 / 171 / 185 / -, 4000 x 1024 61 / 42 / 44 / -,
 // 20000 x 300 309 / 170 / 97 / 62).
 inline int threads_of(long long q) { return q <= 512 ? 64 : q <= 2048 ? 256 : q <= 8192 ? 512 : 1024; }
+inline int lanes_of(long long q) { return q <= 64 ? 8 : q <= 128 ? 16 : q <= 256 ? 32 : 64; }
 int groups_of(const BlockNormArgs& a) {
-  const long long most = a.q > 8192 ? 256 : 131072 / threads_of(a.q), g = (a.M + 1) / 2;
+  const long long sets = 64 / lanes_of(a.q), rows = (a.M + sets - 1) / sets;
+  const long long most = a.q > 8192 ? 256 : 131072 / threads_of(a.q), g = rows < 256 ? rows : rows / 2 > 256 ? rows / 2 : 256;
   return (int)(g < most ? g : most);
 }
 inline size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
-template <typename ST, typename FT, int TH, int NV>
+template <typename ST, typename FT, int TH, int NV, int LANES = 64>
 hipError_t forward_rows(const BlockNormArgs& a, hipStream_t s) {
-  for (long long r = 0; r < a.M; r += MOST_ROWS)
-    hipLaunchKernelGGL((norm_forward_kernel<ST, FT, TH, NV>), dim3((unsigned)(a.M - r < MOST_ROWS ? a.M - r : MOST_ROWS)), dim3(TH), 0, s, a, r);
+  const long long rows = MOST_ROWS * (64 / LANES);
+  for (long long r = 0; r < a.M; r += rows) {
+    const long long n = a.M - r < rows ? a.M - r : rows;
+    hipLaunchKernelGGL((norm_forward_kernel<ST, FT, TH, NV, LANES>), dim3((unsigned)((n + 64 / LANES - 1) / (64 / LANES))), dim3(TH), 0, s, a, r);
+  }
   return hipGetLastError();
 }
 template <typename ST, typename FT>
 hipError_t forward_sizes(const BlockNormArgs& a, hipStream_t s) {
+  if (a.q <= 64) return forward_rows<ST, FT, 64, 1, 8>(a, s);
+  if (a.q <= 128) return forward_rows<ST, FT, 64, 1, 16>(a, s);
+  if (a.q <= 256) return forward_rows<ST, FT, 64, 1, 32>(a, s);
   if (a.q <= 512) return forward_rows<ST, FT, 64, 1>(a, s);
   if (a.q <= 2048) return forward_rows<ST, FT, 256, 1>(a, s);
   if (a.q <= 4096) return forward_rows<ST, FT, 512, 1>(a, s);
@@ -425,12 +450,15 @@ hipError_t forward_sizes(const BlockNormArgs& a, hipStream_t s) {
 }
 template <typename ST, typename FT>
 hipError_t backward_sizes(const BlockNormArgs& a, const ColumnSums& c, int groups, hipStream_t s) {
-#define NORM_BACKWARD(TH, NV) hipLaunchKernelGGL((norm_backward_kernel<ST, FT, TH, NV>), dim3((unsigned)groups), dim3(TH), 0, s, a, c)
-  if (a.q <= 512) NORM_BACKWARD(64, 1);
-  else if (a.q <= 2048) NORM_BACKWARD(256, 1);
-  else if (a.q <= 4096) NORM_BACKWARD(512, 1);
-  else if (a.q <= 8192) NORM_BACKWARD(512, 2);
-  else NORM_BACKWARD(1024, 0);
+#define NORM_BACKWARD(TH, NV, LANES) hipLaunchKernelGGL((norm_backward_kernel<ST, FT, TH, NV, LANES>), dim3((unsigned)groups), dim3(TH), 0, s, a, c)
+  if (a.q <= 64) NORM_BACKWARD(64, 1, 8);
+  else if (a.q <= 128) NORM_BACKWARD(64, 1, 16);
+  else if (a.q <= 256) NORM_BACKWARD(64, 1, 32);
+  else if (a.q <= 512) NORM_BACKWARD(64, 1, 64);
+  else if (a.q <= 2048) NORM_BACKWARD(256, 1, 64);
+  else if (a.q <= 4096) NORM_BACKWARD(512, 1, 64);
+  else if (a.q <= 8192) NORM_BACKWARD(512, 2, 64);
+  else NORM_BACKWARD(1024, 0, 64);
 #undef NORM_BACKWARD
   return hipGetLastError();
 }
