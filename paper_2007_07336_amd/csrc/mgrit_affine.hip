@@ -559,15 +559,30 @@ template <typename T> __device__ __forceinline__ void store4(T* p, floatx4 v, lo
 // X in 8 bits: four entries from a multiple of 4 on are within a block, whose scale lies with its slab's
 struct Mx8 {};
 typedef float floatx2p __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float scale8(const Packed& p, long long row, long long k) {
+  const int block = (int)(k >> 5) & 7;
+  const unsigned byte = p.scales[((k >> 8) * p.rows + row) * 8 + (block & 1) * 4 + (block >> 1)];
+  return byte == 255u ? NAN : __builtin_bit_cast(float, byte ? byte << 23 : 0x00400000u);
+}
 __device__ __forceinline__ floatx4 load4(const Packed& p, long long row, long long k, long long n) {
   floatx4 r = {0.0f, 0.0f, 0.0f, 0.0f};
   if (n <= 0) return r;              // (codes behind the last column are zero)
-  const int block = (int)(k >> 5) & 7;
   const unsigned c = *reinterpret_cast<const unsigned*>(p.codes + row * p.pitch + k);
-  const unsigned byte = p.scales[((k >> 8) * p.rows + row) * 8 + (block & 1) * 4 + (block >> 1)];
-  const float scale = byte == 255u ? NAN : __builtin_bit_cast(float, byte ? byte << 23 : 0x00400000u);
+  const float scale = scale8(p, row, k);
   const floatx2p a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.0f, true);
   return floatx4{a[0] * scale, a[1] * scale, b[0] * scale, b[1] * scale};
+}
+// Eight from a multiple of 8 on, of which `left` exist (zeros behind them, whatever the block's scale); one
+__device__ __forceinline__ void load8(const Packed& p, long long row, long long k, long long left, float (&v)[8]) {
+  const uint2 c = *reinterpret_cast<const uint2*>(p.codes + row * p.pitch + k);
+  const float scale = scale8(p, row, k);
+  const floatx2p a[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.x, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.x, 1.0f, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.y, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c.y, 1.0f, true)};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = j < left ? a[j / 2][j % 2] * scale : 0.0f;
+}
+__device__ __forceinline__ float load1(const Packed& p, long long row, long long k) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((unsigned)p.codes[row * p.pitch + k], 1.0f, false)[0] * scale8(p, row, k);
 }
 template <typename T> __device__ __forceinline__ floatx4 load4_of(const void* p, const Packed& kept, long long row, long long K, long long k, long long n) {
   if constexpr (std::is_same<T, Mx8>::value) return load4(kept, row, k, n);
@@ -582,7 +597,7 @@ struct ThinArgs {
   int chunk, chunks;                  // rows of a workgroup, at most THIN_ROWS
   int outS_type, outT_type;
   float scale;
-  Packed kept;                        // S or T, whichever is Mx8
+  Packed kept, f8;                    // S or T, whichever is Mx8; the factors, if f says that there are some and they have codes
 };
 constexpr int THIN_ROWS = 256;
 
@@ -609,7 +624,8 @@ __global__ __launch_bounds__(256) void thin_backward_kernel(ThinArgs a) {
     float v = 0.0f;
     if (e < a.nt) {
       const long long at = a.by_column ? (r0 + r) * a.F + e : e * a.F + r0 + r;
-      v = f ? widen(g[at]) * widen(f[at]) : a.scale * widen(g[at]);
+      if (f && a.f8.codes) v = widen(g[at]) * (a.by_column ? load1(a.f8, r0 + r, e) : load1(a.f8, e, r0 + r));
+      else v = f ? widen(g[at]) * widen(f[at]) : a.scale * widen(g[at]);
     }
     G[r][e] = v;
   }
@@ -1064,12 +1080,13 @@ struct LayJob {
   const void* p;  const void* f;
   void* out;  float* sums;
   long long rows, K, ldo;
-  int span, kind;                     // kind: type + 2 * (CT is bf16) + 4 * (there are factors) + 8 * (no planes, sums only)
+  int span, kind;                     // kind: type + 2 * (CT is bf16) + 4 * (there are factors) + 8 * (no planes, sums only) + 16 * (p8 or f8)
   float scale;
   unsigned first;                     // workgroup
+  Packed packed;                      // p (without factors) or f in 8 bits
 };
 struct LayJobs { LayJob j[4]; int n; };
-template <typename T, typename CT, int PARTS, bool HF>
+template <typename T, typename CT, int PARTS, bool HF, bool EIGHT = false>
 __device__ __forceinline__ void lay_out(const LayJob& a, unsigned block, float (&sh)[8][256]) {
   const T *p = static_cast<const T*>(a.p), *f = static_cast<const T*>(a.f);
   CT* out = static_cast<CT*>(a.out);
@@ -1083,16 +1100,19 @@ __device__ __forceinline__ void lay_out(const LayJob& a, unsigned block, float (
     for (long long r = r0 + t / 32; r < r1; r += 8) {
       const long long at = r * K + k;
       float v[8], b[8];
-      if (whole) {
+      if (EIGHT && !HF) {
+        load8(a.packed, r, k, left, v);
+      } else if (whole) {
         load8(p + at, v);
-        if (HF) load8(f + at, b);
+        if (HF && !EIGHT) load8(f + at, b);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           v[j] = j < left ? widen(p[at + j]) : 0.0f;
-          if (HF) b[j] = j < left ? widen(f[at + j]) : 0.0f;
+          if (HF && !EIGHT) b[j] = j < left ? widen(f[at + j]) : 0.0f;
         }
       }
+      if (HF && EIGHT) load8(a.packed, r, k, left, b);       // (codes and scales reach as far as ldo)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (HF) v[j] *= b[j];
@@ -1144,6 +1164,14 @@ __global__ __launch_bounds__(256) void lay_out_kernel(LayJobs jobs, unsigned bef
     case 9: lay_out<__bf16, float, 0, false>(a, block, sh); break;
     case 12: lay_out<float, float, 0, true>(a, block, sh); break;
     case 13: lay_out<__bf16, float, 0, true>(a, block, sh); break;
+    case 17: lay_out<__bf16, float, 1, false, true>(a, block, sh); break;
+    case 19: lay_out<__bf16, __bf16, 1, false, true>(a, block, sh); break;
+    case 20: lay_out<float, float, 1, true, true>(a, block, sh); break;
+    case 21: lay_out<__bf16, float, 1, true, true>(a, block, sh); break;
+    case 22: lay_out<float, __bf16, 3, true, true>(a, block, sh); break;
+    case 23: lay_out<__bf16, __bf16, 2, true, true>(a, block, sh); break;
+    case 28: lay_out<float, float, 0, true, true>(a, block, sh); break;
+    case 29: lay_out<__bf16, float, 0, true, true>(a, block, sh); break;
   }
 }
 // out[col] = sum over the chunks; 64 columns and sixteen sets of chunks per workgroup
@@ -1208,7 +1236,7 @@ inline int slab_of(bool bf16) { return bf16 ? 64 : 32; }
 inline bool few_tiles(const Product& q) { return (q.I + 255) / 256 * ((q.J + 255) / 256) < 128; }
 inline bool whole_slabs(const Operand& o, bool bf16) { return o.kslow || o.ld % slab_of(bf16) == 0; }
 inline bool in_place(const Operand& o, bool bf16, long long Kc, bool any_pieces) {
-  if (o.f || (o.type != 0) != bf16) return false;
+  if (o.f || o.p8 || (o.type != 0) != bf16) return false;
   return o.ld % (bf16 ? 8 : 4) == 0 && (o.kslow || ((any_pieces || whole_slabs(o, bf16)) && (o.ld == Kc || o.padded)));
 }
 // The launch that lays out, as it comes together, and what it takes of the workspace
@@ -1221,10 +1249,12 @@ struct Layout {
 
   char* take(size_t n) { char* p = base + bytes; bytes += up(n); return p; }
   // (ldo 0: no planes, sums only.  Not `out`, which may be null where sizes alone are asked for)
-  void add(const void* p, const void* f, int type, bool bf16, long long rows, long long K, void* out, long long ldo, int span, float scale, float* sums) {
+  void add(const void* p, const void* f, int type, bool bf16, long long rows, long long K, void* out, long long ldo, int span, float scale, float* sums,
+           const Packed* packed) {
     const bool planes = ldo > 0;
     LayJob& j = jobs.j[jobs.n++];
-    j = LayJob{p, f, out, sums, rows, K, ldo, span, type + 2 * (planes && bf16) + (f ? 4 : 0) + (planes ? 0 : 8), scale, (unsigned)blocks};
+    j = LayJob{p, f, out, sums, rows, K, ldo, span, type + 2 * (planes && bf16) + (f ? 4 : 0) + (planes ? 0 : 8) + (packed ? 16 : 0), scale, (unsigned)blocks,
+               packed ? *packed : Packed{}};
     blocks += ((planes ? ldo : K) + 255) / 256 * ((rows + span - 1) / span);
     moved += (double)rows * ((double)K * (type ? 2 : 4) * (f ? 2 : 1) + (double)ldo * (bf16 ? 2 * bf16_parts(type, f) : 4));
   }
@@ -1237,7 +1267,7 @@ struct Layout {
     n.parts = bf16 ? bf16_parts(o.type, o.f) : 1;
     n.p = take((size_t)n.parts * r * ld * (bf16 ? 2 : 4));
     n.ld = ld; n.type = bf16; n.kslow = o.kslow; n.padded = 1; n.part = r * ld;
-    add(o.p, o.f, o.type, bf16, r, k, const_cast<void*>(n.p), ld, lay_span(r, (ld + 255) / 256), 1.0f, nullptr);
+    add(o.p, o.f, o.type, bf16, r, k, const_cast<void*>(n.p), ld, lay_span(r, (ld + 255) / 256), 1.0f, nullptr, o.f ? o.f8 : o.p8);
     return n;
   }
   hipError_t launch(hipStream_t s) const {
@@ -1413,6 +1443,7 @@ bool forward_bf16(const Product& q) {
 Product input_product(const BackwardArgs& b) {
   Product q = {};
   q.A = Operand{b.dY, b.D, b.F, b.ytype, 0};
+  if (b.D && b.D8.codes) q.A.f8 = &b.D8;
   q.B = Operand{b.W, nullptr, b.K, b.wtype, 1};
   q.e = Epilogue{0, 0, b.dxtype, b.scale, nullptr, nullptr, b.dX, nullptr};
   q.I = b.M; q.J = b.K; q.Kc = b.F;
@@ -1422,6 +1453,8 @@ Product weight_product(const BackwardArgs& b) {
   Product q = {};
   q.A = Operand{b.dY, b.D, b.F, b.ytype, 1};
   q.B = Operand{b.X, nullptr, b.K, b.xtype, 1};
+  if (b.X8.codes) q.B.p8 = &b.X8;
+  if (b.D && b.D8.codes) q.A.f8 = &b.D8;
   q.e = Epilogue{0, 0, 0, b.scale, nullptr, nullptr, b.dW, nullptr};
   q.I = b.F; q.J = b.K; q.Kc = b.M;
   return q;
@@ -1456,12 +1489,12 @@ BackwardPlan lay_backward(const BackwardArgs& b, char* base, bool x_bf16, bool w
     g.type = bf16; g.padded = 1; g.parts = bf16 ? bf16_parts(b.ytype, b.D) : 1; g.part = b.M * g.ld;
     g.p = p.lay.take((size_t)g.parts * g.part * (bf16 ? 2 : 4));
     p.lay.add(b.dY, b.D, b.ytype, bf16, b.M, b.F, const_cast<void*>(g.p), g.ld, summed ? lay_span(b.M, (g.ld + 255) / 256) : sum_span(b.M), b.scale,
-              summed ? nullptr : p.sums);
+              summed ? nullptr : p.sums, b.D && b.D8.codes ? &b.D8 : nullptr);
     summed = true;
     if (for_x) p.x.A = g;
     if (for_w) { p.w.A = g; p.w.A.kslow = 1; }
   }
-  if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums);
+  if (!summed) p.lay.add(b.dY, b.D, b.ytype, false, b.M, b.F, nullptr, 0, sum_span(b.M), b.scale, p.sums, b.D && b.D8.codes ? &b.D8 : nullptr);
   if (x) p.x.B = p.lay.plane(p.x.B, x_bf16, p.x.J, p.x.Kc, few_tiles(p.x));
   if (w) p.w.B = p.lay.plane(p.w.B, w_bf16, p.w.J, p.w.Kc, few_tiles(p.w));
   return p;
@@ -1544,9 +1577,10 @@ hipError_t launch_thin(const BackwardArgs& b, const ThinPlan& p, char* ws, hipSt
   a.outS_type = c ? b.dxtype : 0;  a.outT_type = c ? 0 : b.dxtype;
   a.scale = b.scale;
   const int ts = c ? b.xtype : b.wtype, tt = c ? b.wtype : b.xtype;
-  a.kept = b.kept;
+  a.kept = b.X8;
+  a.f8 = b.D8;
   hipError_t e;
-  if (b.kept.codes) e = c ? (tt ? launch_thin_y<Mx8, __bf16>(a, b.ytype, s) : launch_thin_y<Mx8, float>(a, b.ytype, s))
+  if (b.X8.codes) e = c ? (tt ? launch_thin_y<Mx8, __bf16>(a, b.ytype, s) : launch_thin_y<Mx8, float>(a, b.ytype, s))
                           : (ts ? launch_thin_y<__bf16, Mx8>(a, b.ytype, s) : launch_thin_y<float, Mx8>(a, b.ytype, s));
   else e = ts ? (tt ? launch_thin_y<__bf16, __bf16>(a, b.ytype, s) : launch_thin_y<__bf16, float>(a, b.ytype, s))
                     : (tt ? launch_thin_y<float, __bf16>(a, b.ytype, s) : launch_thin_y<float, float>(a, b.ytype, s));
@@ -1622,7 +1656,10 @@ size_t backward_workspace(const BackwardArgs& b) {
   return n;
 }
 
-bool backward_reads_kept(const BackwardArgs& b) { return thin_plan(b).thin; }
+bool backward_reads_kept(const BackwardArgs& b) {
+  // (the tiles for offsets beyond 32 bits read their operands as they lie)
+  return thin_plan(b).thin || (wide_sizes(input_product(b)) && wide_sizes(weight_product(b)));
+}
 
 hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s) {
   const ThinPlan t = thin_plan(b);

@@ -5,6 +5,13 @@
 
 namespace mgrit {
 
+// A packed array: codes [rows][pitch bytes], scales [slabs][rows][8] (a slab is 256 columns)
+struct Packed {
+  unsigned char* codes;
+  unsigned char* scales;
+  long long rows, cols, slabs, pitch;
+  int format;
+};
 // One operand of a product C[i][j] = sum_k A(i, k) B(j, k): entry (r, k) lies at p[r * ld + k], or with kslow at p[k * ld + r].
 // With a factor it is p * f, entry by entry (the gradient at an activation's input; f has p's type and layout).
 struct Operand {
@@ -16,6 +23,8 @@ struct Operand {
   // set for planes in the workspace: rows end in zeros up to ld, and the operand is the sum of `parts` planes, `part` entries apart, each on its scale
   int padded, parts;
   long long part;
+  // in 8 bits, p and f only saying whether there is one: p itself, and the factor
+  const Packed *p8, *f8;
 };
 // What becomes of a sum.  Forward (fwd): z = sum + bias, out = R + scale act(z), D = scale act'(z); else out = scale sum.
 struct Epilogue {
@@ -38,13 +47,6 @@ hipError_t launch_product(const Product& q, void* ws, hipStream_t s);
 // out = what e makes of the sums of `parts` arrays [I][J], one behind the other
 hipError_t join_parts(const Epilogue& e, const float* partial, int parts, long long I, long long J, hipStream_t s);
 
-// A packed array: codes [rows][pitch bytes], scales [slabs][rows][8] (a slab is 256 columns)
-struct Packed {
-  unsigned char* codes;
-  unsigned char* scales;
-  long long rows, cols, slabs, pitch;
-  int format;
-};
 // The backward pass of an end layer: G = dY * D (D null: dY, with `scale` on every result), dX = G W, dW = G^T X, db = column
 // sums of G; dX, dW, db null where they are not wanted.
 struct BackwardArgs {
@@ -53,10 +55,10 @@ struct BackwardArgs {
   float scale;
   const void* X;  const void* W;  const void* D;  const void* dY;
   void* dX;  float* dW;  float* db;
-  Packed kept;                       // X in 8 bits (xtype and X count no more), for products that read it so
+  Packed X8, D8;                     // X and D in 8 bits (with codes; xtype is bf16 then, X and D only say whether there is one)
 };
 size_t     backward_workspace(const BackwardArgs& b);
-bool       backward_reads_kept(const BackwardArgs& b);
+bool       backward_reads_kept(const BackwardArgs& b);                     // whether launch_backward takes X8 and D8, or they have to be unpacked
 hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s);
 hipError_t launch_zero(float* out, long long n, hipStream_t s);
 

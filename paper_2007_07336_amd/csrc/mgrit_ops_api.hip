@@ -92,18 +92,23 @@ PackedProduct packed_product(const mgrit_affine_packed_t* p, const void* X, cons
   q.e = Epilogue{1, p->act, p->ytype, p->scale, b, R, Y, D};
   return q;
 }
-// What a backward pass from kept activations unpacks: D as its type and, where it is not read as it is, X as bf16; the rest of the workspace behind them
+// What a backward pass from kept activations has to unpack first: X as bf16 and D as its type, where the products do not read them as they are; the rest of the
+// workspace behind them
 struct KeptPlaces { bool reads; size_t D, bytes; };
 KeptPlaces kept_places(const mgrit_affine_t* p) {
   KeptPlaces k = {};
-  k.reads = backward_reads_kept(BackwardArgs{p->M, p->K, p->F});
+  k.reads = backward_reads_kept(BackwardArgs{p->M, p->K, p->F, MGRIT_BF16, p->wtype, p->ytype, p->xtype});
   k.D = k.reads ? 0 : up((size_t)p->M * p->K * 2);
-  k.bytes = k.D + up((size_t)p->M * p->F * (p->ytype ? 2 : 4));
+  k.bytes = k.reads ? 0 : k.D + up((size_t)p->M * p->F * (p->ytype ? 2 : 4));
   return k;
 }
 BackwardArgs kept_args(const mgrit_affine_t* p, const void* X, const void* W, const void* D, const void* dY, void* dX, float* dW, float* db) {
   BackwardArgs b = backward_args(p, X, W, D, dY, dX, dW, db);
   b.xtype = MGRIT_BF16;
+  if (kept_places(p).reads) {
+    if (X) b.X8 = packed_view(p->M, p->K, MGRIT_MX8, const_cast<void*>(X));
+    if (D) b.D8 = packed_view(p->M, p->F, MGRIT_MX8, const_cast<void*>(D));
+  }
   return b;
 }
 
@@ -285,16 +290,16 @@ int32_t mgrit_affine_kept_backward(const mgrit_affine_t* p, const void* X, const
   if (!dX && !dW && !db) return MGRIT_OK;
   const KeptPlaces at = kept_places(p);
   char* base = static_cast<char*>(workspace);
-  const Packed X8 = packed_view(p->M, p->K, MGRIT_MX8, const_cast<void*>(X));
-  Unpack u[2];
-  int n = 0;
-  if (dW && !at.reads) u[n++] = Unpack{X8, base, MGRIT_BF16, p->K};
-  if (D) u[n++] = Unpack{packed_view(p->M, p->F, MGRIT_MX8, const_cast<void*>(D)), base + at.D, p->ytype, p->F};
-  hipError_t e = n ? launch_unpack(u, n, s) : hipSuccess;
-  if (e != hipSuccess) return MGRIT_ERR_HIP;
-  BackwardArgs b = kept_args(p, base, W, D ? base + at.D : nullptr, dY, dX, dW, db);
-  if (at.reads) b.kept = X8;
-  return launch_backward(b, base + at.bytes, s) == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
+  if (!at.reads) {
+    Unpack u[2];
+    int n = 0;
+    if (dW) u[n++] = Unpack{packed_view(p->M, p->K, MGRIT_MX8, const_cast<void*>(X)), base, MGRIT_BF16, p->K};
+    if (D) u[n++] = Unpack{packed_view(p->M, p->F, MGRIT_MX8, const_cast<void*>(D)), base + at.D, p->ytype, p->F};
+    if (n && launch_unpack(u, n, s) != hipSuccess) return MGRIT_ERR_HIP;
+    X = base;
+    if (D) D = base + at.D;
+  }
+  return launch_backward(kept_args(p, X, W, D, dY, dX, dW, db), base + at.bytes, s) == hipSuccess ? MGRIT_OK : MGRIT_ERR_HIP;
 }
 
 int32_t mgrit_block_norm_forward(const mgrit_block_norm_t* p, const void* f, const void* r, const void* gate, const float* w_post,

@@ -5,7 +5,7 @@ import torch
 import paper_2007_07336_amd as M
 from tests.ops_util import near, normal, sum_bound
 from tests.test_gpu_block_norm import Block
-from tests.test_gpu_packed import PackedLayer, packed, unpacked, values_of
+from tests.test_gpu_packed import PackedLayer, kept, packed, run_kept, unpacked, values_of
 from tests.test_gpu_sample import call, check, uniform, whole
 
 pytestmark = pytest.mark.gpu
@@ -78,6 +78,18 @@ def test_norms_of_very_long_rows(rows, q):
 @pytest.mark.parametrize("form", ["bf16", "mx4"])
 def test_packed_layers_of_extreme_shapes(rows, K, F, form):
     PackedLayer(rows, K, F, "b", form, "f", "identity", seed=7).check()
+
+
+@pytest.mark.parametrize("act", ["tanh", "identity"])
+def test_kept_activations_of_a_layer_of_a_million_outputs(act):
+    """Too wide for the tiles that read activations in 8 bits: they are unpacked first."""
+    rows, K, F = 20, 24, (1 << 20) + 3
+    a, X, X8, D, D8 = kept(rows, K, F, "fff", act, 3)
+    dX, dW, db = run_kept(a, X8, D8)
+    G = a.dY.double() * (D.double() if D is not None else a.scale)
+    near(dX, G @ a.W.double(), sum_bound(G, a.W.double().T, F + 2), "dX")
+    near(dW, G.T @ X.double(), sum_bound(G.T, X.double().T, rows + 2), "dW")
+    near(db, G.sum(0), (rows + 4) * 2.0 ** -23 * G.abs().sum(0) + rows * 2.0 ** -126, "db")
 
 
 def test_calls_at_once_on_two_streams():
