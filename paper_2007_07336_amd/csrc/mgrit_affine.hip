@@ -1193,6 +1193,11 @@ __global__ __launch_bounds__(1024) void add_chunks_kernel(const float* part, int
     __syncthreads();
   }
 }
+hipError_t add_chunks(const float* part, int chunks, long long F, float* out, hipStream_t s) {
+  const long long blocks = (F + 63) / 64;
+  hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(1024), 0, s, part, chunks, F, out);
+  return hipGetLastError();
+}
 
 __global__ __launch_bounds__(256) void zero_kernel(float* out, long long n) {
   for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) out[i] = 0.0f;
@@ -1605,11 +1610,6 @@ hipError_t join_parts(const Epilogue& e, const float* partial, int parts, long l
   return hipGetLastError();
 }
 
-hipError_t add_chunks(const float* part, int chunks, long long F, float* out, hipStream_t s) {
-  const long long blocks = (F + 63) / 64;
-  hipLaunchKernelGGL(add_chunks_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(1024), 0, s, part, chunks, F, out);
-  return hipGetLastError();
-}
 
 size_t product_workspace(const Product& q) {
   const FewPlan f = few_plan(q);

@@ -62,9 +62,6 @@ bool       backward_reads_kept(const BackwardArgs& b);                     // wh
 hipError_t launch_backward(const BackwardArgs& b, void* ws, hipStream_t s);
 hipError_t launch_zero(float* out, long long n, hipStream_t s);
 
-// out[col] = sum over the chunks of part[chunk][col]
-hipError_t add_chunks(const float* part, int chunks, long long F, float* out, hipStream_t s);
-
 Packed     packed_view(long long rows, long long cols, int format, void* p);
 size_t     packed_bytes(long long rows, long long cols, int format);
 // rows at X, cols entries each

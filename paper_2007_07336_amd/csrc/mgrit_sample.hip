@@ -29,10 +29,6 @@ __device__ __forceinline__ u64 shuffle_xor(u64 v, int d) {
   const unsigned lo = __shfl_xor((unsigned)v, d), hi = __shfl_xor((unsigned)(v >> 32), d);
   return (u64)hi << 32 | lo;
 }
-__device__ __forceinline__ u64 shuffle(u64 v, int lane) {
-  const unsigned lo = __shfl((unsigned)v, lane), hi = __shfl((unsigned)(v >> 32), lane);
-  return (u64)hi << 32 | lo;
-}
 // Sum over the lanes up to and with this one
 __device__ __forceinline__ u64 sum_up(u64 v, int lane) {
 #pragma unroll
@@ -90,8 +86,8 @@ template <int TH> struct Shared {
   unsigned bad[16];
 };
 
-// The row's vectors, a contiguous part of the row for each wavefront: in LDS (HELD), each at the thread that uses it, or read again.  (In registers, where an index has to be known, every pass is unrolled
-// and the compiler keeps keys and doubles of one pass for the next, two thousand registers too many.)
+// The row's vectors, a contiguous part of the row for each wavefront: in LDS (HELD), each at the thread that uses it, or read again.  (In registers, where an
+// index has to be known, every pass is unrolled, and the compiler keeps keys and doubles of one pass for the next, two thousand registers too many.)
 template <typename T, int TH, bool HELD>
 struct Row {
   static constexpr int N = Eight<T>::N;
@@ -156,7 +152,7 @@ struct Row {
       for (int j = 0; j < N; ++j) f(entry<T>(v, j), k + j);
     }
   }
-  // measure(x, index, whether it takes part) of this lane's vector, zero without looking at it where no lane has one that passes
+  // measure(x) of those of this lane's vector that take part, zero of the others; false, and nothing computed, where no lane has one that does
   template <typename P, typename M> __device__ __forceinline__ bool measures(int wave, int i, u64 (&m)[N], P part, M measure) const {
     const u32x4 v = vec(wave, i);
     const unsigned k = at(wave, i);
@@ -453,7 +449,7 @@ template <int TH> __device__ __forceinline__ u64 sum_before(u64 v, u64* all, Sha
 }
 // The whole answer where the first k of the order are few.  The k'th largest of the threads' largest logits is at most the k'th largest of all, so the
 // classes from there on hold the first k and little else; they are put in order by comparing each with each.  mine: this thread's largest; returns false if
-// they are more than the threads.  yleast: the least weight asked for.
+// they are more than the threads.  least: the least weight asked for, in the weights' units.
 struct Answer { bool done; unsigned at; u64 sum; };
 template <typename T, int TH, bool HELD>
 __device__ __forceinline__ Answer few_ones(const Row<T, TH, HELD>& row, float mine, float top, float low, int k, float p, double least, float u, const Weights& w,
@@ -478,7 +474,7 @@ __device__ __forceinline__ Answer few_ones(const Row<T, TH, HELD>& row, float mi
   __syncthreads();                                               // (the bins have been read)
   const float behind = (int)sh.bin < BINS - 1 ? (float)(sh.bin + 1) : INFINITY;
   row.each([&](float x, unsigned at) {
-    const bool have = x > -INFINITY && !((half - x * 0.5f) * rate >= behind);
+    const bool have = x > -INFINITY && (behind == INFINITY || !((half - x * 0.5f) * rate >= behind));
     const unsigned slot = slot_for<TH>(have, sh);
     if (slot < TH) sh.candidates[slot] = Candidate{key_of(x), at, 0};
   });

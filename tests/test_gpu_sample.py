@@ -209,3 +209,18 @@ def test_rows_that_crowd_into_few_bins(dtype, V):
         check(x, u, k=torch.full((8,), k, dtype=torch.int32, device="cuda"))
     check(x, u, p=uniform(8, 2, 0.1, 1.0))
     check(x, u, t=uniform(8, 3, 0.01, 3.0), p=uniform(8, 2, 0.5, 1.0), k=torch.full((8,), V // 3, dtype=torch.int32, device="cuda"))
+
+
+def test_logits_that_are_all_but_equal():
+    """Differences far below the smallest normal float: the order is theirs, the weights are all the same."""
+    V = 700
+    x = (torch.arange(V, dtype=torch.float64) * 2.0 ** -149).to(torch.float32).flip(0)[None].repeat(6, 1)
+    x[1] = -x[1]
+    x[2] = x[2] * 2.0 ** 20
+    x[3, ::2] = 0.0
+    x = x.cuda()
+    u = uniform(6, 1)
+    check(x, u, k=whole(6, 2, 30, 2))
+    check(x, u, k=whole(6, 2, 30, 2), p=uniform(6, 3, 0.2, 0.9), least=uniform(6, 4, 0.0, 1.0))
+    check(x, u, k=torch.full((6,), 500, dtype=torch.int32, device="cuda"), p=uniform(6, 3, 0.2, 0.9))
+    check(x, u, p=uniform(6, 3, 0.2, 0.9))
