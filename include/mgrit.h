@@ -407,7 +407,7 @@ int32_t mgrit_block_norm_backward(const mgrit_block_norm_t* p, const void* f, co
  * kept weights, logprob <- log(w_v / the sum of the kept weights).  t = 0: the largest logit, lowest index first, logprob 0.
  * Logits of minus infinity have weight zero.  A row that holds a NaN, +infinity or nothing but minus infinity, or whose t is negative, infinite or NaN, whose u is
  * not in [0, 1), or whose top_p or min_p is NaN, gives index -1 and logprob NaN.
- * Weights are computed to 1e-13 and summed as integers, 2^-(62 - log2 V) each: the same class every time, however the sums are formed. */
+ * Weights are computed to 1e-13 and summed as integers in units of 2^-min(50, 62 - log2 V): the same class every time, however the sums are formed. */
 typedef struct mgrit_sample {
   int32_t B, V;        /* rows >= 0, classes >= 1                                                                */
   int32_t dtype;       /* of the logits: MGRIT_FP32 or MGRIT_BF16                                                */
