@@ -198,6 +198,17 @@ def test_in_place_and_outputs_that_are_not_wanted():
         assert torch.equal(o, want["dpost"])
 
 
+@pytest.mark.parametrize("q", [40, 100, 200, 6000, 12000, 17000])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_forward_in_place_in_each_form(kind, q):
+    """S in r's place and Y in f's where several rows share a wavefront, where a row takes two vectors a thread and where it is read for every step."""
+    b = Block(5, q, kind, "feature", "ff", seed=q)
+    S, Y = b.forward()
+    f, r = b.f.clone(), b.r.clone()
+    M.mgrit_block_norm_forward(b.p, f, r, b.gate, b.post, b.pre, r, f)
+    assert torch.equal(r, S) and torch.equal(f, Y)
+
+
 def test_no_rows_and_rows_that_are_not_finite():
     b = Block(0, 40, gate="feature")
     b.forward()
