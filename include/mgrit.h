@@ -373,7 +373,8 @@ int32_t mgrit_affine_kept_backward(const mgrit_affine_t* p, const void* X, const
  * S is the stream behind the block, Y what the next block takes.  norm(x) = x / sqrt(mean(x^2) + eps), or with MGRIT_NORM_LAYER the same of
  * x less its mean, over the q features of a row.  w_post NULL: n = f; w_pre NULL: no Y.  The gate is absent, one value a feature
  * (float [q]) or one an entry ([M][q], type ftype).  r, S (and dS, dr) are of type stype, f, Y (and df, dY) of type ftype, weights and their
- * gradients float.  Y comes from S before that is rounded to its type.  With eps = 0 a row without deviation gives NaN. */
+ * gradients float.  Y comes from S before that is rounded to its type.  Entries that are all the same have no deviation from their mean, whatever its
+ * rounding; with eps = 0 a row without deviation gives NaN.  A deviation between 2^-126 and 2^126 is a float's, also where its square is none. */
 enum { MGRIT_NORM_ROOT = 0, MGRIT_NORM_LAYER = 1 };
 enum { MGRIT_GATE_NONE = 0, MGRIT_GATE_FEATURE = 1, MGRIT_GATE_ENTRY = 2 };
 typedef struct mgrit_block_norm {

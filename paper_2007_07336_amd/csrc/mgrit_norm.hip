@@ -27,6 +27,39 @@ template <int TH, int LANES, int N> __device__ __forceinline__ void sum_threads(
     place ^= 1;
   }
 }
+// Rows that are hard for floats are found by the mean square m of their deviations, and taken once more then.
+// Deviations from a mean that is far larger than they are: as a float that is a few ulps off, which may be as much as a deviation (of 10000.1 in each of 500 features
+// an ulp or two: 0.89 of a deviation with eps = 1e-6).  The deviations have few bits, so their mean is exact, or nearly, and is taken off them: nothing at all is left
+// where the entries are all the same.
+constexpr float LESS = 0x1p-24f;                                 // entries are summed times this: of the largest floats no sum overflows
+// The mean, a float for everyone: where the compiler takes the product into a subtraction it is not rounded, and deviations of one entry and another are from two means
+__device__ __forceinline__ float mean_of(float sum, float inv) {
+#pragma clang fp contract(off)
+  return sum * (inv * (1.0f / LESS));
+}
+__device__ __forceinline__ bool far_off(float mean, float m) { return mean * mean > 64.0f * m; }
+// Deviations whose squares no float holds, or with few bits: what they are multiplied by before they are squared, 1 for most
+__device__ __forceinline__ float squares_scale(float m, float eps) { return !(m < 0x1p100f) ? 0x1p-80f : m + eps < 0x1p-90f ? 0x1p96f : 1.0f; }
+// The reciprocal deviation from the mean square of deviations times c, times 1 / c
+__device__ __forceinline__ float reciprocal(float m, float eps, float c) { return 1.0f / sqrtf(m + eps * c * c); }
+// The reciprocal deviation.  square(c): the mean square of deviations times c; refine(): takes the deviations' mean off them, and returns it
+template <typename F, typename G> __device__ __forceinline__ float deviation(float mean, float eps, F square, G refine) {
+  float m = square(1.0f), c = 1.0f;
+  if (__builtin_expect(far_off(mean, m) || squares_scale(m, eps) != 1.0f, 0)) {
+    for (int again = 0; again < 5; ++again) {
+      if (far_off(mean * c, m)) {
+        mean = refine();
+        c = 1.0f;
+      } else if (c == 1.0f && squares_scale(m, eps) != 1.0f) {
+        c = squares_scale(m, eps);
+      } else {
+        break;
+      }
+      m = square(c);
+    }
+  }
+  return c * reciprocal(m, eps, c);
+}
 // Eight entries of a row from column k on; zeros where there are none
 template <typename T> __device__ __forceinline__ void take8(const T* p, long long k, long long q, float (&v)[8]) {
   if (k + 8 <= q) {
@@ -50,7 +83,8 @@ template <typename T> __device__ __forceinline__ void take_raw(const T* p, long 
     __builtin_memcpy(&v, e, sizeof(e));
   }
 }
-// d for entries that exist, zero behind them (of sums of deviations, which are not zero there)
+template <int NV> constexpr int ROUNDS = NV > 0 ? NV : 1;       // of a loop over a thread's eights that are unrolled
+// d for entries that exist, zero behind them (deviations from a mean are not zero there)
 __device__ __forceinline__ float there(float d, long long k, long long q) { return k < q ? d : 0.0f; }
 
 // One row per workgroup of TH threads, or (LANES < 64) 64 / LANES rows, LANES lanes each.  NV > 0: the row's eights fit NV registers sets of each thread and are read once; NV = 0: they are read again
@@ -72,36 +106,61 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
   const float inv = 1.0f / (float)q;
   float x[HELD][8], y[HELD][8];
   auto at = [&](int i) { return ((long long)i * TH + thread) * 8; };
-  auto read_f = [&](int i) { if (NV == 0) take8(f, at(i), q, x[0]); };
   if constexpr (NV > 0) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) take8(f, at(i), q, x[i]);
 #pragma unroll
     for (int i = 0; i < NV; ++i) take8(r, at(i), q, y[i]);
   }
-  float mean = 0.0f, dev = 1.0f;
-  if (a.post) {
+  // the reciprocal deviation of the row that read(i) brings into v; of NV > 0 v becomes the deviations, zeros behind the last entry, of NV = 0 the entries' own
+  // are v - mean - less each time that they are read
+  auto normalize = [&](auto read, float (&v)[ROUNDS<NV>][8], float& mean, float& less) {
+    auto take_off = [&](float m) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = there(v[i][j] - m, at(i) + j, q);
+    };
     if (a.layer) {
       float s[1] = {};
-#pragma unroll U
+#pragma unroll ROUNDS<NV>
       for (int i = 0; i < n; ++i) {
-        read_f(i);
+        read(i);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += x[NV ? i : 0][j];
+        for (int j = 0; j < 8; ++j) s[0] = __builtin_fmaf(NV ? v[NV ? i : 0][j] : there(v[0][j], at(i) + j, q), LESS, s[0]);
       }
       sum_threads<TH, LANES>(s, sh, place);
-      mean = s[0] * inv;
+      mean = mean_of(s[0], inv);
+      take_off(mean);
     }
-    float s[1] = {};
-#pragma unroll U
-    for (int i = 0; i < n; ++i) {
-      read_f(i);
+    auto off = [&](int i, int j) { return NV ? v[NV ? i : 0][j] : there(v[0][j] - mean - less, at(i) + j, q); };
+    return deviation(mean, a.eps, [&](float c) {
+      float s[1] = {};
+#pragma unroll ROUNDS<NV>
+      for (int i = 0; i < n; ++i) {
+        read(i);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { const float d = there(x[NV ? i : 0][j] - mean, at(i) + j, q); s[0] += d * d; }
-    }
-    sum_threads<TH, LANES>(s, sh, place);
-    dev = 1.0f / sqrtf(s[0] * inv + a.eps);
-  }
+        for (int j = 0; j < 8; ++j) { const float d = off(i, j) * c; s[0] = __builtin_fmaf(d, d, s[0]); }
+      }
+      sum_threads<TH, LANES>(s, sh, place);
+      return s[0] * inv;
+    }, [&]() {
+      float s[1] = {};
+#pragma unroll ROUNDS<NV>
+      for (int i = 0; i < n; ++i) {
+        read(i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] += off(i, j);
+      }
+      sum_threads<TH, LANES>(s, sh, place);
+      const float m = s[0] / (float)q;
+      less += m;
+      take_off(m);
+      return m;
+    });
+  };
+  float mean = 0.0f, less = 0.0f, dev = 1.0f;
+  if (a.post) dev = normalize([&](int i) { if (NV == 0) take8(f, at(i), q, x[0]); }, x, mean, less);
   // y <- S
   auto stream = [&](int i) {
     const int h = NV ? i : 0;
@@ -112,51 +171,33 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
     if (feature) take8(feature, at(i), q, g);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float m = a.post ? (x[h][j] - mean) * dev * w[j] : x[h][j];
+      const float m = a.post ? (NV ? x[h][j] : x[0][j] - mean - less) * dev * w[j] : x[h][j];
       y[h][j] += a.scale * (entry || feature ? g[j] * m : m);
     }
   };
-  float smean = 0.0f, sdev = 1.0f;
   if constexpr (NV > 0) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       stream(i);
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[i][j] = there(y[i][j], at(i) + j, q);
+      give8(static_cast<ST*>(a.S) + row * q, at(i), q, y[i]);
     }
   }
-  if (a.pre) {
-    if (a.layer) {
-      float s[1] = {};
-#pragma unroll U
-      for (int i = 0; i < n; ++i) {
-        if (NV == 0) stream(i);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += there(y[NV ? i : 0][j], at(i) + j, q);
-      }
-      sum_threads<TH, LANES>(s, sh, place);
-      smean = s[0] * inv;
-    }
-    float s[1] = {};
-#pragma unroll U
-    for (int i = 0; i < n; ++i) {
-      if (NV == 0) stream(i);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) { const float d = there(y[NV ? i : 0][j] - smean, at(i) + j, q); s[0] += d * d; }
-    }
-    sum_threads<TH, LANES>(s, sh, place);
-    sdev = 1.0f / sqrtf(s[0] * inv + a.eps);
-  }
+  float smean = 0.0f, sless = 0.0f, sdev = 1.0f;
+  if (a.pre) sdev = normalize([&](int i) { if (NV == 0) stream(i); }, y, smean, sless);
 #pragma unroll U
   for (int i = 0; i < n; ++i) {
     const int h = NV ? i : 0;
-    if (NV == 0) stream(i);
-    give8(static_cast<ST*>(a.S) + row * q, at(i), q, y[h]);
+    if (NV == 0) {
+      stream(i);
+      give8(static_cast<ST*>(a.S) + row * q, at(i), q, y[0]);
+    }
     if (!a.pre) continue;
     float w[8];
     take8(a.pre, at(i), q, w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] *= (y[h][j] - smean) * sdev;
+    for (int j = 0; j < 8; ++j) w[j] *= (NV ? y[h][j] : y[0][j] - smean - sless) * sdev;
     give8(static_cast<FT*>(a.Y) + row * q, at(i), q, w);
   }
 }
@@ -165,8 +206,9 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
 // d (h - x^ mean(h x^)), with MGRIT_NORM_LAYER less mean(h) inside the brackets too.  A workgroup takes the rows b, b + G, .. and keeps the columns' sums
 // of its rows in registers; they go to part[array][b][q] and are added up by a second launch.
 struct ColumnSums { float* part[3]; };                           // of dw_pre, dw_post, dgate; null where not wanted
+// (a wavefront less on each SIMD where float arrays take two registers an entry anyway)
 template <typename ST, typename FT, int TH, int NV, int LANES>
-__global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, ColumnSums sums) {
+__global__ __launch_bounds__(TH, TH <= 256 && sizeof(ST) + sizeof(FT) < 8 ? 3 : 1) void norm_backward_kernel(BlockNormArgs a, ColumnSums sums) {
   __shared__ float sh[2][TH / 64][4];
   int place = 0;
   const long long q = a.q;
@@ -178,7 +220,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
   const int n = NV > 0 ? NV : (int)((q + 8 * TH - 1) / (8 * TH));
   constexpr int HELD = NV > 0 ? NV : 1, U = HELD;
   const float inv = 1.0f / (float)q;
-  float x[HELD][8], s[HELD][8], ds[HELD][8], h[HELD][8];         // f, S, the gradient by S, that by S's normalised row
+  float x[HELD][8], s[HELD][8], ds[HELD][8], h[HELD][8];         // f, S (or their deviations), the gradient by S, that by S's normalised row
   float cpre[HELD][8] = {}, cpost[HELD][8] = {}, cgate[HELD][8] = {};
   auto at = [&](int i) { return ((long long)i * TH + thread) * 8; };
   // NV = 1: the vectors stay in registers, and the next row is on its way while this one is computed (8192 x 4096 with all of it: one workgroup to a
@@ -211,13 +253,27 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
     const FT* dY = a.dY ? static_cast<const FT*>(a.dY) + row * q : nullptr;
     const FT* entry = entries ? static_cast<const FT*>(a.gate) + row * q : nullptr;
     const bool first = row == row0;
+    // means of f and S and of the deviations from them (layer); x, s become the deviations, zeros behind the last entry, or with NV = 0 each time that they are read
+    float fmean = 0.0f, smean = 0.0f, fless = 0.0f, sless = 0.0f;
+    auto take_off = [&](float fm, float sm) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (a.post) x[k][j] = there(x[k][j] - fm, at(k) + j, q);
+          if (a.pre) s[k][j] = there(s[k][j] - sm, at(k) + j, q);
+        }
+    };
+    auto off_f = [&](int i, int j) { return NV ? x[NV ? i : 0][j] : there(x[0][j] - fmean - fless, at(i) + j, q); };
+    auto off_s = [&](int i, int j) { return NV ? s[NV ? i : 0][j] : there(s[0][j] - smean - sless, at(i) + j, q); };
     auto load = [&](int i) {
       const int k = NV ? i : 0;
       take8(f, at(i), q, x[k]);
       if (dS) take8(dS, at(i), q, ds[k]);
-      if (!a.pre) return;
-      take8(S, at(i), q, s[k]);
-      take8(dY, at(i), q, h[k]);
+      if (a.pre) {
+        take8(S, at(i), q, s[k]);
+        take8(dY, at(i), q, h[k]);
+      }
     };
     auto get_gate = [&](int i, float (&g)[8]) {
       if constexpr (AHEAD) {
@@ -238,8 +294,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
 #pragma unroll
       for (int i = 0; i < NV; ++i) load(i);
     }
-    // sums of f and S (layer), and of h
-    float fmean = 0.0f, smean = 0.0f, hmean = 0.0f;
+    float hmean = 0.0f;
     if (a.layer) {
       float v[3] = {};
 #pragma unroll U
@@ -250,36 +305,82 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
         get_pre(i, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          v[0] += x[k][j];
-          if (a.pre) { v[1] += s[k][j]; v[2] += h[k][j] * w[j]; }
+          v[0] = __builtin_fmaf(x[k][j], LESS, v[0]);
+          if (a.pre) { v[1] = __builtin_fmaf(s[k][j], LESS, v[1]); v[2] = __builtin_fmaf(h[k][j], w[j], v[2]); }
         }
       }
       sum_threads<TH, LANES>(v, sh, place);
-      fmean = v[0] * inv; smean = v[1] * inv; hmean = v[2] * inv;
+      if (a.post) fmean = mean_of(v[0], inv);
+      if (a.pre) smean = mean_of(v[1], inv);
+      hmean = v[2] * inv;
+      take_off(fmean, smean);
     }
     float fdev = 1.0f, sdev = 1.0f, hs = 0.0f;
     {
-      float v[3] = {};
+      float v[3];                                                // means of (x cf)^2, (s cs)^2 and g s cs, with g the gradient by the normalised S
+      auto means = [&](float cf, float cs) {
+        v[0] = v[1] = v[2] = 0.0f;
 #pragma unroll U
-      for (int i = 0; i < n; ++i) {
-        const int k = NV ? i : 0;
-        if (NV == 0) load(i);
-        float w[8];
-        get_pre(i, w);
+        for (int i = 0; i < n; ++i) {
+          const int k = NV ? i : 0;
+          if (NV == 0) load(i);
+          float w[8];
+          get_pre(i, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float d = there(x[k][j] - fmean, at(i) + j, q);
-          v[0] += d * d;
-          if (a.pre) {
-            const float e = there(s[k][j] - smean, at(i) + j, q);
-            v[1] += e * e;
-            v[2] += h[k][j] * w[j] * e;
+          for (int j = 0; j < 8; ++j) {
+            const float d = off_f(i, j) * cf;
+            v[0] = __builtin_fmaf(d, d, v[0]);                   // (in so many words, so that a second time rounds as the first)
+            if (a.pre) {
+              const float e = off_s(i, j) * cs;
+              v[1] = __builtin_fmaf(e, e, v[1]);
+              v[2] = __builtin_fmaf(h[k][j] * w[j], e, v[2]);
+            }
           }
         }
+        sum_threads<TH, LANES>(v, sh, place);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) v[i] *= inv;
+      };
+      means(1.0f, 1.0f);
+      float cf = 1.0f, cs = 1.0f;
+      auto scale_f = [&]() { return a.post ? squares_scale(v[0], a.eps) : 1.0f; };
+      auto scale_s = [&]() { return a.pre ? squares_scale(v[1], a.eps) : 1.0f; };
+      if (__builtin_expect(far_off(fmean, v[0]) || far_off(smean, v[1]) || scale_f() != 1.0f || scale_s() != 1.0f, 0)) {
+        float fm = fmean, sm = smean;
+        for (int again = 0; again < 6; ++again) {                // (as in `deviation`)
+          if (far_off(fm * cf, v[0]) || far_off(sm * cs, v[1])) {
+            float t[2] = {};
+#pragma unroll U
+            for (int i = 0; i < n; ++i) {
+              if (NV == 0) load(i);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                t[0] += off_f(i, j);
+                if (a.pre) t[1] += off_s(i, j);
+              }
+            }
+            sum_threads<TH, LANES>(t, sh, place);
+            fm = a.post ? t[0] / (float)q : 0.0f;
+            sm = a.pre ? t[1] / (float)q : 0.0f;
+            fless += fm;
+            sless += sm;
+            take_off(fm, sm);
+            cf = cs = 1.0f;
+          } else {
+            const float nf = cf == 1.0f ? scale_f() : cf, ns = cs == 1.0f ? scale_s() : cs;
+            if (nf == cf && ns == cs) break;
+            cf = nf;
+            cs = ns;
+          }
+          means(cf, cs);
+        }
       }
-      sum_threads<TH, LANES>(v, sh, place);
-      if (a.post) fdev = 1.0f / sqrtf(v[0] * inv + a.eps);
-      if (a.pre) { sdev = 1.0f / sqrtf(v[1] * inv + a.eps); hs = v[2] * inv * sdev; }
+      if (a.post) fdev = cf * reciprocal(v[0], a.eps, cf);
+      if (a.pre) {
+        const float d = reciprocal(v[1], a.eps, cs);
+        sdev = cs * d;
+        hs = v[2] * d;
+      }
     }
     // ds <- the gradient by S, h <- that by w_pre
     auto by_stream = [&](int i) {
@@ -290,7 +391,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
       for (int j = 0; j < 8; ++j) {
         float d = dS ? ds[k][j] : 0.0f;
         if (a.pre) {
-          const float sn = (s[k][j] - smean) * sdev, g = h[k][j] * w[j];
+          const float sn = off_s(i, j) * sdev, g = h[k][j] * w[j];
           d += sdev * (g - sn * hs - hmean);
           h[k][j] *= sn;
         }
@@ -308,7 +409,7 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
         t[j] = a.scale * ds[k][j];
         dn[j] = gated ? t[j] * g[j] : t[j];
         if (a.post) {
-          x[k][j] = there((x[k][j] - fmean) * fdev, at(i) + j, q);
+          x[k][j] = off_f(i, j) * fdev;
           t[j] *= x[k][j] * w[j];                                // dgate
           h[k][j] = dn[j] * x[k][j];                             // dw_post
           dn[j] *= w[j];
