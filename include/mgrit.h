@@ -361,7 +361,8 @@ int32_t mgrit_affine_packed_forward(const mgrit_affine_packed_t* p, const void* 
                                     void* Y, void* D, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* The backward pass of an affine layer from activations that were kept in 8 bits: mgrit_affine_backward with X [M][K] and D [M][F]
- * packed as MGRIT_MX8 (a quarter of a float state's memory between the passes, half of a bf16 one's), p->xtype the type of dX alone.
+ * packed as MGRIT_MX8, p->xtype the type of dX alone.  Between the passes a row takes 264 bytes for every 256 columns that it begins: over many columns a
+ * quarter of a float state's memory, half of a bf16 one's; up to 66 columns (bf16: 132, and 257 to 264) no less than the state itself.
  *   G = dY * D~ (D NULL: G = scale dY, for the identity only),  dX = G W,  dW = G^T X~,  db = sum over the rows of G
  * X~ and D~ enter as they are packed, but that values of X~ below 2^-126 are rounded to bf16. */
 size_t  mgrit_affine_kept_workspace_bytes(const mgrit_affine_t* p);

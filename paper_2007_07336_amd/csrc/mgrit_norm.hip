@@ -224,7 +224,7 @@ __global__ __launch_bounds__(TH, TH <= 256 && sizeof(ST) + sizeof(FT) < 8 ? 3 : 
   float cpre[HELD][8] = {}, cpost[HELD][8] = {}, cgate[HELD][8] = {};
   auto at = [&](int i) { return ((long long)i * TH + thread) * 8; };
   // NV = 1: the vectors stay in registers, and the next row is on its way while this one is computed (8192 x 4096 with all of it: one workgroup to a
-  // compute unit, 229 us without, 172 so, 153 with half as many workgroups)
+  // compute unit; of the first form 229 us without, 172 so)
   constexpr bool AHEAD = NV == 1;
   float wpre[8] = {}, wpost[8] = {}, wfeature[8] = {}, wentry[8] = {};
   Raw8<FT> nf = {}, nY = {}, ng = {};
@@ -517,8 +517,8 @@ __global__ __launch_bounds__(1024) void norm_columns_kernel(ColumnSums sums, int
 }
 
 // Threads of a row, and workgroups of the backward pass: about 2048 wavefronts, which is what the compute units hold at once, and two rows each at least.  Their
-// columns' sums are written and read once more (us with 256 / 512 / 1024 / 2048 workgroups: 8192 x 4096 170 / 171 / 185 / -, 4000 x 1024 61 / 42 / 44 / -,
-// 20000 x 300 309 / 170 / 97 / 62).
+// columns' sums are written and read once more (whole calls, us with 256 / 512 / 1024 / 2048 workgroups: 8192 x 4096 154 / 159 / 169 / 189, 2000 x 8192
+// 133 / 142 / 162 / 208, 4000 x 1024 56 / 41 / 45 / 52, 20000 x 300 345 / 198 / 117 / 79, 21806 x 52 46 / 31 / 22 / 22).
 inline int threads_of(long long q) { return q <= 512 ? 64 : q <= 2048 ? 256 : q <= 8192 ? 512 : 1024; }
 inline int lanes_of(long long q) { return q <= 64 ? 8 : q <= 128 ? 16 : q <= 256 ? 32 : 64; }
 int groups_of(const BlockNormArgs& a) {
