@@ -206,9 +206,8 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
 // d (h - x^ mean(h x^)), with MGRIT_NORM_LAYER less mean(h) inside the brackets too.  A workgroup takes the rows b, b + G, .. and keeps the columns' sums
 // of its rows in registers; they go to part[array][b][q] and are added up by a second launch.
 struct ColumnSums { float* part[3]; };                           // of dw_pre, dw_post, dgate; null where not wanted
-// (a wavefront less on each SIMD where float arrays take two registers an entry anyway)
 template <typename ST, typename FT, int TH, int NV, int LANES>
-__global__ __launch_bounds__(TH, TH <= 256 && sizeof(ST) + sizeof(FT) < 8 ? 3 : 1) void norm_backward_kernel(BlockNormArgs a, ColumnSums sums) {
+__global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, ColumnSums sums) {
   __shared__ float sh[2][TH / 64][4];
   int place = 0;
   const long long q = a.q;
@@ -345,7 +344,16 @@ __global__ __launch_bounds__(TH, TH <= 256 && sizeof(ST) + sizeof(FT) < 8 ? 3 : 
       float cf = 1.0f, cs = 1.0f;
       auto scale_f = [&]() { return a.post ? squares_scale(v[0], a.eps) : 1.0f; };
       auto scale_s = [&]() { return a.pre ? squares_scale(v[1], a.eps) : 1.0f; };
-      if (__builtin_expect(far_off(fmean, v[0]) || far_off(smean, v[1]) || scale_f() != 1.0f || scale_s() != 1.0f, 0)) {
+      auto deviations = [&]() {
+        if (a.post) fdev = cf * reciprocal(v[0], a.eps, cf);
+        if (a.pre) {
+          const float d = reciprocal(v[1], a.eps, cs);
+          sdev = cs * d;
+          hs = v[2] * d;
+        }
+      };
+      deviations();
+      if (__builtin_expect((a.layer && (far_off(fmean, v[0]) || far_off(smean, v[1]))) || scale_f() != 1.0f || scale_s() != 1.0f, 0)) {
         float fm = fmean, sm = smean;
         for (int again = 0; again < 6; ++again) {                // (as in `deviation`)
           if (far_off(fm * cf, v[0]) || far_off(sm * cs, v[1])) {
@@ -374,12 +382,7 @@ __global__ __launch_bounds__(TH, TH <= 256 && sizeof(ST) + sizeof(FT) < 8 ? 3 : 
           }
           means(cf, cs);
         }
-      }
-      if (a.post) fdev = cf * reciprocal(v[0], a.eps, cf);
-      if (a.pre) {
-        const float d = reciprocal(v[1], a.eps, cs);
-        sdev = cs * d;
-        hs = v[2] * d;
+        deviations();
       }
     }
     // ds <- the gradient by S, h <- that by w_pre
