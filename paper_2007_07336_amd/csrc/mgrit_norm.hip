@@ -31,12 +31,8 @@ template <int TH, int LANES, int N> __device__ __forceinline__ void sum_threads(
 // Deviations from a mean that is far larger than they are: as a float that is a few ulps off, which may be as much as a deviation (of 10000.1 in each of 500 features
 // an ulp or two: 0.89 of a deviation with eps = 1e-6).  The deviations have few bits, so their mean is exact, or nearly, and is taken off them: nothing at all is left
 // where the entries are all the same.
-constexpr float LESS = 0x1p-24f;                                 // entries are summed times this: of the largest floats no sum overflows
-// The mean, a float for everyone: where the compiler takes the product into a subtraction it is not rounded, and deviations of one entry and another are from two means
-__device__ __forceinline__ float mean_of(float sum, float inv) {
-#pragma clang fp contract(off)
-  return sum * (inv * (1.0f / LESS));
-}
+// (Means are sums of entries times 1 / q: those of the largest floats do not overflow, those of the smallest lose half of 2^-149 an addition.  And no product that the
+// compiler might take into a subtraction, where it would not be rounded, and the deviations of one entry and another would be from two means.)
 __device__ __forceinline__ bool far_off(float mean, float m) { return mean * mean > 64.0f * m; }
 // Deviations whose squares no float holds, or with few bits: what they are multiplied by before they are squared, 1 for most
 __device__ __forceinline__ float squares_scale(float m, float eps) { return !(m < 0x1p100f) ? 0x1p-80f : m + eps < 0x1p-90f ? 0x1p96f : 1.0f; }
@@ -127,10 +123,10 @@ __global__ __launch_bounds__(TH) void norm_forward_kernel(BlockNormArgs a, long 
       for (int i = 0; i < n; ++i) {
         read(i);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] = __builtin_fmaf(NV ? v[NV ? i : 0][j] : there(v[0][j], at(i) + j, q), LESS, s[0]);
+        for (int j = 0; j < 8; ++j) s[0] = __builtin_fmaf(NV ? v[NV ? i : 0][j] : there(v[0][j], at(i) + j, q), inv, s[0]);
       }
       sum_threads<TH, LANES>(s, sh, place);
-      mean = mean_of(s[0], inv);
+      mean = s[0];
       take_off(mean);
     }
     auto off = [&](int i, int j) { return NV ? v[NV ? i : 0][j] : there(v[0][j] - mean - less, at(i) + j, q); };
@@ -304,13 +300,13 @@ __global__ __launch_bounds__(TH) void norm_backward_kernel(BlockNormArgs a, Colu
         get_pre(i, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          v[0] = __builtin_fmaf(x[k][j], LESS, v[0]);
-          if (a.pre) { v[1] = __builtin_fmaf(s[k][j], LESS, v[1]); v[2] = __builtin_fmaf(h[k][j], w[j], v[2]); }
+          v[0] = __builtin_fmaf(x[k][j], inv, v[0]);
+          if (a.pre) { v[1] = __builtin_fmaf(s[k][j], inv, v[1]); v[2] = __builtin_fmaf(h[k][j], w[j], v[2]); }
         }
       }
       sum_threads<TH, LANES>(v, sh, place);
-      if (a.post) fmean = mean_of(v[0], inv);
-      if (a.pre) smean = mean_of(v[1], inv);
+      if (a.post) fmean = v[0];
+      if (a.pre) smean = v[1];
       hmean = v[2] * inv;
       take_off(fmean, smean);
     }

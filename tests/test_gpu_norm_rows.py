@@ -103,3 +103,24 @@ def test_rows_whose_squares_no_float_holds(q, kind, size):
     assert torch.equal(want["dpre"], got["dpre"])
     if s > 1:
         near(got["dr"], want["dr"].double() / s, 2.0 ** -126, ("dr", q))
+
+
+@pytest.mark.parametrize("q", SIZES[1:])
+@pytest.mark.parametrize("size", [-90, -105, -113])
+def test_rows_of_the_smallest_floats(q, size):
+    """Entries of 2^-113: those near zero have few bits, and their mean keeps what there is."""
+    b = Block(4, q, "layer", "none", "ff", pre=False, eps=0.0, scale=1.0, seed=q)
+    b.f.copy_(0.5 + b.f).mul_(2.0 ** size)
+    b.r.zero_()
+    b.post.fill_(1.0)
+    S, _ = b.forward()
+    x = b.f.double() * 2.0 ** -size                                # (in 64 bits and so in their own)
+    want, dev = norm_of(x, "layer", 0.0)
+    # a step for each addition of the longest chain and four more, of the deviations' magnitudes (see above); half of 2^-149 for each addition of all, the mean and a
+    # difference to it
+    mean = lambda t: t.mean(1, keepdim=True)                                                       # noqa: E731
+    off = (serial(q) + 4) * 2.0 ** -24 * (mean(want.abs()) + want.abs().max(1, keepdim=True).values + mean(x.abs()) * dev) + (q + 100) * 2.0 ** (-150 - size) * dev
+    near(S, want, (serial(q) + 8) * 2.0 ** -24 * want.abs() + off * (1.0 + want.abs()), ("S", q))
+    got = b.backward(S)
+    # df is beyond the largest float here; dpost is a sum of dS x^
+    near(got["dpost"], (b.dS.double() * want).sum(0), (b.dS.double().abs() * (off * (1.0 + want.abs()) + (serial(q) + 14) * 2.0 ** -24 * want.abs())).sum(0), ("dpost", q))
